@@ -376,6 +376,79 @@ voxzip_status voxzip_evict_paged(const voxzip_cache_desc *desc, const voxzip_pag
                                  voxzip_stream_t stream);
 
 /*
+ * Cache held in 4 bits: K and V rows of 4.5 bits per channel, against 16 or 32.
+ *
+ * A row of D channels is D / 32 groups of 32 consecutive channels, each with a bf16 scale s, and a 4-bit code
+ * c + 8 (c in [-8, 7]) per channel. A channel stands for c s in V and for c s 2^e in K, where e is an exponent
+ * kept per unit and channel: channels of K that are much larger than the others, as attention keys have, would
+ * otherwise leave the rest of their group without codes.
+ *   s = bf16(x_m / -8), x_m the group's element of largest magnitude (the positive one on a tie; for K of
+ *       x = k 2^-e). s = 0 if that is below the smallest normal number; a group with an infinity or a NaN has
+ *       s = NaN and reads back as NaN.
+ *   c = rint(x (1 / s)) clamped to [-8, 7], in fp32; 0 where s is 0 or NaN.
+ *   e   set by voxzip_q4_pack, in [-16, 16]; a cache that was never packed into holds zeros here.
+ *   K codes: 4-byte word q (D / 32) + j of a row (q = 0..3) holds channels 32 j + 8 q + i, i = 0..7, channel i at
+ *   nibble i / 2 + 4 (i % 2). V codes: 2-byte word g (D / 32) + j (g = 0..7) holds channels 32 j + 4 g + i,
+ *   i = 0..3, channel i at nibble i.
+ * Scores, positions and lengths are those of the cache layout above. The descriptor's dtype is that of q, k_new,
+ * v_new, out and of the rows packed and read back; its capacity is a multiple of VOXZIP_Q4_CAPACITY_MULTIPLE.
+ * The arrays are caller-owned device memory, 16-byte aligned. A cache of zero bytes with len = 0 is empty and
+ * ready for decode steps; stage 1 runs into a cache of rows (its score, pos and len may be this cache's own),
+ * which voxzip_q4_pack then packs.
+ */
+#define VOXZIP_Q4_CAPACITY_MULTIPLE 4
+
+typedef struct {
+    void *k_codes;  /* [B][L][Hkv][C][D/2] bytes */
+    void *v_codes;  /* [B][L][Hkv][C][D/2] bytes */
+    void *k_scale;  /* [B][L][Hkv][C][D/32] bf16 */
+    void *v_scale;  /* [B][L][Hkv][C][D/32] bf16 */
+    int8_t *k_exp;  /* [B][L][Hkv][D] */
+} voxzip_q4_cache;
+
+/*
+ * Packs rows [0, len) of every unit of layers [layer_begin, layer_begin + layer_count) and sets the units'
+ * channel exponents: with a_d the largest |k| of channel d over those rows and m the lower median of the a_d, e is
+ * floor(log2((a_d / m) sqrt 2)) in fp32, clamped (0 where a_d or m is 0 or not finite, or the unit is empty).
+ *   k_cache, v_cache  [B][L][Hkv][C][D] in the descriptor's dtype, 16-byte aligned
+ *   len               [B][L][Hkv] device int32, read
+ * Slots from len on are neither read nor written. Device errors: VOXZIP_DEV_CAPACITY (a length outside [0, C]; the
+ * unit is skipped).
+ */
+voxzip_status voxzip_q4_pack(const voxzip_cache_desc *desc, const voxzip_q4_cache *q4, int32_t layer_begin,
+                             int32_t layer_count, const void *k_cache, const void *v_cache, const int32_t *len,
+                             voxzip_stream_t stream);
+
+/*
+ * Reads rows back as the values they stand for, rounded once to the descriptor's dtype: output row r of a unit of
+ * length n is slot first + r, or slot n + first + r if first < 0 (-1: the row appended last); zeros where that
+ * lies outside [0, n).
+ *   k_out, v_out  [B][layer_count][Hkv][rows][D], 16-byte aligned; rows >= 1
+ * Device errors: VOXZIP_DEV_CAPACITY (a length outside [0, C]; the unit's output is not written).
+ */
+voxzip_status voxzip_q4_unpack(const voxzip_cache_desc *desc, const voxzip_q4_cache *q4, int32_t layer_begin,
+                               int32_t layer_count, const int32_t *len, int32_t first, int32_t rows, void *k_out,
+                               void *v_out, voxzip_stream_t stream);
+
+/*
+ * voxzip_decode_step on a cache held in 4 bits: the new row is packed (under the unit's channel exponents) into slot
+ * n and takes part in the attention as packed. Attention, scores and errors are those of voxzip_decode_step, on the
+ * values the rows stand for, at any length up to the capacity.
+ *
+ * Range: the tensor-core products carry powers of two that keep every code exact; |q 2^e| and the scales of V must
+ * lie below 2^40, and magnitudes below 2^-60 count as zero there.
+ */
+voxzip_status voxzip_decode_step_q4(const voxzip_cache_desc *desc, const voxzip_q4_cache *q4, int32_t layer_begin,
+                                    int32_t layer_count, const void *q, const void *k_new, const void *v_new,
+                                    const int32_t *new_pos, float *score, int32_t *pos, int32_t *len, float gamma,
+                                    float sm_scale, int32_t max_len, void *out, voxzip_stream_t stream);
+
+/* voxzip_evict_ex on a cache held in 4 bits: rows move as packed, so no value changes. */
+voxzip_status voxzip_evict_q4(const voxzip_cache_desc *desc, const voxzip_q4_cache *q4, int32_t layer_begin,
+                              int32_t layer_count, float *score, int32_t *pos, int32_t *len, const int32_t *budget,
+                              const voxzip_evict_policy *policy, voxzip_stream_t stream);
+
+/*
  * Waits for `stream`, then returns the device status word of the current device in *bits
  * (VOXZIP_DEV_* flags accumulated by earlier calls) and clears it.
  */

@@ -72,6 +72,11 @@ class CacheDesc:
         return self._slots + (self.head_dim,)
 
     @functools.cached_property
+    def _q4_shapes(self):
+        """Of a cache held in 4 bits: its codes, its scales."""
+        return self._slots + (self.head_dim // 2,), self._slots + (self.head_dim // Q4_GROUP,)
+
+    @functools.cached_property
     def _c(self):
         """The binding's own C struct (never handed out: c_struct makes a new one)."""
         return self.c_struct()
@@ -114,7 +119,13 @@ class _Paged(ctypes.Structure):
                 ("max_pages", ctypes.c_int32)]
 
 
+class _Q4(ctypes.Structure):
+    _fields_ = [("k_codes", ctypes.c_void_p), ("v_codes", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("k_exp", ctypes.c_void_p)]
+
+
 PAGE_TOKENS = 64
+Q4_CAPACITY_MULTIPLE, Q4_GROUP = 4, 32
 
 _lock = threading.Lock()
 _lib = None
@@ -160,6 +171,12 @@ def lib() -> ctypes.CDLL:
                                                    _f32, _i32, _vp, _vp]
             L.voxzip_evict_paged.argtypes = [_DP, _PP, _i32, _i32, _vp, _vp, _vp, _vp, ctypes.POINTER(_EvictPolicy),
                                              _vp]
+            _QP = ctypes.POINTER(_Q4)
+            L.voxzip_q4_pack.argtypes = [_DP, _QP, _i32, _i32, _vp, _vp, _vp, _vp]
+            L.voxzip_q4_unpack.argtypes = [_DP, _QP, _i32, _i32, _vp, _i32, _i32, _vp, _vp, _vp]
+            L.voxzip_decode_step_q4.argtypes = [_DP, _QP, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _f32, _f32,
+                                                _i32, _vp, _vp]
+            L.voxzip_evict_q4.argtypes = [_DP, _QP, _i32, _i32, _vp, _vp, _vp, _vp, ctypes.POINTER(_EvictPolicy), _vp]
             L.voxzip_selftest_bounded_wait.argtypes = [ctypes.c_uint32, _vp]
             L.voxzip_selftest_bounded_wait.restype = _i32
             L.voxzip_stream_read.argtypes = [_vp, _sz, _vp, _vp]
@@ -175,7 +192,8 @@ def lib() -> ctypes.CDLL:
             L.voxzip_version.restype = _i32
             for f in (L.voxzip_anchor_fuse, L.voxzip_decode_step, L.voxzip_evict, L.voxzip_get_status,
                       L.voxzip_segments_to_spans, L.voxzip_embed_fuse, L.voxzip_evict_ex, L.voxzip_paged_init,
-                      L.voxzip_anchor_fuse_paged, L.voxzip_decode_step_paged, L.voxzip_evict_paged):
+                      L.voxzip_anchor_fuse_paged, L.voxzip_decode_step_paged, L.voxzip_evict_paged, L.voxzip_q4_pack,
+                      L.voxzip_q4_unpack, L.voxzip_decode_step_q4, L.voxzip_evict_q4):
                 f.restype = _i32
             _lib = L
     return _lib
@@ -552,6 +570,103 @@ def voxzip_evict_ex(desc: CacheDesc, layer_begin: int, layer_count: int, k_cache
     _check("voxzip_evict_ex", lib().voxzip_evict_ex(
         ctypes.byref(d), int(layer_begin), int(layer_count), _ptr(k_cache), _ptr(v_cache), _ptr(score), _ptr(pos),
         _ptr(len_), _ptr(budget), ctypes.byref(pol), _stream(stream)))
+
+
+def allocate_q4_cache(desc: CacheDesc, device="cuda"):
+    """An empty cache held in 4 bits: codes, scales and channel exponents of K and V, and the score, pos and len of
+    a dense cache (zero-filled). desc.capacity is a multiple of 4; desc.dtype is that of the rows packed into it and
+    of the decode steps' tensors."""
+    if desc.capacity % Q4_CAPACITY_MULTIPLE:
+        raise ValueError("the capacity of a cache held in 4 bits must be a multiple of 4")
+    cs = (desc.batch, desc.layers, desc.kv_heads, desc.capacity)
+    D = desc.head_dim
+    return dict(k_codes=torch.zeros(cs + (D // 2,), dtype=torch.uint8, device=device),
+                v_codes=torch.zeros(cs + (D // 2,), dtype=torch.uint8, device=device),
+                k_scale=torch.zeros(cs + (D // Q4_GROUP,), dtype=torch.bfloat16, device=device),
+                v_scale=torch.zeros(cs + (D // Q4_GROUP,), dtype=torch.bfloat16, device=device),
+                k_exp=torch.zeros(cs[:3] + (D,), dtype=torch.int8, device=device),
+                score=torch.zeros(cs, dtype=torch.float32, device=device),
+                pos=torch.zeros(cs, dtype=torch.int32, device=device),
+                len=torch.zeros(cs[:3], dtype=torch.int32, device=device))
+
+
+def _q4_struct(desc: CacheDesc, qc) -> _Q4:
+    codes, scales = desc._q4_shapes
+    k_codes, v_codes, k_scale, v_scale, k_exp = (qc["k_codes"], qc["v_codes"], qc["k_scale"], qc["v_scale"],
+                                                 qc["k_exp"])
+    _need(k_codes, "k_codes", torch.uint8, codes)
+    _need(v_codes, "v_codes", torch.uint8, codes)
+    _need(k_scale, "k_scale", torch.bfloat16, scales)
+    _need(v_scale, "v_scale", torch.bfloat16, scales)
+    _need(k_exp, "k_exp", torch.int8, desc._units + (desc.head_dim,))
+    return _Q4(k_codes.data_ptr(), v_codes.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), k_exp.data_ptr())
+
+
+def voxzip_q4_pack(desc: CacheDesc, qc, layer_begin: int, layer_count: int, k_cache, v_cache, *, stream=None) -> None:
+    """Packs rows [0, len) of a cache's units (k_cache, v_cache as for voxzip_decode_step; the lengths are
+    qc["len"]) into 4 bits and sets the channel exponents of K."""
+    _need(k_cache, "k_cache", desc.dtype, desc._rows)
+    _need(v_cache, "v_cache", desc.dtype, desc._rows)
+    _need(qc["len"], "len", torch.int32, desc._units)
+    qs = _q4_struct(desc, qc)
+    _check("voxzip_q4_pack", lib().voxzip_q4_pack(
+        ctypes.byref(desc._c), ctypes.byref(qs), int(layer_begin), int(layer_count), _ptr(k_cache), _ptr(v_cache),
+        _ptr(qc["len"]), _stream(stream)))
+
+
+def voxzip_q4_unpack(desc: CacheDesc, qc, layer_begin: int, layer_count: int, k_out, v_out, *, first: int = 0,
+                     stream=None) -> None:
+    """Reads rows of a cache held in 4 bits back as values: k_out and v_out are [B][layer_count][Hkv][rows][D], row r
+    is slot first + r (from the unit's end if first < 0: -1 is the row appended last), zeros where there is none."""
+    if k_out.dim() != 5:
+        raise ValueError("k_out must be [B][layer_count][Hkv][rows][D]")
+    rows = k_out.shape[3]
+    shape = (desc.batch, layer_count, desc.kv_heads, rows, desc.head_dim)
+    _need(k_out, "k_out", desc.dtype, shape)
+    _need(v_out, "v_out", desc.dtype, shape)
+    _need(qc["len"], "len", torch.int32, desc._units)
+    qs = _q4_struct(desc, qc)
+    _check("voxzip_q4_unpack", lib().voxzip_q4_unpack(
+        ctypes.byref(desc._c), ctypes.byref(qs), int(layer_begin), int(layer_count), _ptr(qc["len"]), int(first),
+        int(rows), _ptr(k_out), _ptr(v_out), _stream(stream)))
+
+
+def voxzip_decode_step_q4(desc: CacheDesc, qc, layer_begin: int, layer_count: int, q, k_new, v_new, new_pos,
+                          gamma: float, out, *, sm_scale: float = 0.0, max_len: int = 0, stream=None) -> None:
+    """One decode step (Eq. 1, Eq. 2, Eq. 6) on a cache held in 4 bits; the new row is packed as it is appended."""
+    B, Hq, H, D = desc.batch, desc.q_heads, desc.kv_heads, desc.head_dim
+    _need(q, "q", desc.dtype, (layer_count, B, Hq, D))
+    _need(k_new, "k_new", desc.dtype, (layer_count, B, H, D))
+    _need(v_new, "v_new", desc.dtype, (layer_count, B, H, D))
+    _need(out, "out", desc.dtype, (layer_count, B, Hq, D))
+    _need(new_pos, "new_pos", torch.int32, (B,))
+    score, pos, len_ = qc["score"], qc["pos"], qc["len"]
+    _check_dense_state(desc, score, pos, len_)
+    qs = _q4_struct(desc, qc)
+    _check("voxzip_decode_step_q4", lib().voxzip_decode_step_q4(
+        ctypes.byref(desc._c), ctypes.byref(qs), int(layer_begin), int(layer_count), _ptr(q), _ptr(k_new), _ptr(v_new),
+        _ptr(new_pos), _ptr(score), _ptr(pos), _ptr(len_), float(gamma), float(sm_scale), int(max_len), _ptr(out),
+        _stream(stream)))
+
+
+def voxzip_evict_q4(desc: CacheDesc, qc, layer_begin: int, layer_count: int, budget, *, sink: int = 4,
+                    recent_frac: float = 0.2, history: bool = True, compaction: str = "ordered", stream=None) -> None:
+    """Eviction (Eq. 7-9, under a policy as voxzip_evict_ex) from a cache held in 4 bits."""
+    _check_dense_state(desc, qc["score"], qc["pos"], qc["len"])
+    if budget.dim() == 1:
+        _need(budget, "budget", torch.int32, (desc.batch,))
+        sb, sl = 1, 0
+    else:
+        _need(budget, "budget", torch.int32, (desc.batch, desc.layers))
+        sb, sl = desc.layers, 1
+    if compaction not in ("ordered", "fill"):
+        raise ValueError("compaction must be 'ordered' or 'fill'")
+    pol = _EvictPolicy(int(sink), float(recent_frac), int(bool(history)), sb, sl,
+                       VOXZIP_COMPACT_FILL if compaction == "fill" else VOXZIP_COMPACT_ORDERED)
+    qs = _q4_struct(desc, qc)
+    _check("voxzip_evict_q4", lib().voxzip_evict_q4(
+        ctypes.byref(desc._c), ctypes.byref(qs), int(layer_begin), int(layer_count), _ptr(qc["score"]),
+        _ptr(qc["pos"]), _ptr(qc["len"]), _ptr(budget), ctypes.byref(pol), _stream(stream)))
 
 
 def voxzip_selftest_bounded_wait(limit: int = 1000, stream=None) -> None:
