@@ -433,7 +433,7 @@ voxzip_status voxzip_q4_unpack(const voxzip_cache_desc *desc, const voxzip_q4_ca
 /*
  * voxzip_decode_step on a cache held in 4 bits: the new row is packed (under the unit's channel exponents) into slot
  * n and takes part in the attention as packed. Attention, scores and errors are those of voxzip_decode_step, on the
- * values the rows stand for, at any length up to the capacity.
+ * values the rows stand for, at any length up to the capacity. score is 16-byte aligned.
  *
  * Range: the tensor-core products carry powers of two that keep every code exact; |q 2^e| and the scales of V must
  * lie below 2^40, and magnitudes below 2^-60 count as zero there.

@@ -81,7 +81,8 @@ voxzip_status voxzip_decode_step_q4(const voxzip_cache_desc *desc, const voxzip_
     if (!cache_ok(desc, q4) || !layers_ok(*desc, layer_begin, layer_count)) return VOXZIP_EINVAL;
     if (!q || !k_new || !v_new || !new_pos || !score || !pos || !len || !out) return VOXZIP_EINVAL;
     if (!(gamma > 0.f && gamma <= 1.f) || isnan(sm_scale) || isinf(sm_scale)) return VOXZIP_EINVAL;
-    if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(out)) return VOXZIP_EINVAL;
+    if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(out) || !aligned16(score))
+        return VOXZIP_EINVAL;
     if (desc->q_heads / desc->kv_heads > voxzip::kMaxGroup) return VOXZIP_EUNSUPPORTED;
     if (!units_ok(*desc, layer_count)) return VOXZIP_EUNSUPPORTED;
     int32_t *status = nullptr;

@@ -1,4 +1,5 @@
-// Decode step on a cache held in 4 bits (format: q4.cuh): append, GQA attention and the decayed-score update.
+// Decode step on a cache held in 4 bits, for lengths whose logits no cluster of CTAs can hold in shared memory
+// (see decode_q4_mma.cu): append, GQA attention and the decayed-score update (format: q4.cuh).
 #include "q4.cuh"
 
 namespace voxzip {
@@ -54,9 +55,9 @@ __global__ void __launch_bounds__(kThreads) decode_q4_rows_kernel(const DecodeQ4
             }
         }
         if (warp == 0)
-            q4_store_row<D, true>(x, p.q4.k_codes, p.q4.k_scale, row_base + n_old, true);
+            Q4Row<D, true>(x).store(p.q4.k_codes + (row_base + n_old) * (D / 2), p.q4.k_scale + (row_base + n_old) * J);
         else
-            q4_store_row<D, false>(x, p.q4.v_codes, p.q4.v_scale, row_base + n_old, true);
+            Q4Row<D, false>(x).store(p.q4.v_codes + (row_base + n_old) * (D / 2), p.q4.v_scale + (row_base + n_old) * J);
     }
     if (tid == 0) p.pos[row_base + n_old] = p.new_pos[ui.b];
     __syncthreads();
@@ -171,7 +172,7 @@ __global__ void __launch_bounds__(kThreads) decode_q4_rows_kernel(const DecodeQ4
 
 }  // namespace
 
-cudaError_t launch_decode_q4(const voxzip_cache_desc &d, const Q4View &q4, int32_t layer_begin, int32_t layer_count,
+cudaError_t launch_decode_q4_rows(const voxzip_cache_desc &d, const Q4View &q4, int32_t layer_begin, int32_t layer_count,
                              const void *q, const void *k_new, const void *v_new, const int32_t *new_pos, float *score,
                              int32_t *pos, int32_t *len, float gamma, float sm_scale, int32_t max_len, void *out,
                              int32_t *status, cudaStream_t stream) {

@@ -60,32 +60,40 @@ __device__ __forceinline__ uint32_t q4_code(float x, float inv) {
 }
 __device__ __forceinline__ float q4_inverse(float s) { return s != 0.f && s == s ? __frcp_rn(s) : 0.f; }
 
-// One row, lane l of the first D / 4 lanes holding channels 4 l .. 4 l + 3 as x (for K already times 2^-e).
-// Stores codes and scales at row `row` of the unit-major arrays. All 32 lanes call it; lanes past D / 4 and
-// lanes with on = false hold zeros and store nothing.
+// A row packed by a warp: lane l of the first D / 4 lanes holds channels 4 l .. 4 l + 3 (for K already times 2^-e);
+// the other lanes hold zeros. All 32 lanes make it; store() may then be called with any row of either memory.
 template <int D, bool kIsK>
-__device__ __forceinline__ void q4_store_row(const float4 &x, uint8_t *codes, __nv_bfloat16 *scales, int64_t row,
-                                             bool on) {
-    constexpr int J = D / kQ4Group;
-    const int lane = threadIdx.x & 31;
-    uint32_t key = max(max(magnitude_key(x.x), magnitude_key(x.y)), max(magnitude_key(x.z), magnitude_key(x.w)));
+struct Q4Row {
+    static constexpr int J = D / kQ4Group;
+    uint32_t bits;  // K: a word, the same in lanes 2 i and 2 i + 1; V: a half-word
+    __nv_bfloat16 scale;
+
+    __device__ __forceinline__ explicit Q4Row(const float4 &x) {
+        uint32_t key = max(max(magnitude_key(x.x), magnitude_key(x.y)), max(magnitude_key(x.z), magnitude_key(x.w)));
 #pragma unroll
-    for (int o = 1; o < 8; o <<= 1) key = max(key, __shfl_xor_sync(0xffffffffu, key, o));
-    const float s = q4_scale(key), inv = q4_inverse(s);
-    const uint32_t n0 = q4_code(x.x, inv), n1 = q4_code(x.y, inv), n2 = q4_code(x.z, inv), n3 = q4_code(x.w, inv);
-    const int j = lane >> 3;
-    on = on && lane < D / 4;
-    if constexpr (kIsK) {
-        const uint32_t part = (n0 | n1 << 16 | n2 << 4 | n3 << 20) << ((lane & 1) * 8);
-        const uint32_t word = part | __shfl_xor_sync(0xffffffffu, part, 1);
-        if (on && !(lane & 1)) reinterpret_cast<uint32_t *>(codes + row * (D / 2))[((lane >> 1) & 3) * J + j] = word;
-    } else {
-        if (on)
-            reinterpret_cast<uint16_t *>(codes + row * (D / 2))[(lane & 7) * J + j] =
-                (uint16_t)(n0 | n1 << 4 | n2 << 8 | n3 << 12);
+        for (int o = 1; o < 8; o <<= 1) key = max(key, __shfl_xor_sync(0xffffffffu, key, o));
+        const float s = q4_scale(key), inv = q4_inverse(s);
+        scale = __float2bfloat16_rn(s);
+        const uint32_t n0 = q4_code(x.x, inv), n1 = q4_code(x.y, inv), n2 = q4_code(x.z, inv), n3 = q4_code(x.w, inv);
+        if constexpr (kIsK) {
+            bits = (n0 | n1 << 16 | n2 << 4 | n3 << 20) << ((threadIdx.x & 1) * 8);
+            bits |= __shfl_xor_sync(0xffffffffu, bits, 1);
+        } else {
+            bits = n0 | n1 << 4 | n2 << 8 | n3 << 12;
+        }
     }
-    if (on && (lane & 7) == 0) scales[row * J + j] = __float2bfloat16_rn(s);
-}
+    // codes, scales: the row's own D / 2 bytes and J scales.
+    __device__ __forceinline__ void store(uint8_t *codes, __nv_bfloat16 *scales) const {
+        const int lane = threadIdx.x & 31, j = lane >> 3;
+        if (lane >= D / 4) return;
+        if constexpr (kIsK) {
+            if (!(lane & 1)) reinterpret_cast<uint32_t *>(codes)[((lane >> 1) & 3) * J + j] = bits;
+        } else {
+            reinterpret_cast<uint16_t *>(codes)[(lane & 7) * J + j] = (uint16_t)bits;
+        }
+        if ((lane & 7) == 0) scales[j] = scale;
+    }
+};
 
 // Host-side launchers.
 cudaError_t launch_q4_pack(const voxzip_cache_desc &d, const Q4View &q4, int32_t layer_begin, int32_t layer_count,
@@ -98,6 +106,10 @@ cudaError_t launch_decode_q4(const voxzip_cache_desc &d, const Q4View &q4, int32
                              const void *q, const void *k_new, const void *v_new, const int32_t *new_pos, float *score,
                              int32_t *pos, int32_t *len, float gamma, float sm_scale, int32_t max_len, void *out,
                              int32_t *status, cudaStream_t stream);
+cudaError_t launch_decode_q4_rows(const voxzip_cache_desc &d, const Q4View &q4, int32_t layer_begin,
+                                  int32_t layer_count, const void *q, const void *k_new, const void *v_new,
+                                  const int32_t *new_pos, float *score, int32_t *pos, int32_t *len, float gamma,
+                                  float sm_scale, int32_t max_len, void *out, int32_t *status, cudaStream_t stream);
 cudaError_t launch_evict_q4(const voxzip_cache_desc &d, const Q4View &q4, int32_t layer_begin, int32_t layer_count,
                             float *score, int32_t *pos, int32_t *len, const int32_t *budget,
                             const voxzip_evict_policy &policy, int32_t *status, cudaStream_t stream);

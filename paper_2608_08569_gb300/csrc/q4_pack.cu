@@ -76,8 +76,8 @@ __global__ void __launch_bounds__(kThreads) q4_pack_kernel(const PackParams p) {
             x.x *= f.x, x.y *= f.y, x.z *= f.z, x.w *= f.w;
         }
         const int64_t row = ui.cache_unit * p.C + r;
-        q4_store_row<D, true>(x, p.q4.k_codes, p.q4.k_scale, row, true);
-        q4_store_row<D, false>(y, p.q4.v_codes, p.q4.v_scale, row, true);
+        Q4Row<D, true>(x).store(p.q4.k_codes + row * (D / 2), p.q4.k_scale + row * (D / kQ4Group));
+        Q4Row<D, false>(y).store(p.q4.v_codes + row * (D / 2), p.q4.v_scale + row * (D / kQ4Group));
     }
 }
 

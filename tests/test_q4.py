@@ -68,6 +68,8 @@ def test_bad_arguments_are_einval(V):
     assert _calls(V, d, q, len=None) == [1] * 4
     assert _calls(V, d, q, p=ctypes.c_void_p(260))[:3] == [1] * 3  # misaligned rows
     assert _calls(V, d, q, rows=0)[1] == 1
+    assert V.lib().voxzip_decode_step_q4(ctypes.byref(d), ctypes.byref(q), 0, 1, P, P, P, P, ctypes.c_void_p(260), P, P, 0.9,
+                                         0.0, 0, P, None) == 1  # misaligned scores
     for g in (0.0, -1.0, 1.5, float("nan")):
         assert _calls(V, d, q, gamma=g)[2] == 1
     for s in (float("nan"), float("inf")):
