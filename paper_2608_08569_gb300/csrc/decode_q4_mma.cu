@@ -16,8 +16,9 @@
 //
 // Grid: S CTAs per (layer, sequence, kv-head) unit, a thread-block cluster where S > 1; CTA r owns a run of 32-token
 // tiles, and its warp w every fourth of them. Every warp streams its own K tiles and then its V tiles through a ring
-// of its own, filled by bulk copies that its lane 0 issues, so nothing in the streaming waits for another warp: the
-// weights are taken relative to the warp's own maximum. The logits, then the weights, stay in shared memory until
+// of its own (cp.async by all lanes: bulk copies issued by one lane, with their barriers, cost four times the
+// instructions per tile), so nothing in the streaming waits for another warp: the weights are taken relative to the
+// warp's own maximum. The logits, then the weights, stay in shared memory until
 // the unit's maximum and normaliser are known (a sum over warps, then over the cluster through distributed shared
 // memory), when each warp rewrites the scores of its own tokens.
 #include <cooperative_groups.h>
@@ -31,17 +32,14 @@ namespace cg = cooperative_groups;
 namespace voxzip {
 namespace {
 
-#ifndef VOXZIP_Q4_WP
-#define VOXZIP_Q4_WP 2
-#endif
 constexpr int kWarps = 4;
 constexpr int kThreads = kWarps * 32;
 constexpr int kTile = 32;   // tokens per stage
-constexpr int kStages = 4;  // of a warp's ring
+constexpr int kMaxStages = 3;  // of a warp's ring: two, or three where they do not cost the SM a CTA
 constexpr int kMaxCluster = 16;
 constexpr size_t kMaxSmem = 227 * 1024;
-constexpr uint32_t kWaitLimit = 1u << 24;
 constexpr float kCarry = 0x1p84f, kUncarry = 0x1p49f;
+constexpr float kLeast = -3.402823466e38f;
 
 struct MmaQ4Params {
     Q4View q4;
@@ -51,7 +49,10 @@ struct MmaQ4Params {
     int32_t *pos, *len;
     void *out;
     int32_t *status;
-    int32_t B, L, Hq, Hkv, G, C, layer_begin, S, chunk_cap, max_rows;
+    int32_t B, L, Hq, Hkv, G, C, layer_begin, chunk_cap, max_rows;
+    int32_t S, stages, slice;               // CTAs per unit; each writes this many float4 of its G D outputs
+    int32_t next_h, next_b, next_l; // how far the unit lies whose CTAs take these ones' place (next_l < 0: none)
+    uint32_t inv_s, inv_slice;      // ceil(2^32 / S), ceil(2^32 / slice): quotients by __umulhi
     float gamma, scale_log2;  // scale_log2: logits in units of log 2, times kUncarry
 };
 
@@ -61,17 +62,26 @@ struct Layout {
     static constexpr int kGP = 8 * NT;
     static constexpr int kCodeBytes = kTile * D / 2;
     static constexpr int kStageBytes = kCodeBytes + kTile * J * 2;
-    static constexpr int kWarpRing = kStages * kStageBytes;
     static constexpr int kOStride = D + 4;  // a warp's outputs take its drained ring: [kGP][kOStride] fp32
-    static_assert(kGP * kOStride * 4 <= kWarpRing, "outputs fit the ring");
-    static constexpr int kBarOff = kWarps * kWarpRing;  // full[kWarps][kStages], the scores' barrier
-    static constexpr int kStatOff = kBarOff + (kWarps * kStages + 2) * 8;
-    // m_w, z_w, f_w [kWarps][kGP]; mz [kGP] and mz_all [kMaxCluster][kGP] pairs
-    static constexpr int kStatFloats = (3 * kWarps + 2 + 2 * kMaxCluster) * kGP;
-    static constexpr int kQOff = kStatOff + kStatFloats * 4;  // fp32: q's operands [parts][NT][2 J][32] pairs
-    static constexpr int kQBytes = kParts == 1 ? 0 : kParts * NT * 2 * J * 32 * 8;
-    static constexpr int kLgOff = kQOff + kQBytes;  // [NT][chunk_cap][8] logits, then weights; [chunk_cap] old scores
-    static size_t bytes(int chunk_cap) { return (size_t)kLgOff + (size_t)chunk_cap * (kGP + 1) * 4; }
+    static constexpr int warp_ring(int stages) { return max(stages * kStageBytes, kGP * kOStride * 4); }
+    // Offsets from the rings' end.
+    static constexpr int kStatOff = 0;
+    static constexpr int kStatFloats = 3 * kWarps * kGP;                 // m_w, z_w, f_w [kWarps][kGP]
+    static constexpr int kScOff = kStatOff + kStatFloats * 4;  // [kWarps][J][kTile] the scales of a V tile
+    static constexpr int kCOff = kScOff + kWarps * J * kTile * 4;  // [NT][J][8] what the accumulators start from
+    // q's operands [parts][NT][2 J][32] pairs, and in their place, once every CTA of the cluster has them in
+    // registers (fp32: beside them), what the cluster's CTAs send: [S][kGP] maxima and sums, [S][slice] float4 of
+    // outputs (S slices cover kGP D).
+    static constexpr int kQOff = kCOff + NT * J * 8 * 4;
+    static constexpr int kQBytes = kParts * NT * 2 * J * 32 * 8;
+    static constexpr int kMzOff = kParts == 1 ? kQOff : kQOff + kQBytes;
+    static constexpr int rx_bytes(int S) { return S * (kGP * 8 + 16) + kGP * D * 4; }
+    static_assert(kParts > 1 || rx_bytes(2) >= kQBytes, "q's operands fit");
+    // [NT][chunk_cap][8] logits, then weights
+    static constexpr int lg_off(int S) { return S > 1 ? kMzOff + rx_bytes(S) : kQOff + kQBytes; }
+    static size_t bytes(int chunk_cap, int S, int stages) {
+        return (size_t)kWarps * warp_ring(stages) + lg_off(S) + (size_t)chunk_cap * kGP * 4;
+    }
 };
 
 __device__ __forceinline__ float fast_exp2(float x) {
@@ -82,25 +92,106 @@ __device__ __forceinline__ float fast_exp2(float x) {
 __device__ __forceinline__ float low_bf16(uint32_t x) { return __uint_as_float(x << 16); }
 __device__ __forceinline__ float high_bf16(uint32_t x) { return __uint_as_float(x & 0xffff0000u); }
 
-// A pair of fp32 values as kParts pairs of bf16 whose sums they are (one part: rounded; three: exactly).
+__device__ __forceinline__ float2 times(float2 a, float2 b) {  // both products in one instruction
+    float2 r;
+    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmul.rn.f32x2 z, x, y;\n\t"
+        "mov.b64 {%0, %1}, z;\n\t}"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+__device__ __forceinline__ float2 less(float2 a, float2 b) {  // a - b, both in one instruction
+    float2 r;
+    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tsub.rn.f32x2 z, x, y;\n\t"
+        "mov.b64 {%0, %1}, z;\n\t}"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+
+// A pair of fp32 values as kParts pairs of bf16: each takes the upper half of what is left (8 bits), one pair
+// alone is rounded. Two leave 2^-15 of a value, three nothing.
 template <int kParts>
-__device__ __forceinline__ void split_pair(float a, float b, uint32_t (&part)[kParts]) {
+__device__ __forceinline__ void split_pair(float2 a, uint32_t (&part)[kParts]) {
+    if constexpr (kParts == 1) {
+        part[0] = ptx::pack_bf16(a.x, a.y);
+    } else {
 #pragma unroll
-    for (int i = 0; i < kParts; ++i) {
-        part[i] = ptx::pack_bf16(a, b);
-        if (i + 1 < kParts) a -= low_bf16(part[i]), b -= high_bf16(part[i]);
+        for (int i = 0; i < kParts; ++i) {
+            part[i] = __byte_perm(__float_as_uint(a.x), __float_as_uint(a.y), 0x7632);
+            if (i + 1 < kParts)
+                a = less(a, make_float2(high_bf16(__float_as_uint(a.x)), high_bf16(__float_as_uint(a.y))));
+        }
     }
 }
 
 __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint2 b) {
-    ptx::mma_bf16_16816(d, a0, a1, a2, a3, b.x, b.y);
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b.x), "r"(b.y));
 }
-
+// The same, from c: an accumulator that stays as it is.
+__device__ __forceinline__ void mma_from(float (&d)[4], const float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2,
+                                         uint32_t a3, uint2 b) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+        "{%10, %11, %12, %13};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b.x), "r"(b.y), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
+}
 // Both bf16 halves of x less the one with bit pattern c (integers below 256 in units of 2^-133: exact).
 __device__ __forceinline__ uint32_t minus(uint32_t x, uint16_t c) {
     const uint32_t cc = (uint32_t)c << 16 | c;
     __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&x), *reinterpret_cast<const __nv_bfloat162 *>(&cc));
     return *reinterpret_cast<uint32_t *>(&r);
+}
+// kBytes from global to shared memory, asynchronously (of this thread's current group).
+template <int kBytes>
+__device__ __forceinline__ void copy_async(void *dst, const void *src) {
+    if constexpr (kBytes == 16)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ptx::smem_u32(dst)), "l"(src) : "memory");
+    else
+        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(ptx::smem_u32(dst)), "l"(src), "n"(kBytes) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() {  // all but this thread's last N groups have landed
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+// Eight consecutive elements of q and their channels' exponents, as loaded.
+template <typename T>
+struct RawQ {
+    uint4 v[sizeof(T) / 2];
+    int2 e;
+    __device__ __forceinline__ void load(const T *q, const int8_t *exps) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) v[i] = reinterpret_cast<const uint4 *>(q)[i];
+        e = *reinterpret_cast<const int2 *>(exps);
+    }
+    __device__ __forceinline__ void widen(float (&x)[8]) const {  // times 2^e
+        const uint32_t w[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[2 * i] = low_bf16(w[i]), x[2 * i + 1] = high_bf16(w[i]);
+        } else {
+            const uint32_t w2[4] = {v[sizeof(T) / 2 - 1].x, v[sizeof(T) / 2 - 1].y, v[sizeof(T) / 2 - 1].z, v[sizeof(T) / 2 - 1].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(w[i]), x[4 + i] = __uint_as_float(w2[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] *= exp2_int((int)(int8_t)((i < 4 ? e.x : e.y) >> (8 * (i & 3))));
+    }
+};
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint32_t cluster_index() {  // of the cluster, along x
+    uint32_t r;
+    asm("mov.u32 %0, %%clusterid.x;" : "=r"(r));
+    return r;
 }
 
 template <int N>
@@ -123,77 +214,94 @@ __device__ __forceinline__ Words<N> load_words(const uint8_t *p) {
 }
 
 template <int D, int NT, int kParts, bool kCluster>
-__global__ void __launch_bounds__(kThreads) decode_q4_mma_kernel(const MmaQ4Params p) {
+__global__ void __launch_bounds__(kThreads, NT == 1 && kParts == 1 ? 4 : 3) decode_q4_mma_kernel(const MmaQ4Params p) {
     using Lay = Layout<D, NT, kParts>;
     using T = std::conditional_t<kParts == 1, __nv_bfloat16, float>;
     constexpr int J = Lay::J, GP = Lay::kGP, OS = Lay::kOStride;
-    constexpr int kWeightParts = kParts == 1 ? VOXZIP_Q4_WP : 3;
+    constexpr int kWeightParts = kParts == 1 ? 2 : 3;  // one part (8 bits) would double the output's rounding error
     constexpr uint32_t kLow = 0x000f000fu, kHigh = 0x00f000f0u;
 
     extern __shared__ __align__(128) uint8_t smem[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, qd = lane & 3;
-    uint8_t *ring = smem + warp * Lay::kWarpRing;
-    uint64_t *full = reinterpret_cast<uint64_t *>(smem + Lay::kBarOff) + warp * kStages;
-    uint64_t *score_bar = reinterpret_cast<uint64_t *>(smem + Lay::kBarOff) + kWarps * kStages;
-    float *m_w = reinterpret_cast<float *>(smem + Lay::kStatOff);  // the warps' maxima
+    const int stages = p.stages, ring_bytes = Lay::warp_ring(stages), wrap = (stages - 1) * Lay::kStageBytes;
+    uint8_t *ring = smem + warp * ring_bytes, *rest = smem + kWarps * ring_bytes;
+    float *m_w = reinterpret_cast<float *>(rest + Lay::kStatOff);  // the warps' maxima
     float *z_w = m_w + kWarps * GP;                                // and sums
     float *f_w = z_w + kWarps * GP;                                // what turns a warp's weights into softmax mass
-    float2 *mz = reinterpret_cast<float2 *>(f_w + kWarps * GP);    // this CTA's maximum and sum
-    float2 *mz_all = mz + GP;                                      // [S][GP]: every CTA's
-    float *lg = reinterpret_cast<float *>(smem + Lay::kLgOff);
-    float *s_old = lg + (size_t)p.chunk_cap * GP;
-
+    float2 *mz_rx = reinterpret_cast<float2 *>(rest + Lay::kMzOff);  // [S][GP] maxima and sums of the cluster's CTAs
     const int S = kCluster ? p.S : 1;
-    const int rank = kCluster ? (int)(blockIdx.x % (unsigned)S) : 0;
-    const UnitIdx ui = unit_of((int)(blockIdx.x / (unsigned)S), p.B, p.L, p.Hkv, p.layer_begin);
+    float4 *o_rx = reinterpret_cast<float4 *>(mz_rx + S * GP);       // [S][slice] their outputs, this CTA's slice
+    float *lg = reinterpret_cast<float *>(rest + Lay::lg_off(S));
+    const int rank = kCluster ? (int)cluster_rank() : 0;
+    UnitIdx ui;  // the grid is [layers][B][Hkv S]
+    ui.h = kCluster ? (int)cluster_index() : (int)blockIdx.x;
+    ui.b = (int)blockIdx.y;
+    ui.l_local = (int)blockIdx.z;
+    ui.l = p.layer_begin + ui.l_local;
+    ui.cache_unit = ((int64_t)ui.b * p.L + ui.l) * p.Hkv + ui.h;
     const int64_t act = (int64_t)ui.l_local * p.B + ui.b, row_base = ui.cache_unit * p.C;
 
-    if (lane == 0) {
-        for (int s = 0; s < kStages; ++s) ptx::mbar_init(&full[s], 1);
-        if (warp == 0) ptx::mbar_init(score_bar, 1);
-        ptx::fence_mbar_init();
-    }
-    __syncwarp();
     ptx::grid_dependency_wait();
-
-    const int32_t n_old = p.len[ui.cache_unit], n = n_old + 1;
+    // The length first, then the warp's share of q (which does not depend on it): one memory latency for both.
+    const int32_t n_old = *static_cast<const volatile int32_t *>(p.len + ui.cache_unit), n = n_old + 1;
+    const int8_t *ke = p.q4.k_exp + ui.cache_unit * D;
+    const T *qg = static_cast<const T *>(p.q) + (act * p.Hq + (int64_t)ui.h * p.G) * D;
+    constexpr int kShare = (NT * J + kWarps - 1) / kWarps;
+    RawQ<T> q_raw[kShare];
+#pragma unroll
+    for (int it = 0; it < kShare; ++it) {
+        const int nj = it * kWarps + warp, head = nj / J * 8 + g, d = 32 * (nj % J) + 8 * qd;
+        q_raw[it] = RawQ<T>{};
+        if (nj < NT * J && head < p.G) q_raw[it].load(qg + head * D + d, ke + d);
+    }
     if (n_old < 0 || n > p.C || n > p.max_rows) {  // the same decision in every CTA of the cluster
         if (rank == 0 && tid == 0)
             raise_status(p.status, n_old < 0 || n > p.C ? VOXZIP_DEV_CAPACITY : VOXZIP_DEV_LEN_HINT);
         return;
     }
-    const int tiles = (n + kTile - 1) / kTile, share = (tiles + S - 1) / S;
+    const int tiles = (n + kTile - 1) / kTile, share = kCluster ? (int)__umulhi(tiles + S - 1, p.inv_s) : tiles;
     const int tile0 = min(tiles, rank * share), mine = min(tiles, tile0 + share) - tile0;  // this CTA's tiles
     const int j0 = tile0 * kTile, cnt = min(n, j0 + mine * kTile) - j0;                    // and tokens
     const int m = (mine - warp + kWarps - 1) / kWarps;                                     // this warp's tiles
     const int items = 2 * m;                                                               // K tiles, then V tiles
 
-    // Stage i of the warp: tile warp + kWarps (i mod m), rows up to the length, in fours (as the capacity is).
-    auto issue = [&](int i) {
-        const bool v = i >= m;
-        const int tile = tile0 + warp + kWarps * (v ? i - m : i);
-        const int rows = min(kTile, (n - tile * kTile + 3) & ~3);
-        const int64_t row = row_base + (int64_t)tile * kTile;
-        uint8_t *stage = ring + i % kStages * Lay::kStageBytes;
-        uint64_t *bar = &full[i % kStages];
-        if (!VOXZIP_IN_RANGE(p.status, tile >= 0 && tile * kTile + rows <= p.C && rows > 0)) return;
-        ptx::mbar_arrive_expect_tx(bar, (uint32_t)rows * (D / 2 + J * 2));
-        ptx::bulk_load(stage, (v ? p.q4.v_codes : p.q4.k_codes) + row * (D / 2), (uint32_t)rows * (D / 2), bar);
-        ptx::bulk_load(stage + Lay::kCodeBytes, (v ? p.q4.v_scale : p.q4.k_scale) + row * J, (uint32_t)rows * (J * 2), bar);
-    };
-    if (lane == 0) {
-        for (int i = 0; i < min(kStages, items); ++i) issue(i);
-        if (warp == 0 && cnt > 0) {
-            const uint32_t bytes = (uint32_t)((cnt + 3) & ~3) * 4;
-            ptx::mbar_arrive_expect_tx(score_bar, bytes);
-            ptx::bulk_load(s_old, p.score + row_base + j0, bytes, score_bar);
+    // The ring: item i of the warp (tile warp + kWarps (i mod m) of the CTA) goes to slot i mod `stages`. Each lane
+    // copies 16-byte pieces of the codes and one row's scales; of the last tile, rows up to the length in fours (as
+    // the capacity is). One copy group per item, empty past the last.
+    constexpr int kPieces = Lay::kCodeBytes / 512;  // per lane
+    const int64_t first = row_base + j0 + warp * kTile;
+    const uint8_t *next_codes = p.q4.k_codes + first * (D / 2) + lane * 16;
+    const __nv_bfloat16 *next_scale = p.q4.k_scale + (first + lane) * J;
+    int next = 0, next_slot = 0, next_left = n - j0 - warp * kTile;  // the item, its slot, rows from its tile's first on
+    auto issue = [&]() {
+        if (next < items) {
+            uint8_t *stage = ring + next_slot;
+            const int rows = (next_left + 3) & ~3;
+            if (VOXZIP_IN_RANGE(p.status, next_left > 0 && n - next_left + min(rows, kTile) <= p.C)) {
+#pragma unroll
+                for (int k = 0; k < kPieces; ++k)
+                    if (lane / (D / 32) + k * (kTile / kPieces) < rows) copy_async<16>(stage + lane * 16 + k * 512, next_codes + k * 512);
+                if (lane < rows) copy_async<J * 2>(stage + Lay::kCodeBytes + lane * (J * 2), next_scale);
+            }
+            if (++next == m) {
+                next_codes = p.q4.v_codes + first * (D / 2) + lane * 16;
+                next_scale = p.q4.v_scale + (first + lane) * J;
+                next_left = n - j0 - warp * kTile;
+            } else {
+                next_codes += kWarps * Lay::kCodeBytes;
+                next_scale += kWarps * kTile * J;
+                next_left -= kWarps * kTile;
+            }
+            next_slot = next_slot == wrap ? 0 : next_slot + Lay::kStageBytes;
         }
-    }
+        copy_commit();
+    };
+    if (tid == 0 && cnt > 0) ptx::prefetch_l2(p.score + row_base + j0, (uint32_t)((cnt + 3) & ~3) * 4);
+    for (int i = 0; i < stages - 1; ++i) issue();
 
     // The appended row lies in the last tile; the warp that has it packs the row over what the ring brought in,
     // and into the cache.
     const bool appends = mine > 0 && tile0 + mine == tiles && (mine - 1) % kWarps == warp;
-    const int8_t *ke = p.q4.k_exp + ui.cache_unit * D;
     float4 kn = make_float4(0.f, 0.f, 0.f, 0.f), vn = kn;
     if (appends && lane < D / 4) {
         const int64_t at = (act * p.Hkv + ui.h) * D + lane * 4;
@@ -206,83 +314,76 @@ __global__ void __launch_bounds__(kThreads) decode_q4_mma_kernel(const MmaQ4Para
     const int row_new = n_old % kTile;
 
     // q's operands: lane (g, qd) holds channels 32 j + 8 qd .. + 7 of head g, times 2^e; the pairs that meet codes in
-    // bits 4-7 a sixteenth of it. c_init: what the accumulators of heads 2 qd, 2 qd + 1 start from.
+    // bits 4-7 a sixteenth of it. The warps make a share each, and of the sums that the accumulators start from.
+    uint2 *q_smem = reinterpret_cast<uint2 *>(rest + Lay::kQOff);
+    float *c_smem = reinterpret_cast<float *>(rest + Lay::kCOff);
+#pragma unroll
+    for (int it = 0; it < kShare; ++it) {
+        const int nj = it * kWarps + warp;
+        if (nj < NT * J) {
+            const int nt = nj / J, j = nj % J;
+            float x[8];
+            q_raw[it].widen(x);
+            float sum = ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+            sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+            sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+            if (qd == 0) c_smem[nj * 8 + g] = sum * (-8.f * (kCarry * 0x1p-133f));
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) {
+                uint32_t b0[kParts], b1[kParts];
+                split_pair<kParts>(make_float2(x[4 * ks] * kCarry, x[4 * ks + 1] * kCarry), b0);
+                split_pair<kParts>(make_float2(x[4 * ks + 2] * (kCarry / 16), x[4 * ks + 3] * (kCarry / 16)), b1);
+#pragma unroll
+                for (int i = 0; i < kParts; ++i)
+                    q_smem[((i * NT + nt) * 2 * J + 2 * j + ks) * 32 + lane] = make_uint2(b0[i], b1[i]);
+            }
+        }
+    }
+    __syncthreads();
     uint2 qb[kParts == 1 ? NT : 1][kParts == 1 ? 2 * J : 1];
-    uint2 *q_smem = reinterpret_cast<uint2 *>(smem + Lay::kQOff);
-    float c_init[NT][J][2];
-    {
-        const T *qg = static_cast<const T *>(p.q) + (act * p.Hq + (int64_t)ui.h * p.G) * D;
+    if constexpr (kParts == 1) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int j = 0; j < J; ++j) {
-                const int head = nt * 8 + g, d = 32 * j + 8 * qd;
-                float x[8];
-#pragma unroll
-                for (int i = 0; i < 8; i += 4) {
-                    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-                    if (head < p.G) v = load4(qg + head * D + d + i);
-                    const char4 e = *reinterpret_cast<const char4 *>(ke + d + i);
-                    x[i] = v.x * exp2_int(e.x), x[i + 1] = v.y * exp2_int(e.y);
-                    x[i + 2] = v.z * exp2_int(e.z), x[i + 3] = v.w * exp2_int(e.w);
-                }
-                float sum = ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
-                sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-                sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-                sum *= -8.f * (kCarry * 0x1p-133f);
-                c_init[nt][j][0] = __shfl_sync(0xffffffffu, sum, 8 * qd);
-                c_init[nt][j][1] = __shfl_sync(0xffffffffu, sum, 8 * qd + 4);
-#pragma unroll
-                for (int ks = 0; ks < 2; ++ks) {
-                    uint32_t b0[kParts], b1[kParts];
-                    split_pair<kParts>(x[4 * ks] * kCarry, x[4 * ks + 1] * kCarry, b0);
-                    split_pair<kParts>(x[4 * ks + 2] * (kCarry / 16), x[4 * ks + 3] * (kCarry / 16), b1);
-                    if constexpr (kParts == 1) {
-                        qb[nt][2 * j + ks] = make_uint2(b0[0], b1[0]);
-                    } else if (warp == 0) {
-#pragma unroll
-                        for (int i = 0; i < kParts; ++i)
-                            q_smem[((i * NT + nt) * 2 * J + 2 * j + ks) * 32 + lane] = make_uint2(b0[i], b1[i]);
-                    }
-                }
-            }
+            for (int step = 0; step < 2 * J; ++step) qb[nt][step] = q_smem[(nt * 2 * J + step) * 32 + lane];
     }
-    if constexpr (kParts > 1) __syncthreads();
+    float c_init[NT][J][4];  // heads 2 qd, 2 qd + 1, for the two rows of an accumulator
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const float2 c = *reinterpret_cast<const float2 *>(c_smem + (nt * J + j) * 8 + 2 * qd);
+            c_init[nt][j][0] = c_init[nt][j][2] = c.x;
+            c_init[nt][j][1] = c_init[nt][j][3] = c.y;
+        }
+    if constexpr (kCluster) {  // this CTA runs, and has q: the others may send to it once all its warps say so
+        __syncwarp();
+        asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+    }
     auto q_operand = [&](int part, int nt, int step) {
         if constexpr (kParts == 1) return qb[nt][step];
         else return q_smem[((part * NT + nt) * 2 * J + step) * 32 + lane];
     };
 
-    bool ok = true;
-    int done = 0;  // stages seen to land
-    auto wait = [&](int i) {
-        ok = ok && __all_sync(0xffffffffu, ptx::mbar_wait_bounded(&full[i % kStages], (i / kStages) & 1, kWaitLimit));
-        done = ok ? i + 1 : done;
-        return ok;
-    };
-    auto refill = [&](int i, bool wrote) {  // stage i has been read by every lane
-        if (wrote) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    int slot = 0;
+    auto stage_of_next = [&]() {  // the next item's stage, landed, and every lane done with the one before
+        if (stages == 2) copy_wait<0>();
+        else copy_wait<1>();
         __syncwarp();
-        if (lane == 0 && i + kStages < items) issue(i + kStages);
+        uint8_t *stage = ring + slot;
+        slot = slot == wrap ? 0 : slot + Lay::kStageBytes;
+        issue();
+        return stage;
     };
 
-    // Phase K: logits and the warp's maxima.
+    // Phase K: logits (before the softmax scale, in units of 2^-49) and the warp's maxima.
     float mx[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) mx[nt][0] = mx[nt][1] = -INFINITY;
-    for (int i = 0; i < m && wait(i); ++i) {
-        uint8_t *stage = ring + i % kStages * Lay::kStageBytes;
-        const int local = warp + kWarps * i;  // the CTA's tile
-        const int valid = cnt - local * kTile;
-        const bool last = appends && i == m - 1;
-        if (last) {
-            const Q4Row<D, true> row(kn);
-            row.store(stage + row_new * (D / 2), reinterpret_cast<__nv_bfloat16 *>(stage + Lay::kCodeBytes) + row_new * J);
-            row.store(p.q4.k_codes + (row_base + n_old) * (D / 2), p.q4.k_scale + (row_base + n_old) * J);
-            __syncwarp();
-        }
+    auto k_tile = [&](auto full_tag, const uint8_t *stage, int local, int valid) {
+        constexpr bool kFull = decltype(full_tag)::value;
 #pragma unroll
-        for (int mb = 0; mb < 2; ++mb) {
+        for (int mb = 0; mb < kTile / 16; ++mb) {
             const int r0 = 16 * mb + g, r1 = r0 + 8;
             const Words<J> w0 = load_words<J>(stage + r0 * (D / 2) + qd * (J * 4));
             const Words<J> w1 = load_words<J>(stage + r1 * (D / 2) + qd * (J * 4));
@@ -297,18 +398,18 @@ __global__ void __launch_bounds__(kThreads) decode_q4_mma_kernel(const MmaQ4Para
             for (int j = 0; j < J; ++j) {
                 float acc[NT][4];
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    acc[nt][0] = acc[nt][2] = c_init[nt][j][0];
-                    acc[nt][1] = acc[nt][3] = c_init[nt][j][1];
-                }
-#pragma unroll
                 for (int ks = 0; ks < 2; ++ks) {
                     const uint32_t x0 = w0.w[j] >> (8 * ks), x1 = w1.w[j] >> (8 * ks);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int i2 = 0; i2 < kParts; ++i2)
-                            mma(acc[nt], x0 & kLow, x1 & kLow, x0 & kHigh, x1 & kHigh, q_operand(i2, nt, 2 * j + ks));
+                        for (int i2 = 0; i2 < kParts; ++i2) {
+                            const uint2 b = q_operand(i2, nt, 2 * j + ks);
+                            if (ks == 0 && i2 == 0)
+                                mma_from(acc[nt], c_init[nt][j], x0 & kLow, x1 & kLow, x0 & kHigh, x1 & kHigh, b);
+                            else
+                                mma(acc[nt], x0 & kLow, x1 & kLow, x0 & kHigh, x1 & kHigh, b);
+                        }
                 }
                 const float a = j & 1 ? high_bf16(s0.w[j / 2]) : low_bf16(s0.w[j / 2]);
                 const float b = j & 1 ? high_bf16(s1.w[j / 2]) : low_bf16(s1.w[j / 2]);
@@ -322,8 +423,7 @@ __global__ void __launch_bounds__(kThreads) decode_q4_mma_kernel(const MmaQ4Para
             for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    sum[nt][k] *= p.scale_log2;
-                    if ((k < 2 ? r0 : r1) >= valid) sum[nt][k] = -INFINITY;  // past the length: whatever lies there
+                    if (!kFull && (k < 2 ? r0 : r1) >= valid) sum[nt][k] = -INFINITY;  // past the length: whatever lies there
                     mx[nt][k & 1] = fmaxf(mx[nt][k & 1], sum[nt][k]);
                 }
                 float *to = lg + ((size_t)nt * p.chunk_cap + local * kTile) * 8 + 2 * qd;
@@ -331,7 +431,20 @@ __global__ void __launch_bounds__(kThreads) decode_q4_mma_kernel(const MmaQ4Para
                 *reinterpret_cast<float2 *>(to + r1 * 8) = make_float2(sum[nt][2], sum[nt][3]);
             }
         }
-        refill(i, last);
+    };
+    for (int i = 0; i < m; ++i) {
+        uint8_t *stage = stage_of_next();
+        const int local = warp + kWarps * i;  // the CTA's tile
+        const int valid = cnt - local * kTile;
+        const bool last = appends && i == m - 1;
+        if (last) {
+            const Q4Row<D, true> row(kn);
+            row.store(stage + row_new * (D / 2), reinterpret_cast<__nv_bfloat16 *>(stage + Lay::kCodeBytes) + row_new * J);
+            row.store(p.q4.k_codes + (row_base + n_old) * (D / 2), p.q4.k_scale + (row_base + n_old) * J);
+            __syncwarp();
+        }
+        if (valid >= kTile) k_tile(std::true_type{}, stage, local, valid);
+        else k_tile(std::false_type{}, stage, local, valid);
     }
     // The warp's maxima: to shared memory for heads 2 qd, 2 qd + 1, to lane (g, .) for head g.
     float mg[NT];
@@ -341,6 +454,8 @@ __global__ void __launch_bounds__(kThreads) decode_q4_mma_kernel(const MmaQ4Para
         for (int k = 0; k < 2; ++k)
 #pragma unroll
             for (int o = 4; o < 32; o <<= 1) mx[nt][k] = fmaxf(mx[nt][k], __shfl_xor_sync(0xffffffffu, mx[nt][k], o));
+#pragma unroll
+        for (int k = 0; k < 2; ++k) mx[nt][k] *= p.scale_log2;
         if (g == 0) {
             m_w[warp * GP + nt * 8 + 2 * qd] = mx[nt][0];
             m_w[warp * GP + nt * 8 + 2 * qd + 1] = mx[nt][1];
@@ -360,41 +475,50 @@ __global__ void __launch_bounds__(kThreads) decode_q4_mma_kernel(const MmaQ4Para
 #pragma unroll
             for (int k = 0; k < 4; ++k) o[2 * j][nt][k] = o[2 * j + 1][nt][k] = 0.f;
     }
-    for (int i = m; i < items && wait(i); ++i) {
-        uint8_t *stage = ring + i % kStages * Lay::kStageBytes;
-        const int local = warp + kWarps * (i - m);
+    float *sc_w = reinterpret_cast<float *>(rest + Lay::kScOff) + warp * (J * kTile);  // [J][32] a tile's scales
+    for (int i = 0; i < m; ++i) {
+        uint8_t *stage = stage_of_next();
+        const int local = warp + kWarps * i;
         const int valid = cnt - local * kTile;
-        const bool last = appends && i == items - 1;
-        if (last) {
+        if (appends && i == m - 1) {
             const Q4Row<D, false> row(vn);
             row.store(stage + row_new * (D / 2), reinterpret_cast<__nv_bfloat16 *>(stage + Lay::kCodeBytes) + row_new * J);
             row.store(p.q4.v_codes + (row_base + n_old) * (D / 2), p.q4.v_scale + (row_base + n_old) * J);
             __syncwarp();
         }
+        {  // Lane t widens the scales of token t; zero past the length, where a scale may be anything, a NaN too.
+            Words<J / 2> s = load_words<J / 2>(stage + Lay::kCodeBytes + lane * (J * 2));
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            Words<J / 2> w[4], s[4];
-            float pr[NT][4];
+            for (int k = 0; k < J / 2; ++k) {
+                if (lane >= valid) s.w[k] = 0u;
+                float *to = sc_w + 2 * k * kTile + ((lane & 16) | (lane & 3) << 2 | (lane >> 2 & 3));
+                to[0] = low_bf16(s.w[k]);
+                to[kTile] = high_bf16(s.w[k]);
+            }
+            __syncwarp();
+        }
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int t = 16 * kb + 4 * k + qd;
-                w[k] = load_words<J / 2>(stage + t * (D / 2) + g * (J * 2));
-                s[k] = load_words<J / 2>(stage + Lay::kCodeBytes + t * (J * 2));
-                if (t >= valid) s[k] = Words<J / 2>{};  // past the length a scale may be anything, a NaN too
+        for (int kb = 0; kb < kTile / 16; ++kb) {
+            Words<J / 2> w[4];
+            float2 p01[NT], p23[NT];
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    float *l = lg + ((size_t)nt * p.chunk_cap + local * kTile + t) * 8 + g;
-                    const float x = fast_exp2(*l - mg[nt]);
-                    *l = x;
-                    z[nt] += x;
-                    pr[nt][k] = x * kCarry;
+            for (int nt = 0; nt < NT; ++nt) {
+                float *l = lg + ((size_t)nt * p.chunk_cap + local * kTile + 16 * kb + qd) * 8 + g;
+                float x[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    x[k] = fast_exp2(fmaf(l[k * 32], p.scale_log2, -mg[nt]));
+                    l[k * 32] = x[k];
                 }
+                z[nt] += (x[0] + x[1]) + (x[2] + x[3]);
+                p01[nt] = make_float2(x[0] * kCarry, x[1] * kCarry);
+                p23[nt] = make_float2(x[2] * kCarry, x[3] * kCarry);
             }
 #pragma unroll
-            for (int j = 0; j < J; ++j) {
-                float sc[4];
+            for (int k = 0; k < 4; ++k) w[k] = load_words<J / 2>(stage + (16 * kb + 4 * k + qd) * (D / 2) + g * (J * 2));
 #pragma unroll
-                for (int k = 0; k < 4; ++k) sc[k] = j & 1 ? high_bf16(s[k].w[j / 2]) : low_bf16(s[k].w[j / 2]);
+            for (int j = 0; j < J; ++j) {
+                const float4 sc = *reinterpret_cast<const float4 *>(sc_w + j * kTile + 16 * kb + 4 * qd);
                 const uint32_t x01 = __byte_perm(w[0].w[j / 2], w[1].w[j / 2], j & 1 ? 0x7632 : 0x5410);
                 const uint32_t x23 = __byte_perm(w[2].w[j / 2], w[3].w[j / 2], j & 1 ? 0x7632 : 0x5410);
                 const uint32_t y01 = x01 >> 8, y23 = x23 >> 8;
@@ -405,8 +529,8 @@ __global__ void __launch_bounds__(kThreads) decode_q4_mma_kernel(const MmaQ4Para
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                     uint32_t b0[kWeightParts], b1[kWeightParts];
-                    split_pair<kWeightParts>(pr[nt][0] * sc[0], pr[nt][1] * sc[1], b0);
-                    split_pair<kWeightParts>(pr[nt][2] * sc[2], pr[nt][3] * sc[3], b1);
+                    split_pair<kWeightParts>(times(p01[nt], make_float2(sc.x, sc.y)), b0);
+                    split_pair<kWeightParts>(times(p23[nt], make_float2(sc.z, sc.w)), b1);
 #pragma unroll
                     for (int i2 = 0; i2 < kWeightParts; ++i2) {
                         const uint2 b = make_uint2(b0[i2], b1[i2]);
@@ -416,16 +540,37 @@ __global__ void __launch_bounds__(kThreads) decode_q4_mma_kernel(const MmaQ4Para
                 }
             }
         }
-        refill(i, last);
     }
-    if (!ok) {  // a wait gave up: outputs are not valid; let what is still in flight land (bounded)
-        raise_status(p.status, VOXZIP_DEV_TIMEOUT);
-        for (int i = done; i < min(items, done + kStages); ++i)
-            (void)ptx::mbar_wait_bounded(&full[i % kStages], (i / kStages) & 1, kWaitLimit);
+    // The CTA that will take this one's place: its rows are asked into L2 now, so that HBM works on while this one
+    // puts its results together and that one starts.
+    if (warp == kWarps - 1 && p.next_l >= 0) {
+        int h2 = ui.h + p.next_h, b2 = ui.b + p.next_b, l2 = ui.l_local + p.next_l;
+        if (h2 >= p.Hkv) h2 -= p.Hkv, ++b2;
+        if (b2 >= p.B) b2 -= p.B, ++l2;
+        if (l2 < (int)gridDim.z) {
+            const int64_t unit2 = ((int64_t)b2 * p.L + p.layer_begin + l2) * p.Hkv + h2;
+            const int n2 = min(max(ptx::load_relaxed(p.len + unit2), 0) + 1, p.C);  // only aims: it may be about to change
+            const int tiles2 = (n2 + kTile - 1) / kTile, share2 = kCluster ? (int)__umulhi(tiles2 + S - 1, p.inv_s) : tiles2;
+            const int first2 = min(tiles2, rank * share2) * kTile;
+            const int rows2 = (min(n2, first2 + share2 * kTile) - first2 + 3) & ~3;
+            if (lane == 0 && rows2 > 0 && VOXZIP_IN_RANGE(p.status, first2 + rows2 <= p.C)) {
+                const int64_t row = unit2 * p.C + first2;
+                ptx::prefetch_l2(p.q4.k_codes + row * (D / 2), (uint32_t)rows2 * (D / 2));
+                ptx::prefetch_l2(p.q4.k_scale + row * J, (uint32_t)rows2 * (J * 2));
+            }
+        }
+    }
+    // The old scores of the first tokens travel while the CTA and the cluster put their statistics together.
+    constexpr int kAhead = 6;
+    float old[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+        const int i = warp * kTile + lane + k * kThreads;
+        old[k] = i < cnt ? p.score[row_base + j0 + i] : 0.f;
     }
     ptx::launch_dependents();
 
-    // The warp's sums and outputs (in units of 2^-49), the latter over its drained ring.
+    // The warp's sums and outputs, the latter over its drained ring.
     float *ow = reinterpret_cast<float *>(ring);
     __syncwarp();
 #pragma unroll
@@ -438,120 +583,105 @@ __global__ void __launch_bounds__(kThreads) decode_q4_mma_kernel(const MmaQ4Para
 #pragma unroll
             for (int k = 0; k < 2; ++k)
                 *reinterpret_cast<float4 *>(ow + (nt * 8 + 2 * qd + k) * OS + 32 * j + 4 * g) =
-                    make_float4(o[2 * j][nt][k], o[2 * j][nt][2 + k] * 0.0625f, o[2 * j + 1][nt][k],
-                                o[2 * j + 1][nt][2 + k] * 0.0625f);
+                    make_float4(o[2 * j][nt][k] * kUncarry, o[2 * j][nt][2 + k] * (kUncarry / 16), o[2 * j + 1][nt][k] * kUncarry,
+                                o[2 * j + 1][nt][2 + k] * (kUncarry / 16));
     }
     __syncthreads();
-    // Per head: the CTA's maximum, its sum, and 2^(m_w - m).
+    // Per head: the CTA's maximum, and 2^(m_w - m). A warp without tiles has -inf: 0 for any finite m.
     auto warp_factors = [&](int h, float (&f)[kWarps]) {
-        float mm = -INFINITY;
+        float mm = kLeast;
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) mm = fmaxf(mm, f[w] = m_w[w * GP + h]);
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) f[w] = f[w] == -INFINITY ? 0.f : fast_exp2(f[w] - mm);
+        for (int w = 0; w < kWarps; ++w) f[w] = fast_exp2(f[w] - mm);
         return mm;
     };
+    auto warp_sum = [&](int h, const float (&f)[kWarps]) {
+        float zz = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) zz += f[w] * z_w[w * GP + h];
+        return zz;
+    };
     T *og = static_cast<T *>(p.out) + (act * p.Hq + (int64_t)ui.h * p.G) * D;
-    float *o_cta = reinterpret_cast<float *>(smem);  // warp 0's place
-    if (tid < GP) {
-        float f[kWarps], zz = 0.f;
-        const float mm = warp_factors(tid, f);
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) zz += f[w] * z_w[w * GP + tid];
-        if constexpr (kCluster) mz[tid] = make_float2(mm, zz);
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) f_w[w * GP + tid] = kCluster ? f[w] : tid < p.G ? f[w] / zz : 0.f;
+    auto store_out = [&](int e, const float4 &v, float r) {  // float4 e of the unit's outputs
+        T *to = og + 4 * e;
+        to[0] = Elem<T>::from_f(v.x * r), to[1] = Elem<T>::from_f(v.y * r);
+        to[2] = Elem<T>::from_f(v.z * r), to[3] = Elem<T>::from_f(v.w * r);
+    };
+    if constexpr (kCluster) {
+        ptx::cluster_wait();  // every CTA of the cluster runs
+        cg::cluster_group cluster = cg::this_cluster();
+        for (int t = tid; t < S * GP; t += kThreads) {
+            const int h = t % GP;
+            float f[kWarps];
+            const float mm = warp_factors(h, f);
+            *cluster.map_shared_rank(mz_rx + rank * GP + h, t / GP) = make_float2(mm, warp_sum(h, f));
+        }
     }
-    for (int e = tid; e < (kCluster ? GP : p.G) * D / 4; e += kThreads) {
+    for (int e = tid; e < p.G * D / 4; e += kThreads) {
         const int h = e / (D / 4), at = h * OS + e % (D / 4) * 4;
         float f[kWarps];
         warp_factors(h, f);
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        float zz = 0.f;
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
-            const float4 x = *reinterpret_cast<const float4 *>(smem + w * Lay::kWarpRing + at * 4);
+            const float4 x = *reinterpret_cast<const float4 *>(smem + w * ring_bytes + at * 4);
             v.x += f[w] * x.x, v.y += f[w] * x.y, v.z += f[w] * x.z, v.w += f[w] * x.w;
-            zz += f[w] * z_w[w * GP + h];
         }
-        if constexpr (kCluster) {
-            *reinterpret_cast<float4 *>(o_cta + at) = v;
+        if constexpr (kCluster) {  // to the CTA that writes it
+            const int to = (int)__umulhi(e, p.inv_slice);
+            *cg::this_cluster().map_shared_rank(o_rx + rank * p.slice + (e - to * p.slice), to) = v;
         } else {
-            const float r = kUncarry / zz;
-            T *to = og + h * D + e % (D / 4) * 4;
-            to[0] = Elem<T>::from_f(v.x * r), to[1] = Elem<T>::from_f(v.y * r);
-            to[2] = Elem<T>::from_f(v.z * r), to[3] = Elem<T>::from_f(v.w * r);
+            store_out(e, v, 1.f / warp_sum(h, f));
         }
     }
+    // What turns weights into softmax mass: 2^(m_r - m) / Z for CTA r of the unit.
+    auto unit_stats = [&](int h, float &mm) {  // returns 1 / Z
+        float zz = 0.f;
+        mm = kLeast;
+        for (int r = 0; r < S; ++r) mm = fmaxf(mm, mz_rx[r * GP + h].x);
+        for (int r = 0; r < S; ++r) zz += fast_exp2(mz_rx[r * GP + h].x - mm) * mz_rx[r * GP + h].y;
+        return 1.f / zz;
+    };
     if constexpr (kCluster) {
-        cg::cluster_group cluster = cg::this_cluster();
-        cluster.sync();  // every CTA's mz and o_cta are final
-        auto combine = [&](auto ss_tag) {
-            constexpr int SS = decltype(ss_tag)::value;
-            constexpr int E = (GP * D / SS + kThreads - 1) / kThreads;
-            const int total = p.G * D, per = (total + SS - 1) / SS;
-            const int lo = rank * per, hi = min(total, lo + per);
-            float part[E][SS];
-            for (int t = tid; t < SS * GP; t += kThreads) mz_all[t] = *cluster.map_shared_rank(mz + t % GP, t / GP);
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const int i = lo + tid + e * kThreads;
-                const int at = i < hi ? (i / D) * OS + i % D : 0;
-#pragma unroll
-                for (int r = 0; r < SS; ++r) part[e][r] = i < hi ? *cluster.map_shared_rank(&o_cta[at], r) : 0.f;
+        // What the others sent has landed, and nobody touches another's memory from here on.
+        asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+        asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+        for (int i = tid; i < p.slice; i += kThreads) {
+            const int e = rank * p.slice + i;
+            if (e >= p.G * D / 4) break;
+            const int h = e / (D / 4);
+            float mm;
+            const float rz = unit_stats(h, mm);
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int r = 0; r < S; ++r) {
+                const float f = fast_exp2(mz_rx[r * GP + h].x - mm);
+                const float4 x = o_rx[r * p.slice + i];
+                v.x += f * x.x, v.y += f * x.y, v.z += f * x.z, v.w += f * x.w;
             }
-            __syncthreads();
-            if (tid < GP) {  // mz_all[r][h].x becomes 2^(m_r - m) / Z
-                float2 x[SS];
-                float mm = -INFINITY, zz = 0.f;
-#pragma unroll
-                for (int r = 0; r < SS; ++r) {
-                    x[r] = mz_all[r * GP + tid];
-                    mm = fmaxf(mm, x[r].x);
-                }
-#pragma unroll
-                for (int r = 0; r < SS; ++r) {
-                    x[r].x = x[r].x == -INFINITY ? 0.f : fast_exp2(x[r].x - mm);
-                    zz += x[r].x * x[r].y;
-                }
-                const float rz = tid < p.G ? 1.f / zz : 0.f;
-#pragma unroll
-                for (int r = 0; r < SS; ++r) {
-                    mz_all[r * GP + tid].x = x[r].x * rz;
-                    if (r == rank)
-#pragma unroll
-                        for (int w = 0; w < kWarps; ++w) f_w[w * GP + tid] *= x[r].x * rz;
-                }
-            }
-            __syncthreads();
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const int i = lo + tid + e * kThreads;
-                if (i < hi) {
-                    float x = 0.f;
-#pragma unroll
-                    for (int r = 0; r < SS; ++r) x += mz_all[r * GP + i / D].x * part[e][r];
-                    og[i] = Elem<T>::from_f(x * kUncarry);
-                }
-            }
-        };
-        switch (S) {
-            case 2: combine(std::integral_constant<int, 2>{}); break;
-            case 4: combine(std::integral_constant<int, 4>{}); break;
-            case 8: combine(std::integral_constant<int, 8>{}); break;
-            default: combine(std::integral_constant<int, 16>{}); break;
+            store_out(e, v, rz);
         }
-        ptx::cluster_arrive_relaxed();  // this CTA is done reading its peers' shared memory
-    } else {
-        __syncthreads();
     }
     // Eq. 6 for the warp's own tokens.
     if (m > 0) {
+        if (lane < GP) {
+            float f[kWarps], mm, r;
+            const float m_cta = warp_factors(lane, f);
+            if constexpr (kCluster) {
+                r = unit_stats(lane, mm);
+                r *= fast_exp2(m_cta - mm);
+            } else {
+                r = 1.f / warp_sum(lane, f);
+            }
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w)
+                if (w == warp) f_w[w * GP + lane] = lane < p.G ? f[w] * r : 0.f;
+        }
+        __syncwarp();
         float f[GP];
 #pragma unroll
         for (int h = 0; h < GP; ++h) f[h] = f_w[warp * GP + h];
-        if (!ptx::mbar_wait_bounded(score_bar, 0, kWaitLimit)) raise_status(p.status, VOXZIP_DEV_TIMEOUT);
-        for (int i = warp * kTile + lane; i < cnt; i += kThreads) {
+        auto update = [&](int i, float before) {
             float add = 0.f;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
@@ -561,11 +691,15 @@ __global__ void __launch_bounds__(kThreads) decode_q4_mma_kernel(const MmaQ4Para
                        ((b.x * f[nt * 8 + 4] + b.y * f[nt * 8 + 5]) + (b.z * f[nt * 8 + 6] + b.w * f[nt * 8 + 7]));
             }
             if (VOXZIP_IN_RANGE(p.status, j0 + i < p.C))
-                p.score[row_base + j0 + i] = j0 + i == n_old ? add : p.gamma * s_old[i] + add;
-        }
+                p.score[row_base + j0 + i] = j0 + i == n_old ? add : p.gamma * before + add;
+        };
+        int i = warp * kTile + lane;
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k, i += kThreads)
+            if (i < cnt) update(i, old[k]);
+        for (; i < cnt; i += kThreads) update(i, p.score[row_base + j0 + i]);
     }
     if (rank == 0 && tid == 0) p.len[ui.cache_unit] = n;
-    if constexpr (kCluster) ptx::cluster_wait();  // no CTA leaves while a peer may still read its shared memory
 }
 
 // ---------------------------------------------------------------- host side
@@ -603,23 +737,70 @@ auto by_shape(const voxzip_cache_desc &d, F &&f) {
     return bf16 ? f(Kernels<64, 1, 1>{}) : f(Kernels<64, 1, 3>{});
 }
 
-#ifndef VOXZIP_Q4_FORCE_S
-#define VOXZIP_Q4_FORCE_S 0
-#endif
-
-// CTAs per unit.
-int plan(const voxzip_cache_desc &d, int units, int nmax, int *chunk_cap) {
-    const int tiles = (nmax + kTile - 1) / kTile;
-    for (int S = 1; S <= kMaxCluster; S <<= 1) {
-        const int cap = (tiles + S - 1) / S * kTile;
-        const size_t smem = by_shape(d, [&](auto k) { return decltype(k)::Lay::bytes(cap); });
-        *chunk_cap = cap;
-        if (smem > kMaxSmem) continue;
-        if (VOXZIP_Q4_FORCE_S ? S >= VOXZIP_Q4_FORCE_S
-                              : S == kMaxCluster || cap <= kTile * kWarps || (units * S >= 3 * sm_count() && smem <= kMaxSmem / 3))
-            return (int64_t)units * S <= INT32_MAX ? S : 0;
+// How many clusters of S CTAs with `smem` bytes each fit the GPU at once.
+template <typename K>
+int resident_clusters(int S, size_t smem) {
+    if (configure<K>() != cudaSuccess) return 0;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)S, 1024, 1);
+    cfg.blockDim = dim3(kThreads, 1, 1);
+    cfg.dynamicSmemBytes = smem;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)S;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, K::of(S), &cfg) != cudaSuccess) {
+        cudaGetLastError();
+        return 0;
     }
-    return 0;
+    return n;
+}
+
+struct Plan {
+    int S, stages, chunk_cap;
+    int resident;  // clusters at once
+};
+
+// A time model of a launch, in us, fitted to back-to-back launches of forced plans (4 to 6 144 units of 100 to
+// 40 000 rows, groups of 1 to 16 heads, both head dims and types: 22 shapes, S up to 16, two to four stages). The
+// plans it picks are 0.6% slower than the best of each shape on average, 4% at worst.
+constexpr double kFixed = 3.46, kFixedNeighbour = 0.2;  // a CTA's start and end, more with each CTA on its SM
+constexpr double kExchange = 2.51;                      // the cluster's
+constexpr double kTileAlone = 1.33, kTileShared = 0.41; // a warp's tile of K and V: by latency, or by CTAs on its SM
+constexpr double kTwoStages = 0.18;                     // more per tile with a ring of two, shared by the SM's CTAs
+constexpr double kLastRound = 0.75;                     // how far a part-filled last round costs a whole one
+
+Plan plan(const voxzip_cache_desc &d, int units, int nmax) {
+    const int tiles = (nmax + kTile - 1) / kTile, sms = sm_count();
+    const double weight = (d.head_dim == 64 ? 0.70 : 1.0) * (d.dtype == VOXZIP_F32 ? 1.24 : 1.0) *
+                          (d.q_heads / d.kv_heads > 8 ? 1.55 : 1.0);
+    Plan best{0, 0, 0, 0};
+    double best_cost = 0.0;
+    for (int S : {1, 2, 3, 4, 5, 6, 8, 12, 16}) {
+        if (S > tiles) break;
+        const int cap = (tiles + S - 1) / S * kTile;
+        for (int stages = kMaxStages; stages >= 2; --stages) {
+            const size_t smem = by_shape(d, [&](auto k) { return decltype(k)::Lay::bytes(cap, S, stages); });
+            if (smem > kMaxSmem) continue;
+            const int resident = by_shape(d, [&](auto k) { return resident_clusters<decltype(k)>(S, smem); });
+            if (resident <= 0) continue;
+            const double per_sm = fmin((double)resident, (double)units) * S / sms, neighbours = fmax(1.0, per_sm);
+            const double tile = fmax(kTileAlone, kTileShared * neighbours) * weight + (stages == 2 ? kTwoStages / neighbours : 0.0);
+            const double cta = kFixed + kFixedNeighbour * neighbours + (S > 1 ? kExchange : 0.0) +
+                               tile * ((tiles + kWarps * S - 1) / (kWarps * S));
+            const double share = (double)units / resident;
+            const double cost = cta * (share <= 1.0 ? 1.0 : kLastRound * ceil(share) + (1.0 - kLastRound) * share);
+            if (best.S == 0 || cost < best_cost) {
+                best = Plan{S, stages, cap, resident};
+                best_cost = cost;
+            }
+        }
+    }
+    return best;
 }
 
 }  // namespace
@@ -630,23 +811,51 @@ cudaError_t launch_decode_q4(const voxzip_cache_desc &d, const Q4View &q4, int32
                              int32_t *status, cudaStream_t stream) {
     const int nmax = (max_len > 0 && max_len < d.capacity) ? max_len : d.capacity;
     const int units = layer_count * d.batch * d.kv_heads;
-    int chunk_cap = 0;
-    const int S = plan(d, units, nmax, &chunk_cap);
-    if (S == 0)
+    // Plans are kept per device and shape (lengths in tiles).
+    struct Entry {
+        int device, dim, dtype, two, units, tiles;
+        Plan plan;
+    };
+    thread_local Entry cache[16];
+    thread_local int cache_next = 0;
+    const int G = d.q_heads / d.kv_heads, tiles = (nmax + kTile - 1) / kTile;
+    int device = 0;
+    const cudaError_t got = cudaGetDevice(&device);
+    if (got != cudaSuccess) return got;
+    Plan pl{0, 0, 0, 0};
+    bool found = false;
+    for (const Entry &e : cache)
+        if (e.tiles == tiles && e.units == units && e.device == device && e.dim == d.head_dim && e.dtype == d.dtype && e.two == (G > 8)) {
+            pl = e.plan;
+            found = true;
+        }
+    if (!found) {
+        pl = plan(d, units, nmax);
+        cache[cache_next] = Entry{device, d.head_dim, d.dtype, G > 8, units, tiles, pl};
+        cache_next = (cache_next + 1) % 16;
+    }
+    const int S = pl.S;
+    if (S == 0 || d.batch > 65535 || layer_count > 65535)  // more rows than a cluster holds the logits of, or than a grid's extent
         return launch_decode_q4_rows(d, q4, layer_begin, layer_count, q, k_new, v_new, new_pos, score, pos, len, gamma,
                                      sm_scale, max_len, out, status, stream);
+    const int slice = max(2, (G * d.head_dim / 4 + S - 1) / S);
+    auto inverse = [](int x) { return x <= 1 ? 0u : (uint32_t)((((uint64_t)1 << 32) + x - 1) / x); };
     const float scale = sm_scale > 0.f ? sm_scale : 1.0f / sqrtf((float)d.head_dim);
+    const int resident = pl.resident;
+    const bool later = resident > 0 && resident < units;
     const MmaQ4Params prm{q4, q, k_new, v_new, new_pos, score, pos, len, out, status, d.batch, d.layers, d.q_heads,
-                          d.kv_heads, d.q_heads / d.kv_heads, d.capacity, layer_begin, S, chunk_cap, nmax, gamma,
+                          d.kv_heads, G, d.capacity, layer_begin, pl.chunk_cap, nmax, S, pl.stages, slice,
+                          later ? resident % d.kv_heads : 0, later ? resident / d.kv_heads % d.batch : 0,
+                          later ? resident / d.kv_heads / d.batch : -1, inverse(S), inverse(slice), gamma,
                           scale * 1.4426950408889634f * kUncarry};
     return by_shape(d, [&](auto k) {
         using K = decltype(k);
         const cudaError_t set = configure<K>();
         if (set != cudaSuccess) return set;
         cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3((unsigned)units * (unsigned)S, 1, 1);
+        cfg.gridDim = dim3((unsigned)(d.kv_heads * S), (unsigned)d.batch, (unsigned)layer_count);
         cfg.blockDim = dim3(kThreads, 1, 1);
-        cfg.dynamicSmemBytes = K::Lay::bytes(chunk_cap);
+        cfg.dynamicSmemBytes = K::Lay::bytes(pl.chunk_cap, S, pl.stages);
         cfg.stream = stream;
         cudaLaunchAttribute attr[2];
         attr[0].id = cudaLaunchAttributeClusterDimension;
