@@ -77,6 +77,10 @@ class CacheDesc:
         return self._slots + (self.head_dim // 2,), self._slots + (self.head_dim // Q4_GROUP,)
 
     @functools.cached_property
+    def _q4_exps(self):
+        return self._units + (self.head_dim,)
+
+    @functools.cached_property
     def _c(self):
         """The binding's own C struct (never handed out: c_struct makes a new one)."""
         return self.c_struct()
@@ -592,26 +596,36 @@ def allocate_q4_cache(desc: CacheDesc, device="cuda"):
 
 def _q4_struct(desc: CacheDesc, qc) -> _Q4:
     codes, scales = desc._q4_shapes
-    k_codes, v_codes, k_scale, v_scale, k_exp = (qc["k_codes"], qc["v_codes"], qc["k_scale"], qc["v_scale"],
-                                                 qc["k_exp"])
-    _need(k_codes, "k_codes", torch.uint8, codes)
-    _need(v_codes, "v_codes", torch.uint8, codes)
-    _need(k_scale, "k_scale", torch.bfloat16, scales)
-    _need(v_scale, "v_scale", torch.bfloat16, scales)
-    _need(k_exp, "k_exp", torch.int8, desc._units + (desc.head_dim,))
-    return _Q4(k_codes.data_ptr(), v_codes.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), k_exp.data_ptr())
+    kc, vc, ks, vs, ke = qc["k_codes"], qc["v_codes"], qc["k_scale"], qc["v_scale"], qc["k_exp"]
+    # One pass over what must hold, as in _need (an eager call of a small cache is bound by this binding).
+    try:
+        ok = (kc.dtype is torch.uint8 and vc.dtype is torch.uint8 and ks.dtype is torch.bfloat16 and
+              vs.dtype is torch.bfloat16 and ke.dtype is torch.int8 and kc.is_cuda and vc.is_cuda and ks.is_cuda and
+              vs.is_cuda and ke.is_cuda and kc.is_contiguous() and vc.is_contiguous() and ks.is_contiguous() and
+              vs.is_contiguous() and ke.is_contiguous() and kc.shape == codes and vc.shape == codes and
+              ks.shape == scales and vs.shape == scales and ke.shape == desc._q4_exps)
+    except AttributeError:
+        ok = False
+    if not ok:
+        _need(kc, "k_codes", torch.uint8, codes)
+        _need(vc, "v_codes", torch.uint8, codes)
+        _need(ks, "k_scale", torch.bfloat16, scales)
+        _need(vs, "v_scale", torch.bfloat16, scales)
+        _need(ke, "k_exp", torch.int8, desc._q4_exps)
+    return _Q4(kc.data_ptr(), vc.data_ptr(), ks.data_ptr(), vs.data_ptr(), ke.data_ptr())
 
 
 def voxzip_q4_pack(desc: CacheDesc, qc, layer_begin: int, layer_count: int, k_cache, v_cache, *, stream=None) -> None:
     """Packs rows [0, len) of a cache's units (k_cache, v_cache as for voxzip_decode_step; the lengths are
     qc["len"]) into 4 bits and sets the channel exponents of K."""
+    len_ = qc["len"]
     _need(k_cache, "k_cache", desc.dtype, desc._rows)
     _need(v_cache, "v_cache", desc.dtype, desc._rows)
-    _need(qc["len"], "len", torch.int32, desc._units)
+    _need(len_, "len", torch.int32, desc._units)
     qs = _q4_struct(desc, qc)
     _check("voxzip_q4_pack", lib().voxzip_q4_pack(
-        ctypes.byref(desc._c), ctypes.byref(qs), int(layer_begin), int(layer_count), _ptr(k_cache), _ptr(v_cache),
-        _ptr(qc["len"]), _stream(stream)))
+        ctypes.byref(desc._c), ctypes.byref(qs), layer_begin, layer_count, k_cache.data_ptr(), v_cache.data_ptr(),
+        len_.data_ptr(), _stream(stream)))
 
 
 def voxzip_q4_unpack(desc: CacheDesc, qc, layer_begin: int, layer_count: int, k_out, v_out, *, first: int = 0,
@@ -620,33 +634,47 @@ def voxzip_q4_unpack(desc: CacheDesc, qc, layer_begin: int, layer_count: int, k_
     is slot first + r (from the unit's end if first < 0: -1 is the row appended last), zeros where there is none."""
     if k_out.dim() != 5:
         raise ValueError("k_out must be [B][layer_count][Hkv][rows][D]")
-    rows = k_out.shape[3]
+    rows, len_ = k_out.shape[3], qc["len"]
     shape = (desc.batch, layer_count, desc.kv_heads, rows, desc.head_dim)
     _need(k_out, "k_out", desc.dtype, shape)
     _need(v_out, "v_out", desc.dtype, shape)
-    _need(qc["len"], "len", torch.int32, desc._units)
+    _need(len_, "len", torch.int32, desc._units)
     qs = _q4_struct(desc, qc)
     _check("voxzip_q4_unpack", lib().voxzip_q4_unpack(
-        ctypes.byref(desc._c), ctypes.byref(qs), int(layer_begin), int(layer_count), _ptr(qc["len"]), int(first),
-        int(rows), _ptr(k_out), _ptr(v_out), _stream(stream)))
+        ctypes.byref(desc._c), ctypes.byref(qs), layer_begin, layer_count, len_.data_ptr(), first, rows,
+        k_out.data_ptr(), v_out.data_ptr(), _stream(stream)))
 
 
 def voxzip_decode_step_q4(desc: CacheDesc, qc, layer_begin: int, layer_count: int, q, k_new, v_new, new_pos,
                           gamma: float, out, *, sm_scale: float = 0.0, max_len: int = 0, stream=None) -> None:
     """One decode step (Eq. 1, Eq. 2, Eq. 6) on a cache held in 4 bits; the new row is packed as it is appended."""
-    B, Hq, H, D = desc.batch, desc.q_heads, desc.kv_heads, desc.head_dim
-    _need(q, "q", desc.dtype, (layer_count, B, Hq, D))
-    _need(k_new, "k_new", desc.dtype, (layer_count, B, H, D))
-    _need(v_new, "v_new", desc.dtype, (layer_count, B, H, D))
-    _need(out, "out", desc.dtype, (layer_count, B, Hq, D))
-    _need(new_pos, "new_pos", torch.int32, (B,))
+    dt, B = desc.dtype, desc.batch
+    heads = (layer_count, B, desc.q_heads, desc.head_dim)
+    rows = (layer_count, B, desc.kv_heads, desc.head_dim)
     score, pos, len_ = qc["score"], qc["pos"], qc["len"]
-    _check_dense_state(desc, score, pos, len_)
+    try:
+        ok = (q.dtype is dt and k_new.dtype is dt and v_new.dtype is dt and out.dtype is dt and
+              new_pos.dtype is torch.int32 and score.dtype is torch.float32 and pos.dtype is torch.int32 and
+              len_.dtype is torch.int32 and q.is_cuda and k_new.is_cuda and v_new.is_cuda and out.is_cuda and
+              new_pos.is_cuda and score.is_cuda and pos.is_cuda and len_.is_cuda and q.is_contiguous() and
+              k_new.is_contiguous() and v_new.is_contiguous() and out.is_contiguous() and new_pos.is_contiguous() and
+              score.is_contiguous() and pos.is_contiguous() and len_.is_contiguous() and q.shape == heads and
+              out.shape == heads and k_new.shape == rows and v_new.shape == rows and new_pos.shape == (B,) and
+              score.shape == desc._slots and pos.shape == desc._slots and len_.shape == desc._units)
+    except AttributeError:
+        ok = False
+    if not ok:
+        _need(q, "q", dt, heads)
+        _need(k_new, "k_new", dt, rows)
+        _need(v_new, "v_new", dt, rows)
+        _need(out, "out", dt, heads)
+        _need(new_pos, "new_pos", torch.int32, (B,))
+        _check_dense_state(desc, score, pos, len_)
     qs = _q4_struct(desc, qc)
     _check("voxzip_decode_step_q4", lib().voxzip_decode_step_q4(
-        ctypes.byref(desc._c), ctypes.byref(qs), int(layer_begin), int(layer_count), _ptr(q), _ptr(k_new), _ptr(v_new),
-        _ptr(new_pos), _ptr(score), _ptr(pos), _ptr(len_), float(gamma), float(sm_scale), int(max_len), _ptr(out),
-        _stream(stream)))
+        ctypes.byref(desc._c), ctypes.byref(qs), layer_begin, layer_count, q.data_ptr(), k_new.data_ptr(),
+        v_new.data_ptr(), new_pos.data_ptr(), score.data_ptr(), pos.data_ptr(), len_.data_ptr(), gamma, sm_scale, max_len,
+        out.data_ptr(), _stream(stream)))
 
 
 def voxzip_evict_q4(desc: CacheDesc, qc, layer_begin: int, layer_count: int, budget, *, sink: int = 4,
