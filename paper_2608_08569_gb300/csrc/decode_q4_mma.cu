@@ -9,7 +9,7 @@
 // pattern, the integer v in 0..255 is v 2^-133 (a subnormal or in the first binade above, one straight line), so a
 // code in bits 0-3 is c 2^-133 and one in bits 4-7 is 16 c 2^-133; q and p carry 2^84 (q of the odd pairs 2^80), and
 // what is left, 2^-49, goes into factors that are applied anyway. The stored code is c + 8: for K the accumulators
-// start from -8 sum q; for V eight is subtracted from the operands (an output may be far smaller than its weights'
+// start from -8 sum q (with fp32 activations 8 is subtracted from the operands, as for V); for V eight is subtracted from the operands (an output may be far smaller than its weights'
 // sum, so that a correction afterwards would cancel: with one, outputs of 1e-6 were off by as much).
 // fp32 activations are split into three bf16 parts (24 bits), of which each makes a product of its own, so that
 // only fp32 sums round.
@@ -327,7 +327,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && kParts == 1 ? 4 : 3) deco
             float sum = ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
             sum += __shfl_xor_sync(0xffffffffu, sum, 1);
             sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-            if (qd == 0) c_smem[nj * 8 + g] = sum * (-8.f * (kCarry * 0x1p-133f));
+            if (qd == 0) c_smem[nj * 8 + g] = kParts == 1 ? sum * (-8.f * (kCarry * 0x1p-133f)) : 0.f;
 #pragma unroll
             for (int ks = 0; ks < 2; ++ks) {
                 uint32_t b0[kParts], b1[kParts];
@@ -397,19 +397,34 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && kParts == 1 ? 4 : 3) deco
 #pragma unroll
             for (int j = 0; j < J; ++j) {
                 float acc[NT][4];
+                uint32_t x[2][4];
 #pragma unroll
                 for (int ks = 0; ks < 2; ++ks) {
                     const uint32_t x0 = w0.w[j] >> (8 * ks), x1 = w1.w[j] >> (8 * ks);
+                    x[ks][0] = x0 & kLow, x[ks][1] = x1 & kLow, x[ks][2] = x0 & kHigh, x[ks][3] = x1 & kHigh;
+                    if constexpr (kParts > 1)  // codes without their offset: sums of smaller terms round less
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
+                        for (int k = 0; k < 4; ++k) x[ks][k] = minus(x[ks][k], k < 2 ? 0x0008 : 0x0080);
+                }
 #pragma unroll
-                        for (int i2 = 0; i2 < kParts; ++i2) {
-                            const uint2 b = q_operand(i2, nt, 2 * j + ks);
-                            if (ks == 0 && i2 == 0)
-                                mma_from(acc[nt], c_init[nt][j], x0 & kLow, x1 & kLow, x0 & kHigh, x1 & kHigh, b);
-                            else
-                                mma(acc[nt], x0 & kLow, x1 & kLow, x0 & kHigh, x1 & kHigh, b);
-                        }
+                for (int nt = 0; nt < NT; ++nt) {
+                    if constexpr (kParts == 1) {
+                        mma_from(acc[nt], c_init[nt][j], x[0][0], x[0][1], x[0][2], x[0][3], q_operand(0, nt, 2 * j));
+                        mma(acc[nt], x[1][0], x[1][1], x[1][2], x[1][3], q_operand(0, nt, 2 * j + 1));
+                    } else {
+                        // The tensor cores cut off what an addition does not hold: the lesser parts' sum first, and the
+                        // greatest part's products added to it with rounding.
+                        float hi[2][4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) acc[nt][k] = hi[0][k] = hi[1][k] = 0.f;
+#pragma unroll
+                        for (int part = kParts - 1; part >= 0; --part)
+#pragma unroll
+                            for (int ks = 0; ks < 2; ++ks)
+                                mma(part ? acc[nt] : hi[ks], x[ks][0], x[ks][1], x[ks][2], x[ks][3], q_operand(part, nt, 2 * j + ks));
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) acc[nt][k] += hi[0][k] + hi[1][k];
+                    }
                 }
                 const float a = j & 1 ? high_bf16(s0.w[j / 2]) : low_bf16(s0.w[j / 2]);
                 const float b = j & 1 ? high_bf16(s1.w[j / 2]) : low_bf16(s1.w[j / 2]);
@@ -531,11 +546,23 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && kParts == 1 ? 4 : 3) deco
                     uint32_t b0[kWeightParts], b1[kWeightParts];
                     split_pair<kWeightParts>(times(p01[nt], make_float2(sc.x, sc.y)), b0);
                     split_pair<kWeightParts>(times(p23[nt], make_float2(sc.z, sc.w)), b1);
+                    if constexpr (kParts == 1) {
 #pragma unroll
-                    for (int i2 = 0; i2 < kWeightParts; ++i2) {
-                        const uint2 b = make_uint2(b0[i2], b1[i2]);
-                        mma(o[2 * j][nt], a0, a1, a2, a3, b);
-                        mma(o[2 * j + 1][nt], c0, c1, c2, c3, b);
+                        for (int part = kWeightParts - 1; part >= 0; --part) {
+                            const uint2 b = make_uint2(b0[part], b1[part]);
+                            mma(o[2 * j][nt], a0, a1, a2, a3, b);
+                            mma(o[2 * j + 1][nt], c0, c1, c2, c3, b);
+                        }
+                    } else {  // 16 tokens' sums, least parts first, added with rounding
+                        float t0[4] = {0.f, 0.f, 0.f, 0.f}, t1[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int part = kWeightParts - 1; part >= 0; --part) {
+                            const uint2 b = make_uint2(b0[part], b1[part]);
+                            mma(t0, a0, a1, a2, a3, b);
+                            mma(t1, c0, c1, c2, c3, b);
+                        }
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) o[2 * j][nt][k] += t0[k], o[2 * j + 1][nt][k] += t1[k];
                     }
                 }
             }
