@@ -6,6 +6,10 @@ generated token over all layers and an eviction every ``interval`` steps. It kee
 upper bound on the cache length (read back once after stage 1) so that every decode launch is
 sized without a device-to-host sync; the decode loop of a request can therefore be captured once
 in a CUDA graph and replayed (``capture_loop``).
+
+With ``kv_bits=4`` the session's cache holds its rows in 4 bits per channel: stage 1 runs into a staging cache of
+plain rows, which is packed right after it, and decode steps and evictions work on the packed rows. The staging
+rows are needed during ``prefill`` alone, so sessions may share them (``staging``).
 """
 from __future__ import annotations
 
@@ -16,11 +20,18 @@ from . import _native as N
 
 class Session:
     """`budget` holds one budget per sequence, or per sequence and layer ([B][L]); `history` and
-    `compaction` select the eviction policy (see voxzip_evict_ex)."""
+    `compaction` select the eviction policy (see voxzip_evict_ex). `kv_bits` is 16 (rows in the descriptor's
+    dtype) or 4; `staging`, with 4, a dict of k and v [B][L][Hkv][C][D] that stage 1 may overwrite."""
 
     def __init__(self, desc: N.CacheDesc, budget, gamma: float, *, sink: int = 4, recent_frac: float = 0.2,
                  history: bool = True, compaction: str = "ordered", device="cuda", cache=None,
-                 pages: int | None = None):
+                 pages: int | None = None, kv_bits: int = 16, staging=None):
+        if kv_bits not in (4, 16):
+            raise ValueError("kv_bits must be 4 or 16")
+        if kv_bits == 4 and pages is not None:
+            raise ValueError("a paged cache holds its rows in the descriptor's dtype: kv_bits=4 needs pages=None")
+        self.kv_bits = kv_bits
+        self.staging = staging
         self.desc = desc
         self.device = torch.device(device)
         self.gamma = float(gamma)
@@ -35,6 +46,8 @@ class Session:
             self.cache = cache
         elif self.paged:
             self.cache = N.allocate_paged_cache(desc, pages, self.device)
+        elif kv_bits == 4:
+            self.cache = N.allocate_q4_cache(desc, self.device)
         else:
             self.cache = N.allocate_cache(desc, self.device)
         self.n_max = 0
@@ -53,10 +66,18 @@ class Session:
                                        span_start, span_end, span_groups, slot_map=slot_map, anchor_k=anchor_k,
                                        anchor_v=anchor_v, workspace=self.workspace, stream=stream)
         else:
+            rows = c
+            if self.kv_bits == 4:
+                if self.staging is None:
+                    new = lambda: torch.empty(self.desc._rows, dtype=self.desc.dtype, device=self.device)  # noqa: E731
+                    self.staging = dict(k=new(), v=new())
+                rows = self.staging
             N.voxzip_anchor_fuse(self.desc, k_prefill, v_prefill, in_len, audio_begin, audio_len, span_off,
-                                 span_start, span_end, span_groups, c["k"], c["v"], c["score"], c["pos"], c["len"],
-                                 slot_map=slot_map, anchor_k=anchor_k, anchor_v=anchor_v, workspace=self.workspace,
-                                 stream=stream)
+                                 span_start, span_end, span_groups, rows["k"], rows["v"], c["score"], c["pos"],
+                                 c["len"], slot_map=slot_map, anchor_k=anchor_k, anchor_v=anchor_v,
+                                 workspace=self.workspace, stream=stream)
+            if self.kv_bits == 4:
+                N.voxzip_q4_pack(self.desc, c, 0, self.desc.layers, rows["k"], rows["v"], stream=stream)
         if read_back:
             self.n_max = int(c["len"].max().item())
         else:
@@ -70,6 +91,9 @@ class Session:
         if self.paged:
             N.voxzip_decode_step_paged(self.desc, c, layer_begin, lc, q, k_new, v_new, new_pos, self.gamma, out,
                                        max_len=self.n_max + 1, stream=stream)
+        elif self.kv_bits == 4:
+            N.voxzip_decode_step_q4(self.desc, c, layer_begin, lc, q, k_new, v_new, new_pos, self.gamma, out,
+                                    max_len=self.n_max + 1, stream=stream)
         else:
             N.voxzip_decode_step(self.desc, layer_begin, lc, q, k_new, v_new, new_pos, c["k"], c["v"], c["score"],
                                  c["pos"], c["len"], self.gamma, out, max_len=self.n_max + 1, stream=stream)
@@ -83,6 +107,9 @@ class Session:
             N.voxzip_evict_paged(self.desc, c, layer_begin, lc, self.budget, sink=self.sink,
                                  recent_frac=self.recent_frac, history=self.history, compaction=self.compaction,
                                  stream=stream)
+        elif self.kv_bits == 4:
+            N.voxzip_evict_q4(self.desc, c, layer_begin, lc, self.budget, sink=self.sink, recent_frac=self.recent_frac,
+                              history=self.history, compaction=self.compaction, stream=stream)
         elif self.history and self.compaction == "ordered" and self.budget.dim() == 1:
             N.voxzip_evict(self.desc, layer_begin, lc, c["k"], c["v"], c["score"], c["pos"], c["len"], self.budget,
                            sink=self.sink, recent_frac=self.recent_frac, stream=stream)

@@ -143,3 +143,14 @@ def test_outlier_channels_do_not_cost_the_others_their_codes():
 def test_the_header_states_the_capacity_rule(V):
     text = open(os.path.join(B.ROOT, "include", "voxzip.h")).read()
     assert int(re.search(r"VOXZIP_Q4_CAPACITY_MULTIPLE (\d+)", text).group(1)) == V.Q4_CAPACITY_MULTIPLE
+
+
+def test_the_session_checks_kv_bits(V):
+    from paper_2608_08569_gb300.session import Session
+    desc = V.CacheDesc(1, 1, 2, 1, 64, 64)
+    with pytest.raises(ValueError, match="kv_bits"):
+        Session(desc, (32,), 0.9, device="cpu", kv_bits=8)
+    with pytest.raises(ValueError, match="paged"):
+        Session(desc, (32,), 0.9, device="cpu", kv_bits=4, pages=4)
+    s = Session(desc, (32,), 0.9, device="cpu", kv_bits=4)
+    assert s.cache["k_codes"].shape == (1, 1, 1, 64, 32) and "k" not in s.cache

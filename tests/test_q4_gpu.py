@@ -400,6 +400,57 @@ def test_evict_device_errors(V):
     assert V.voxzip_get_status() == V.DEV_BAD_POSITIONS
 
 
+# ----------------------------------------------------------------------------- a request
+
+@pytest.mark.parametrize("compaction", ["ordered", "fill"])
+def test_session_runs_a_request(V, compaction):
+    """Session(kv_bits=4) is stage 1, packing, decode steps and evictions in turn; its loop replays from a graph; stage 1
+    and lengths are those of the plain session, and the first outputs are near its own (keys and values are held to
+    about a tenth of their spread: cosine above 0.9)."""
+    from gpu_harness import make_inputs
+    from paper_2608_08569_gb300 import workloads as W
+    from paper_2608_08569_gb300.session import Session
+
+    w = W.scaled(W.CONFIGS["short"], layers=3, steps=70, name="short_l3")
+    inp = make_inputs(w, "cuda:0")
+    B, L, Hq, H, D = w.batch, w.layers, w.q_heads, w.kv_heads, w.head_dim
+    desc = V.CacheDesc(B, L, Hq, H, D, -(-w.capacity // 4) * 4, w.dtype)
+    i32 = lambda a: torch.as_tensor(np.asarray(a), dtype=torch.int32, device="cuda")
+    sp = inp["spans"]
+    prompt = (inp["k_pre"], inp["v_pre"], i32(w.in_len), i32([w.audio_begin] * B), i32(w.audio_len), i32(sp.off),
+              i32(sp.start), i32(sp.end), i32(sp.groups))
+    plain = Session(desc, w.budget, w.gamma, compaction=compaction)
+    s = Session(desc, w.budget, w.gamma, compaction=compaction, kv_bits=4)
+    plain.prefill(*prompt)
+    s.prefill(*prompt)
+    assert torch.equal(plain.cache["len"], s.cache["len"]) and torch.equal(plain.cache["pos"], s.cache["pos"])
+    by_hand = V.allocate_q4_cache(desc)
+    for n in ("score", "pos", "len"):
+        by_hand[n].copy_(s.cache[n])
+    V.voxzip_q4_pack(desc, by_hand, 0, L, plain.cache["k"], plain.cache["v"])
+    outs = [torch.empty(w.steps, L, B, Hq, D, dtype=w.dtype, device="cuda") for _ in range(3)]
+    n = s.n_max
+    for t in range(w.steps):
+        args = (inp["q"][t], inp["kn"][t], inp["vn"][t], inp["new_pos"][t])
+        s.decode(*args, outs[0][t])
+        V.voxzip_decode_step_q4(desc, by_hand, 0, L, *args, w.gamma, outs[1][t], max_len=n + 1)
+        n += 1
+        if t == 0:
+            plain.decode(*args, outs[2][t])
+        if (t + 1) % 32 == 0:
+            s.evict()
+            V.voxzip_evict_q4(desc, by_hand, 0, L, s.budget, compaction=compaction)
+            n = min(n, max(w.budget))
+    assert torch.equal(outs[0], outs[1])
+    assert all(torch.equal(by_hand[x], s.cache[x]) for x in ("score", "pos", "len", "k_codes", "v_codes", "k_exp"))
+    assert torch.nn.functional.cosine_similarity(outs[0][0].float(), outs[2][0].float(), dim=-1).min() > 0.9
+    s.prefill(*prompt)
+    graph = s.capture_loop(inp["q"], inp["kn"], inp["vn"], inp["new_pos"], outs[2], 32)
+    graph.replay()
+    assert torch.equal(outs[0], outs[2]) and torch.equal(by_hand["score"], s.cache["score"])
+    assert V.voxzip_get_status() == 0
+
+
 # ----------------------------------------------------------------------------- the checked build
 
 @pytest.mark.skipif(os.environ.get("VOXZIP_CHECKED", "0") not in ("", "0"), reason="this is the checked run")
