@@ -708,7 +708,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && kParts == 1 ? 4 : 3) deco
         float f[GP];
 #pragma unroll
         for (int h = 0; h < GP; ++h) f[h] = f_w[warp * GP + h];
-        auto update = [&](int i, float before) {
+        auto mass = [&](int i) {
             float add = 0.f;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
@@ -717,14 +717,19 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && kParts == 1 ? 4 : 3) deco
                 add += ((a.x * f[nt * 8] + a.y * f[nt * 8 + 1]) + (a.z * f[nt * 8 + 2] + a.w * f[nt * 8 + 3])) +
                        ((b.x * f[nt * 8 + 4] + b.y * f[nt * 8 + 5]) + (b.z * f[nt * 8 + 6] + b.w * f[nt * 8 + 7]));
             }
-            if (VOXZIP_IN_RANGE(p.status, j0 + i < p.C))
+            return add;
+        };
+        auto update = [&](int i, float before, float add) {
+            if (i < cnt && VOXZIP_IN_RANGE(p.status, j0 + i < p.C))
                 p.score[row_base + j0 + i] = j0 + i == n_old ? add : p.gamma * before + add;
         };
-        int i = warp * kTile + lane;
+        const int i0 = warp * kTile + lane;  // below the weights' room, whatever cnt is
+        float add[kAhead];
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k, i += kThreads)
-            if (i < cnt) update(i, old[k]);
-        for (; i < cnt; i += kThreads) update(i, p.score[row_base + j0 + i]);
+        for (int k = 0; k < kAhead; ++k) add[k] = mass(i0 + k * kThreads < cnt ? i0 + k * kThreads : i0);
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) update(i0 + k * kThreads, old[k], add[k]);
+        for (int i = i0 + kAhead * kThreads; i < cnt; i += kThreads) update(i, p.score[row_base + j0 + i], mass(i));
     }
     if (rank == 0 && tid == 0) p.len[ui.cache_unit] = n;
 }

@@ -37,14 +37,15 @@ __device__ __forceinline__ int channel_exponent(uint32_t amax, uint32_t mid) {
     return min(max((int)(__float_as_uint(r) >> 23) - 127, -kQ4MaxExp), kQ4MaxExp);
 }
 
-// Sixteen channels as they lie in memory: half a group.
+// Sixteen channels as they lie in memory: half a group, the eight at p and the eight at p + 16 (two lanes then load
+// whole 32-byte sectors).
 template <typename T>
 struct Half {
     static constexpr int kVecs = (int)sizeof(T);
     uint4 v[kVecs];
     __device__ __forceinline__ void load(const T *p) {
 #pragma unroll
-        for (int i = 0; i < kVecs; ++i) v[i] = reinterpret_cast<const uint4 *>(p)[i];
+        for (int i = 0; i < kVecs; ++i) v[i] = reinterpret_cast<const uint4 *>(p)[i + (i >= kVecs / 2 ? kVecs / 2 : 0)];
     }
     __device__ __forceinline__ const uint32_t *words() const { return reinterpret_cast<const uint32_t *>(v); }
     __device__ __forceinline__ uint32_t *words() { return reinterpret_cast<uint32_t *>(v); }
@@ -124,8 +125,8 @@ __device__ __forceinline__ uint32_t eight_codes(X &&x, float inv) {
 template <typename T, int D, bool kCluster>
 __global__ void __launch_bounds__(kThreads, 4) q4_pack_kernel(const PackParams p) {
     constexpr int J = D / kQ4Group, kLanes = D / 16, kRows = 32 / kLanes * kWarps;  // rows the CTA takes at a time
-    constexpr int kAhead = sizeof(T) == 2 ? 4 : 2;                                  // of which so many are on their way
-    __shared__ uint32_t amax[D], amax_unit[D];
+    constexpr int kAhead = 2;  // of which so many are on their way
+    __shared__ __align__(16) uint32_t amax[D], amax_unit[D];
     __shared__ float inv_pow[D];
     __shared__ uint32_t mid;
     const int tid = threadIdx.x;
@@ -140,20 +141,23 @@ __global__ void __launch_bounds__(kThreads, 4) q4_pack_kernel(const PackParams p
         return;
     }
     __syncthreads();
-    const int c16 = tid % kLanes, r0 = rank * kRows + tid / kLanes, step = S * kRows;
-    const T *k = static_cast<const T *>(p.k_cache) + ui.cache_unit * p.C * D + c16 * 16;
-    const T *v = static_cast<const T *>(p.v_cache) + ui.cache_unit * p.C * D + c16 * 16;
+    // This CTA's rows are [first, last).
+    const int share = ((n + S - 1) / S + kRows - 1) / kRows * kRows, first = min(n, rank * share), last = min(n, first + share);
+    const int j = tid % kLanes >> 1, half = tid & 1, r0 = first + tid / kLanes;
+    const T *k = static_cast<const T *>(p.k_cache) + ui.cache_unit * p.C * D + 32 * j + 8 * half;
+    const T *v = static_cast<const T *>(p.v_cache) + ui.cache_unit * p.C * D + 32 * j + 8 * half;
+    auto channel = [&](int i) { return 32 * j + 8 * half + i + (i & 8); };  // of the lane's i-th value
     // Largest magnitudes: of bf16 as pairs of 16-bit integers (the order of magnitudes is that of their bits).
     constexpr int kTop = 4 * Half<T>::kVecs;
     uint32_t top[kTop];
 #pragma unroll
     for (int i = 0; i < kTop; ++i) top[i] = 0u;
-    for (int r = r0; r < n; r += kAhead * step) {
+    for (int r = r0; r < last; r += kAhead * kRows) {
         Half<T> x[kAhead];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             x[u] = Half<T>{};
-            if (r + u * step < n) x[u].load(k + (int64_t)(r + u * step) * D);
+            if (r + u * kRows < last) x[u].load(k + (int64_t)(r + u * kRows) * D);
         }
 #pragma unroll
         for (int u = 0; u < kAhead; ++u)
@@ -166,7 +170,7 @@ __global__ void __launch_bounds__(kThreads, 4) q4_pack_kernel(const PackParams p
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
         const uint32_t t = sizeof(T) == 2 ? (i & 1 ? top[i / 2] & 0xffff0000u : top[i / 2] << 16) : top[i % kTop];
-        atomicMax(&amax[c16 * 16 + i], t);
+        atomicMax(&amax[channel(i)], t);
     }
     if constexpr (kCluster) {
         cg::cluster_group cluster = cg::this_cluster();
@@ -186,7 +190,11 @@ __global__ void __launch_bounds__(kThreads, 4) q4_pack_kernel(const PackParams p
     if (tid < D) {
         int before = 0;
         const uint32_t own = amax_unit[tid];
-        for (int d = 0; d < D; ++d) before += amax_unit[d] < own || (amax_unit[d] == own && d < tid);
+#pragma unroll 4
+        for (int d = 0; d < D; d += 4) {
+            const uint4 x = *reinterpret_cast<const uint4 *>(amax_unit + d);
+            before += (x.x < own + (d < tid)) + (x.y < own + (d + 1 < tid)) + (x.z < own + (d + 2 < tid)) + (x.w < own + (d + 3 < tid));
+        }
         if (before == (D - 1) / 2) mid = own;
     }
     __syncthreads();
@@ -196,28 +204,27 @@ __global__ void __launch_bounds__(kThreads, 4) q4_pack_kernel(const PackParams p
         if (rank == 0) p.q4.k_exp[ui.cache_unit * D + tid] = (int8_t)e;
     }
     __syncthreads();
-    const float *f = inv_pow + c16 * 16;
+    auto f = [&](int i) { return inv_pow[channel(i)]; };
     uint32_t f2[8];  // as bf16 pairs
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f2[i] = ptx::pack_bf16(f[2 * i], f[2 * i + 1]);
+    for (int i = 0; i < 8; ++i) f2[i] = ptx::pack_bf16(f(2 * i), f(2 * i + 1));
 
-    const int j = c16 >> 1, half = c16 & 1;
-    const int rounds = (n - rank * kRows + step - 1) / step;  // the same for the warp's lanes: shuffles
+    const int rounds = (last - first + kRows - 1) / kRows;  // the same for the warp's lanes: shuffles
     constexpr int kBoth = kAhead / 2;
     for (int i0 = 0; i0 < rounds; i0 += kBoth) {
         Half<T> a[kBoth], b[kBoth];
 #pragma unroll
         for (int u = 0; u < kBoth; ++u) {
-            const int r = r0 + (i0 + u) * step;
+            const int r = r0 + (i0 + u) * kRows;
             a[u] = b[u] = Half<T>{};
-            if (r < n) {
+            if (r < last) {
                 a[u].load(k + (int64_t)r * D);
                 b[u].load(v + (int64_t)r * D);
             }
         }
 #pragma unroll
         for (int u = 0; u < kBoth; ++u) {
-            const int r = r0 + (i0 + u) * step;
+            const int r = r0 + (i0 + u) * kRows;
             const int64_t row = ui.cache_unit * p.C + r;
             uint32_t kw[2], vw[2];
             float ks, vs;
@@ -227,13 +234,13 @@ __global__ void __launch_bounds__(kThreads, 4) q4_pack_kernel(const PackParams p
 #pragma unroll
                 for (int i = 0; i < kTop; ++i) {
                     if constexpr (sizeof(T) == 2) x.words()[i] = as_word(__hmul2(as_pair(x.words()[i]), as_pair(f2[i])));
-                    else x.words()[i] = __float_as_uint(x.at(i) * f[i]);
+                    else x.words()[i] = __float_as_uint(x.at(i) * f(i));
                 }
                 ks = q4_scale(group_key(x));
                 const float inv = q4_inverse(ks);
                 if (sizeof(T) == 2 && fabsf(ks) < 0x1p-118f)  // where those would be codes
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) kw[h] = eight_codes<true>([&](int i) { return a[u].at(8 * h + i) * f[8 * h + i]; }, inv);
+                    for (int h = 0; h < 2; ++h) kw[h] = eight_codes<true>([&](int i) { return a[u].at(8 * h + i) * f(8 * h + i); }, inv);
                 else
 #pragma unroll
                     for (int h = 0; h < 2; ++h) kw[h] = eight_codes<true>([&](int i) { return x.at(8 * h + i); }, inv);
@@ -242,17 +249,17 @@ __global__ void __launch_bounds__(kThreads, 4) q4_pack_kernel(const PackParams p
                 vs = q4_scale(group_key(b[u]));
                 const float inv = q4_inverse(vs);
 #pragma unroll
-                for (int h = 0; h < 2; ++h)  // half-words g = 4 half + 2 h, + 1
+                for (int h = 0; h < 2; ++h)  // half-words g = 2 half + 4 h, + 1
                     vw[h] = eight_codes<false>([&](int i) { return b[u].at(8 * h + i); }, inv);
             }
-            // Words of V pair the groups 2 i and 2 i + 1: the even one's lane takes the first two g, the odd one's the rest.
+            // Words of V pair the groups 2 i and 2 i + 1: the even one's lane takes the first two g, the odd one's the others.
             const uint32_t other = __shfl_xor_sync(0xffffffffu, j & 1 ? vw[0] : vw[1], 2);
             const uint32_t even = j & 1 ? other : vw[0], odd = j & 1 ? vw[1] : other;
-            if (r < n) {
-                uint32_t *kc = reinterpret_cast<uint32_t *>(p.q4.k_codes + row * (D / 2)) + 2 * half * J + j;
-                uint32_t *vc = reinterpret_cast<uint32_t *>(p.q4.v_codes + row * (D / 2)) + (4 * half + 2 * (j & 1)) * (J / 2) + (j >> 1);
+            if (r < last) {
+                uint32_t *kc = reinterpret_cast<uint32_t *>(p.q4.k_codes + row * (D / 2)) + half * J + j;
+                uint32_t *vc = reinterpret_cast<uint32_t *>(p.q4.v_codes + row * (D / 2)) + (2 * half + 4 * (j & 1)) * (J / 2) + (j >> 1);
                 kc[0] = kw[0];
-                kc[J] = kw[1];
+                kc[2 * J] = kw[1];
                 vc[0] = __byte_perm(even, odd, 0x5410);
                 vc[J / 2] = __byte_perm(even, odd, 0x7632);
                 if (half == 0) {
@@ -300,75 +307,69 @@ __device__ __forceinline__ void eight_values(uint32_t w, S &&scale, float2 (&x)[
         x[i] = mul2(add2(make_float2(y[2 * i], y[2 * i + 1]), make_float2(-8388616.f, -8388616.f)), scale(i));
 }
 
-// Row r of the output is slot first + r (from the unit's end if first < 0); zeros where there is none. A lane takes 16
-// channels (two words of K, and of V the half-words of its group from two words that it shares with the next group's
-// lane), a CTA kAhead times kRows rows of a unit.
+// Row r of the output is slot first + r (from the unit's end if first < 0); zeros where there is none. A lane takes 8
+// channels, so that a warp's stores are whole lines: a word of K, and of V the half-words of its group from two words
+// that it shares with the next group's lane. A CTA takes kAhead times kRows rows of a unit.
 template <int D>
 struct Unpack {
-    static constexpr int kLanes = D / 16, kRows = kThreads / kLanes, kAhead = 2;
+    static constexpr int kLanes = D / 8, kRows = kThreads / kLanes, kAhead = 2;
 };
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads, 4) q4_unpack_kernel(const UnpackParams p) {
+__global__ void __launch_bounds__(kThreads, 6) q4_unpack_kernel(const UnpackParams p) {
     using U = Unpack<D>;
     constexpr int J = D / kQ4Group, kRows = U::kRows, kAhead = U::kAhead;
-    const int c16 = threadIdx.x % U::kLanes, j = c16 >> 1, half = c16 & 1;
+    const int c8 = threadIdx.x % U::kLanes, j = c8 >> 2, q = c8 & 3;
     const UnitIdx ui = unit_of(blockIdx.x, p.B, p.L, p.Hkv, p.layer_begin);
     ptx::grid_dependency_wait();
     const int32_t n = p.len[ui.cache_unit];
-    const int4 exps = *reinterpret_cast<const int4 *>(p.q4.k_exp + ui.cache_unit * D + c16 * 16);
+    const int2 exps = *reinterpret_cast<const int2 *>(p.q4.k_exp + ui.cache_unit * D + c8 * 8);
     if (n < 0 || n > p.C) {
         if (threadIdx.x == 0 && blockIdx.y == 0) raise_status(p.status, VOXZIP_DEV_CAPACITY);
         return;
     }
-    float2 f[8];
+    float2 f[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int e = (i < 2 ? exps.x : i < 4 ? exps.y : i < 6 ? exps.z : exps.w) >> (16 * (i & 1));
+    for (int i = 0; i < 4; ++i) {
+        const int e = (i < 2 ? exps.x : exps.y) >> (16 * (i & 1));
         f[i] = make_float2(exp2_int((int)(int8_t)e), exp2_int((int)(int8_t)(e >> 8)));
     }
     const int64_t out_unit = ((int64_t)ui.b * p.layer_count + ui.l_local) * p.Hkv + ui.h;
     const int64_t shift = (int64_t)p.first + (p.first < 0 ? n : 0);
-    T *k_out = static_cast<T *>(p.k_out) + out_unit * p.rows * D + c16 * 16;
-    T *v_out = static_cast<T *>(p.v_out) + out_unit * p.rows * D + c16 * 16;
+    T *k_out = static_cast<T *>(p.k_out) + out_unit * p.rows * D + c8 * 8;
+    T *v_out = static_cast<T *>(p.v_out) + out_unit * p.rows * D + c8 * 8;
+    const uint32_t *kc = reinterpret_cast<const uint32_t *>(p.q4.k_codes + ui.cache_unit * p.C * (D / 2)) + q * J + j;
+    const uint32_t *vc = reinterpret_cast<const uint32_t *>(p.q4.v_codes + ui.cache_unit * p.C * (D / 2)) + (2 * q + (j & 1)) * (J / 2) + (j >> 1);
+    const __nv_bfloat16 *ks0 = p.q4.k_scale + ui.cache_unit * p.C * J + j, *vs0 = p.q4.v_scale + ui.cache_unit * p.C * J + j;
     // every lane of a warp goes round as often: shuffles
-    for (int64_t base = (int64_t)blockIdx.y * (kAhead * kRows); base < p.rows; base += (int64_t)gridDim.y * (kAhead * kRows)) {
-        const int64_t r0 = base + threadIdx.x / U::kLanes;
-        uint32_t kw[kAhead][2], vw[kAhead][2];
+    for (int base = blockIdx.y * (kAhead * kRows); base < p.rows; base += gridDim.y * (kAhead * kRows)) {
+        const int r0 = base + (int)threadIdx.x / U::kLanes;
+        uint32_t kw[kAhead], vw[kAhead];
         float ks[kAhead], vs[kAhead];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             const int64_t slot = r0 + u * kRows + shift;
-            kw[u][0] = kw[u][1] = vw[u][0] = vw[u][1] = 0u;
+            kw[u] = vw[u] = 0u;
             ks[u] = vs[u] = 0.f;
             if (r0 + u * kRows < p.rows && slot >= 0 && slot < n) {
-                const int64_t row = ui.cache_unit * p.C + slot;
-                const uint32_t *kc = reinterpret_cast<const uint32_t *>(p.q4.k_codes + row * (D / 2)) + 2 * half * J + j;
-                const uint32_t *vc = reinterpret_cast<const uint32_t *>(p.q4.v_codes + row * (D / 2)) + (4 * half + 2 * (j & 1)) * (J / 2) + (j >> 1);
-                kw[u][0] = kc[0];
-                kw[u][1] = kc[J];
-                vw[u][0] = vc[0];
-                vw[u][1] = vc[J / 2];
-                ks[u] = __bfloat162float(p.q4.k_scale[row * J + j]);
-                vs[u] = __bfloat162float(p.q4.v_scale[row * J + j]);
+                kw[u] = kc[slot * (D / 8)];
+                vw[u] = vc[slot * (D / 8)];
+                ks[u] = __bfloat162float(ks0[slot * J]);
+                vs[u] = __bfloat162float(vs0[slot * J]);
             }
         }
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            // even lanes hold the first two half-words of both groups, odd ones the last two
-            const uint32_t even = __byte_perm(vw[u][0], vw[u][1], 0x5410), odd = __byte_perm(vw[u][0], vw[u][1], 0x7632);
-            const uint32_t other = __shfl_xor_sync(0xffffffffu, j & 1 ? even : odd, 2);
-            const uint32_t v0 = j & 1 ? other : even, v1 = j & 1 ? odd : other;
-            const int64_t r = r0 + u * kRows;
+            // even groups' lanes hold half-words g = 2 q of both, odd ones' g = 2 q + 1
+            const uint32_t other = __shfl_xor_sync(0xffffffffu, vw[u], 4);
+            const uint32_t v = j & 1 ? __byte_perm(other, vw[u], 0x7632) : __byte_perm(vw[u], other, 0x5410);
+            const int r = r0 + u * kRows;
             if (r < p.rows) {
                 const float2 k2 = make_float2(ks[u], ks[u]), v2 = make_float2(vs[u], vs[u]);
                 float2 x[4];
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    eight_values<true>(kw[u][h], [&](int i) { return mul2(k2, f[4 * h + i]); }, x);
-                    store8(k_out + r * D + 8 * h, x);
-                    eight_values<false>(h ? v1 : v0, [&](int) { return v2; }, x);
-                    store8(v_out + r * D + 8 * h, x);
-                }
+                eight_values<true>(kw[u], [&](int i) { return mul2(k2, f[i]); }, x);
+                store8(k_out + (int64_t)r * D, x);
+                eight_values<false>(v, [&](int) { return v2; }, x);
+                store8(v_out + (int64_t)r * D, x);
             }
         }
     }
