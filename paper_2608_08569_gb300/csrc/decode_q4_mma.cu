@@ -130,6 +130,12 @@ __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uin
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b.x), "r"(b.y));
 }
+// Half of it: the first operands of A's rows, 8 of the 16 terms.
+__device__ __forceinline__ void mma_half(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t b) {
+    asm("mma.sync.aligned.m16n8k8.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5}, {%6}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(b));
+}
 // The same, from c: an accumulator that stays as it is.
 __device__ __forceinline__ void mma_from(float (&d)[4], const float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2,
                                          uint32_t a3, uint2 b) {
@@ -553,16 +559,26 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && kParts == 1 ? 4 : 3) deco
                             mma(o[2 * j][nt], a0, a1, a2, a3, b);
                             mma(o[2 * j + 1][nt], c0, c1, c2, c3, b);
                         }
-                    } else {  // 16 tokens' sums, least parts first, added with rounding
-                        float t0[4] = {0.f, 0.f, 0.f, 0.f}, t1[4] = {0.f, 0.f, 0.f, 0.f};
+                    } else {
+                        // The tensor cores cut off, of every term, what their sum does not hold: the lesser parts apart,
+                        // the greatest part 8 tokens at a time, and rounding between.
+                        float t[2][4], u[2][2][4];
 #pragma unroll
-                        for (int part = kWeightParts - 1; part >= 0; --part) {
+                        for (int k = 0; k < 4; ++k) t[0][k] = t[1][k] = u[0][0][k] = u[0][1][k] = u[1][0][k] = u[1][1][k] = 0.f;
+#pragma unroll
+                        for (int part = kWeightParts - 1; part > 0; --part) {
                             const uint2 b = make_uint2(b0[part], b1[part]);
-                            mma(t0, a0, a1, a2, a3, b);
-                            mma(t1, c0, c1, c2, c3, b);
+                            mma(t[0], a0, a1, a2, a3, b);
+                            mma(t[1], c0, c1, c2, c3, b);
                         }
+                        mma_half(u[0][0], a0, a1, b0[0]);
+                        mma_half(u[0][1], a2, a3, b1[0]);
+                        mma_half(u[1][0], c0, c1, b0[0]);
+                        mma_half(u[1][1], c2, c3, b1[0]);
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) o[2 * j][nt][k] += t0[k], o[2 * j + 1][nt][k] += t1[k];
+                        for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) o[2 * j + mt][nt][k] += (t[mt][k] + u[mt][0][k]) + u[mt][1][k];
                     }
                 }
             }
