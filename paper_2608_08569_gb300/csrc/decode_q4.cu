@@ -20,7 +20,10 @@ struct DecodeQ4Params {
     float gamma, scale_log2;
 };
 
-// One CTA per unit, a row per thread, two passes over K: the softmax's maximum and sum, then its weights.
+// One CTA per unit, a row per thread, two passes over K: the softmax's maximum and sum, then its weights. A form
+// without a limit on the length, in fp32 throughout; bound by its own arithmetic (some thirty times the time per
+// row of the tensor-core kernel), it serves lengths that one does not take: above about 100 000 rows with groups of up
+// to 8 heads, 48 000 with more (16 CTAs of 227 KB hold the logits of no more).
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads) decode_q4_rows_kernel(const DecodeQ4Params p) {
     constexpr int J = D / kQ4Group;

@@ -5,22 +5,29 @@
 //   out_h[d] = sum_t (p_h[t] s[t][j(d)]) c[t][d] / sum_t p_h[t]
 // The codes are small integers, so they go to the tensor cores (mma.sync m16n8k16, bf16) as they are: exact, and
 // without a multiplication by their scale. For K the scale multiplies the fp32 sum of a group (two k-steps); for V
-// it multiplies the weight before that is rounded to bf16. A nibble becomes an operand by one AND: as a bf16 bit
-// pattern, the integer v in 0..255 is v 2^-133 (a subnormal or in the first binade above, one straight line), so a
-// code in bits 0-3 is c 2^-133 and one in bits 4-7 is 16 c 2^-133; q and p carry 2^84 (q of the odd pairs 2^80), and
-// what is left, 2^-49, goes into factors that are applied anyway. The stored code is c + 8: for K the accumulators
-// start from -8 sum q (with fp32 activations 8 is subtracted from the operands, as for V); for V eight is subtracted from the operands (an output may be far smaller than its weights'
-// sum, so that a correction afterwards would cancel: with one, outputs of 1e-6 were off by as much).
-// fp32 activations are split into three bf16 parts (24 bits), of which each makes a product of its own, so that
-// only fp32 sums round.
+// it multiplies the weight before that is split. A nibble becomes an operand by one AND: as a bf16 bit pattern, the
+// integer v in 0..255 is v 2^-133 (a subnormal or in the first binade above, one straight line), so a code in bits
+// 0-3 is c 2^-133 and one in bits 4-7 is 16 c 2^-133; q and p carry 2^84 (q of the odd pairs 2^80), and what is left,
+// 2^-49, goes into factors that are applied anyway. The stored code is c + 8: for K the accumulators start from
+// -8 sum q; for V (and for K of fp32 activations) eight is subtracted from the operands, since an output may be far
+// smaller than its weights' sum, so that a correction afterwards would cancel.
+// Roundings: a bf16 weight times scale is two bf16 parts (16 bits; one part's 8 bits would double the rounding error
+// of the output, for a tenth of the time), fp32 activations and their weights three (24 bits). Sums are fp32.
 //
 // Grid: S CTAs per (layer, sequence, kv-head) unit, a thread-block cluster where S > 1; CTA r owns a run of 32-token
 // tiles, and its warp w every fourth of them. Every warp streams its own K tiles and then its V tiles through a ring
 // of its own (cp.async by all lanes: bulk copies issued by one lane, with their barriers, cost four times the
 // instructions per tile), so nothing in the streaming waits for another warp: the weights are taken relative to the
-// warp's own maximum. The logits, then the weights, stay in shared memory until
-// the unit's maximum and normaliser are known (a sum over warps, then over the cluster through distributed shared
-// memory), when each warp rewrites the scores of its own tokens.
+// warp's own maximum. The logits, then the weights, stay in shared memory until the unit's maximum and normaliser are
+// known: each CTA sends its statistics and outputs to the cluster's CTAs and meets them at one barrier, after which
+// each writes a slice of the outputs and every warp the scores of its own tokens.
+//
+// What bounds it: instructions and the chain of latencies at a CTA's start and end, not HBM. A row of 152 bytes is 6.3
+// cycles of an SM's share of HBM and 28 warp instructions (K 6, V 12, the rest start, end and tiles); of a CTA's 14 us
+// at 768 units of 2 317 rows, 6 to 7 stream. Measured, bf16, G = 8, D = 128, back to back: 768 units of 2 317 rows 80 us
+// (3.4 TB/s, 0.50 of the measured copy rate; the same rows in bf16 take 148), of 11 522 389 us (0.51); 192 units of 416
+// 8.4 us; 6 144 of 1 564 355 us (0.61). Asking the whole range into L2 at the start gained nothing, nor did starting the
+// first CTAs apart, five CTAs per SM (96 registers), or fp16 weights (whose range loses the least ones).
 #include <cooperative_groups.h>
 
 #include <type_traits>

@@ -1,12 +1,17 @@
 // Budgeted eviction from a cache held in 4 bits (format: q4.cuh): the policies of voxzip_evict_ex.
 //
-// One CTA per unit. Selection: MSB-first radix selects (four passes of 8 bits over order-preserving 32-bit keys)
-// give the N-th best history score and, where that score is tied and not all tied rows fit, the position up to
-// which its rows stay. Compaction: the kept rows that move are listed in shared memory, a segment at a time, and
-// go through registers a batch of rows at a time. A batch is loaded whole before any of it is stored: in the
-// ordered compaction a destination may be a source of the same batch, never of a later one (a row's destination
-// is its rank among the kept rows, which no source of a higher rank lies below); when holes are filled, sources
-// lie at or above the budget and destinations below it.
+// One CTA per unit. Selection: MSB-first radix selects (passes of 8 bits over order-preserving 32-bit keys, the scores,
+// and to fill holes the positions, held in shared memory) give the N-th best history score and, where that score is
+// tied and not all tied rows fit, the position up to which its rows stay. Compaction: the kept rows are listed in shared
+// memory, a segment at a time, and go through a cp.async ring in batches. A batch is stored when all of it has
+// landed: in the ordered compaction a destination may be a source of the same batch, never of a later one (a row's
+// destination is its rank among the kept rows, which no source of a higher rank lies below); when holes are filled,
+// sources lie at or above the budget and destinations below it.
+//
+// The ordered compaction moves nearly every row (the first to leave is early) and is bound by memory, as far as three
+// CTAs per SM keep it busy: 768 units of 2 333 rows down to 2 301 take 100 us (0.78 of the measured copy rate), 192 units
+// of 11 554 to 11 522 163 us (0.61: 192 CTAs on 152 SMs). Hole filling moves 32 rows of those and is bound by the
+// selection's passes: 32 and 62 us. 192 units of 189 rows to 157: 8 us.
 #include <type_traits>
 
 #include "q4.cuh"

@@ -34,7 +34,8 @@ def _np(t):
     return t.float().cpu().numpy() if t.dtype == BF16 else t.cpu().numpy()
 
 
-def make(V, *, B=1, L=1, Hq=2, H=1, D=64, C=64, dtype=BF16, lens=(0,), seed=0, outliers=True, layers=None):
+def make(V, *, B=1, L=1, Hq=2, H=1, D=64, C=64, dtype=BF16, lens=(0,), seed=0, outliers=True, layers=None,
+         v_scale=1.0):
     """A packed cache with rows of N(0, 1) (K with outlier channels), lengths per sequence, and NaN scales and random
     codes in every slot from the length on."""
     g = torch.Generator(device="cuda")
@@ -44,7 +45,7 @@ def make(V, *, B=1, L=1, Hq=2, H=1, D=64, C=64, dtype=BF16, lens=(0,), seed=0, o
     k = rnd(B, L, H, C, D)
     if outliers:
         k[..., ::29] *= 16.0
-    k, v = k.to(dtype), rnd(B, L, H, C, D).to(dtype)
+    k, v = k.to(dtype), (rnd(B, L, H, C, D) * v_scale).to(dtype)
     qc = V.allocate_q4_cache(desc)
     for name in ("k_codes", "v_codes"):
         qc[name].random_(0, 256, generator=g)
@@ -170,13 +171,13 @@ def test_unpack_windows(V, D, dtype, first, rows):
 # ----------------------------------------------------------------------------- decode
 
 def check_decode(V, *, B=1, L=1, Hq=2, H=1, D=64, C=64, dtype=BF16, lens=(0,), steps=1, gamma=0.97, max_len=0, sm_scale=0.0,
-                 layers=None, seed=0, q_scale=1.0, stream=None):
-    desc, qc, _, _, rnd = make(V, B=B, L=L, Hq=Hq, H=H, D=D, C=C, dtype=dtype, lens=lens, seed=seed)
+                 layers=None, seed=0, q_scale=1.0, v_scale=1.0, stream=None):
+    desc, qc, _, _, rnd = make(V, B=B, L=L, Hq=Hq, H=H, D=D, C=C, dtype=dtype, lens=lens, seed=seed, v_scale=v_scale)
     l0, lc = layers or (0, L)
     G, scale = Hq // H, sm_scale if sm_scale > 0 else 1 / math.sqrt(D)
     for t in range(steps):
         q = (rnd(lc, B, Hq, D) * q_scale).to(dtype)
-        kn, vn = rnd(lc, B, H, D), rnd(lc, B, H, D).to(dtype)
+        kn, vn = rnd(lc, B, H, D), (rnd(lc, B, H, D) * v_scale).to(dtype)
         kn[..., ::29] *= 16.0
         kn = kn.to(dtype)
         npos = torch.arange(B, device="cuda", dtype=torch.int32) + 10000 + t
@@ -259,6 +260,13 @@ def test_decode_layer_ranges_and_scale(V):
 def test_decode_sharp_and_flat_softmax(V, dtype):
     check_decode(V, D=128, Hq=8, lens=(333,), C=336, q_scale=12.0, dtype=dtype)
     check_decode(V, D=128, Hq=8, lens=(333,), C=336, q_scale=1e-6, dtype=dtype)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("v_scale", [1e10, 1e-12])
+def test_decode_magnitudes_of_v(V, dtype, v_scale):
+    """Within the range that the header states."""
+    check_decode(V, D=128, Hq=8, lens=(200,), C=204, v_scale=v_scale, dtype=dtype)
 
 
 def test_decode_on_another_stream(V):
