@@ -624,8 +624,8 @@ def voxzip_q4_pack(desc: CacheDesc, qc, layer_begin: int, layer_count: int, k_ca
     _need(len_, "len", torch.int32, desc._units)
     qs = _q4_struct(desc, qc)
     _check("voxzip_q4_pack", lib().voxzip_q4_pack(
-        ctypes.byref(desc._c), ctypes.byref(qs), layer_begin, layer_count, k_cache.data_ptr(), v_cache.data_ptr(),
-        len_.data_ptr(), _stream(stream)))
+        ctypes.byref(desc._c), ctypes.byref(qs), int(layer_begin), int(layer_count), k_cache.data_ptr(),
+        v_cache.data_ptr(), len_.data_ptr(), _stream(stream)))
 
 
 def voxzip_q4_unpack(desc: CacheDesc, qc, layer_begin: int, layer_count: int, k_out, v_out, *, first: int = 0,
@@ -641,7 +641,7 @@ def voxzip_q4_unpack(desc: CacheDesc, qc, layer_begin: int, layer_count: int, k_
     _need(len_, "len", torch.int32, desc._units)
     qs = _q4_struct(desc, qc)
     _check("voxzip_q4_unpack", lib().voxzip_q4_unpack(
-        ctypes.byref(desc._c), ctypes.byref(qs), layer_begin, layer_count, len_.data_ptr(), first, rows,
+        ctypes.byref(desc._c), ctypes.byref(qs), int(layer_begin), int(layer_count), len_.data_ptr(), int(first), rows,
         k_out.data_ptr(), v_out.data_ptr(), _stream(stream)))
 
 
@@ -672,9 +672,9 @@ def voxzip_decode_step_q4(desc: CacheDesc, qc, layer_begin: int, layer_count: in
         _check_dense_state(desc, score, pos, len_)
     qs = _q4_struct(desc, qc)
     _check("voxzip_decode_step_q4", lib().voxzip_decode_step_q4(
-        ctypes.byref(desc._c), ctypes.byref(qs), layer_begin, layer_count, q.data_ptr(), k_new.data_ptr(),
-        v_new.data_ptr(), new_pos.data_ptr(), score.data_ptr(), pos.data_ptr(), len_.data_ptr(), gamma, sm_scale, max_len,
-        out.data_ptr(), _stream(stream)))
+        ctypes.byref(desc._c), ctypes.byref(qs), int(layer_begin), int(layer_count), q.data_ptr(), k_new.data_ptr(),
+        v_new.data_ptr(), new_pos.data_ptr(), score.data_ptr(), pos.data_ptr(), len_.data_ptr(), float(gamma),
+        float(sm_scale), int(max_len), out.data_ptr(), _stream(stream)))
 
 
 def voxzip_evict_q4(desc: CacheDesc, qc, layer_begin: int, layer_count: int, budget, *, sink: int = 4,

@@ -408,6 +408,54 @@ def test_evict_device_errors(V):
     assert V.voxzip_get_status() == V.DEV_BAD_POSITIONS
 
 
+def test_offsets_beyond_32_bits(V):
+    """Units whose rows lie more than 2^32 bytes into the codes: packing, a decode step, reading back and an eviction of
+    the last one (and its neighbours' bytes unchanged)."""
+    L, D, C, n = 5, 128, 17_000_000, 150
+    desc = V.CacheDesc(1, L, 8, 1, D, C, BF16)
+    assert (L - 1) * C * (D // 2) > 2 ** 32
+    e = lambda *shape, dtype: torch.empty((1, L, 1) + shape, dtype=dtype, device="cuda")
+    qc = dict(k_codes=e(C, D // 2, dtype=torch.uint8), v_codes=e(C, D // 2, dtype=torch.uint8),
+              k_scale=e(C, D // 32, dtype=BF16), v_scale=e(C, D // 32, dtype=BF16), k_exp=e(D, dtype=torch.int8),
+              score=e(C, dtype=F32), pos=e(C, dtype=torch.int32), len=e(dtype=torch.int32))
+    k, v = e(C, D, dtype=BF16), e(C, D, dtype=BF16)
+    head = lambda t, m=n + 8: t[0, L - 1, 0, :m]
+    g = torch.Generator(device="cuda")
+    g.manual_seed(9)
+    for t in (k, v):
+        head(t).normal_(generator=g)
+    head(qc["score"]).uniform_(generator=g)
+    head(qc["pos"]).copy_(torch.arange(n + 8, device="cuda"))
+    qc["len"].fill_(n)
+    guard = qc["k_codes"][0, L - 2, 0, -64:].fill_(77)
+    V.voxzip_q4_pack(desc, qc, L - 1, 1, k, v)
+    q, kn, vn = (torch.randn(1, 1, x, D, generator=g, device="cuda").to(BF16) for x in (8, 1, 1))
+    out = torch.empty_like(q)
+    old = _np(head(qc["score"])).astype(np.float64)
+    V.voxzip_decode_step_q4(desc, qc, L - 1, 1, q, kn, vn, torch.tensor([n], dtype=torch.int32, device="cuda"), 0.9, out,
+                            max_len=n + 1)
+    m = n + 1
+    ko, vo = (torch.empty(1, 1, 1, m, D, dtype=BF16, device="cuda") for _ in range(2))
+    V.voxzip_q4_unpack(desc, qc, L - 1, 1, ko, vo)
+    kf = _np(head(k, n))
+    ex = R.channel_exponents(kf)
+    ks, kc = R.quantise(np.concatenate([kf, _np(kn)[0, 0]]) * np.float32(2.0) ** -ex)
+    vs, vc = R.quantise(np.concatenate([_np(head(v, n)), _np(vn)[0, 0]]))
+    K, Vv = R.values(kc, ks, ex), R.values(vc, vs)
+    assert torch.equal(ko[0, 0, 0].cpu(), torch.from_numpy(K).to(BF16)) and torch.equal(vo[0, 0, 0].cpu(), torch.from_numpy(Vv).to(BF16))
+    o, sc, pv, qk, mass = R.decode_unit(_np(q)[0, 0].astype(np.float64), K, Vv, old[:n], np.float64(np.float32(0.9)), 1 / math.sqrt(D))
+    rel = 2 * 4 * (D + 16) * 2.0 ** -24 * qk + 2.0 ** -20
+    assert (np.abs(_np(out)[0, 0] - o) <= (rel + 2.0 ** -8 * 1.01) * pv).all()
+    assert (np.abs(_np(head(qc["score"], m)) - sc) <= rel * mass + 2.0 ** -22 * sc).all()
+    before = {x: _np(head(qc[x], m)).copy() for x in ("k_codes", "v_codes", "k_scale", "v_scale", "score", "pos")}
+    V.voxzip_evict_q4(desc, qc, L - 1, 1, torch.tensor([100], dtype=torch.int32, device="cuda"))
+    _, src = R.kept_slots(before["score"], before["pos"], m, 100, 4, 0.2, True, False)
+    for x, b in before.items():
+        assert np.array_equal(b[src], _np(head(qc[x], 100))), x
+    assert qc["len"].ravel().tolist() == [n] * (L - 1) + [100]
+    assert bool((guard == 77).all()) and V.voxzip_get_status() == 0
+
+
 # ----------------------------------------------------------------------------- a request
 
 @pytest.mark.parametrize("compaction", ["ordered", "fill"])
