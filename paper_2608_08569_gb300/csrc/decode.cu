@@ -89,11 +89,11 @@ __global__ void __launch_bounds__(kThreads) decode_kernel(const DecodeParams p) 
     const UnitIdx ui = unit_of(blockIdx.y, p.B, p.L, p.Hkv, p.layer_begin);
     ptx::grid_dependency_wait();  // a programmatic dependent of the previous kernel: wait for its writes
     const int32_t n_old = p.len[ui.cache_unit];
-    const int32_t n = n_old + 1;
-    if (n_old < 0 || n > p.C) {  // same decision in every CTA of the cluster
+    if (n_old < 0 || n_old >= p.C) {  // same decision in every CTA of the cluster
         if (rank == 0 && tid == 0) raise_status(p.status, VOXZIP_DEV_CAPACITY);
         return;
     }
+    const int32_t n = n_old + 1;
     const int chunk = (n + S - 1) / S;
     if (chunk > p.chunk_cap) {
         if (rank == 0 && tid == 0) raise_status(p.status, VOXZIP_DEV_LEN_HINT);

@@ -259,11 +259,11 @@ decode_mma_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constant
         }
     }
     const int32_t n_old = p.len[ui.cache_unit];
-    const int32_t n = n_old + 1;
-    if (n_old < 0 || n > p.C) {  // the same decision in every CTA of the cluster
+    if (n_old < 0 || n_old >= p.C) {  // the same decision in every CTA of the cluster
         if (rank == 0 && tid == 0) raise_status(p.status, VOXZIP_DEV_CAPACITY);
         return;
     }
+    const int32_t n = n_old + 1;
     int32_t page_new = 0;  // paged: page of the appended row (slot n - 1)
     if constexpr (kPaged) {
         page_new = p.pv.table[ui.cache_unit * p.pv.max_pages + (n_old >> 6)];

@@ -34,11 +34,12 @@ __global__ void __launch_bounds__(kThreads) decode_q4_rows_kernel(const DecodeQ4
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const UnitIdx ui = unit_of(blockIdx.x, p.B, p.L, p.Hkv, p.layer_begin);
     ptx::grid_dependency_wait();
-    const int32_t n_old = p.len[ui.cache_unit], n = n_old + 1;
-    if (n_old < 0 || n > p.C) {
+    const int32_t n_old = p.len[ui.cache_unit];
+    if (n_old < 0 || n_old >= p.C) {
         if (tid == 0) raise_status(p.status, VOXZIP_DEV_CAPACITY);
         return;
     }
+    const int32_t n = n_old + 1;
     if (n > p.max_rows) {
         if (tid == 0) raise_status(p.status, VOXZIP_DEV_LEN_HINT);
         return;

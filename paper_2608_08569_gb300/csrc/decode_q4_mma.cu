@@ -256,7 +256,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && kParts == 1 ? 4 : 3) deco
 
     ptx::grid_dependency_wait();
     // The length first, then the warp's share of q (which does not depend on it): one memory latency for both.
-    const int32_t n_old = *static_cast<const volatile int32_t *>(p.len + ui.cache_unit), n = n_old + 1;
+    const int32_t n_old = *static_cast<const volatile int32_t *>(p.len + ui.cache_unit);
     const int8_t *ke = p.q4.k_exp + ui.cache_unit * D;
     const T *qg = static_cast<const T *>(p.q) + (act * p.Hq + (int64_t)ui.h * p.G) * D;
     constexpr int kShare = (NT * J + kWarps - 1) / kWarps;
@@ -267,11 +267,12 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && kParts == 1 ? 4 : 3) deco
         q_raw[it] = RawQ<T>{};
         if (nj < NT * J && head < p.G) q_raw[it].load(qg + head * D + d, ke + d);
     }
-    if (n_old < 0 || n > p.C || n > p.max_rows) {  // the same decision in every CTA of the cluster
+    if (n_old < 0 || n_old >= min(p.C, p.max_rows)) {  // the same decision in every CTA of the cluster
         if (rank == 0 && tid == 0)
-            raise_status(p.status, n_old < 0 || n > p.C ? VOXZIP_DEV_CAPACITY : VOXZIP_DEV_LEN_HINT);
+            raise_status(p.status, n_old < 0 || n_old >= p.C ? VOXZIP_DEV_CAPACITY : VOXZIP_DEV_LEN_HINT);
         return;
     }
+    const int32_t n = n_old + 1;
     const int tiles = (n + kTile - 1) / kTile, share = kCluster ? (int)__umulhi(tiles + S - 1, p.inv_s) : tiles;
     const int tile0 = min(tiles, rank * share), mine = min(tiles, tile0 + share) - tile0;  // this CTA's tiles
     const int j0 = tile0 * kTile, cnt = min(n, j0 + mine * kTile) - j0;                    // and tokens
@@ -599,7 +600,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && kParts == 1 ? 4 : 3) deco
         if (b2 >= p.B) b2 -= p.B, ++l2;
         if (l2 < (int)gridDim.z) {
             const int64_t unit2 = ((int64_t)b2 * p.L + p.layer_begin + l2) * p.Hkv + h2;
-            const int n2 = min(max(ptx::load_relaxed(p.len + unit2), 0) + 1, p.C);  // only aims: it may be about to change
+            const int n2 = min(max(ptx::load_relaxed(p.len + unit2), 0), p.C - 1) + 1;  // only aims: it may be about to change
             const int tiles2 = (n2 + kTile - 1) / kTile, share2 = kCluster ? (int)__umulhi(tiles2 + S - 1, p.inv_s) : tiles2;
             const int first2 = min(tiles2, rank * share2) * kTile;
             const int rows2 = (min(n2, first2 + share2 * kTile) - first2 + 3) & ~3;
