@@ -185,7 +185,7 @@ __global__ void __launch_bounds__(kThreads, 4) q4_pack_kernel(const PackParams p
             for (int q = 0; q < S; ++q) t = max(t, *cluster.map_shared_rank(&amax[d], q));
             amax_unit[d] = t;
         }
-        ptx::cluster_arrive_relaxed();  // done reading the others
+        ptx::cluster_arrive();  // done reading the others: they may leave
     } else {
         __syncthreads();
         for (int d = tid; d < D; d += kThreads) amax_unit[d] = amax[d];
