@@ -9,19 +9,32 @@ in a CUDA graph and replayed (``capture_loop``).
 
 With ``kv_bits=4`` the session's cache holds its rows in 4 bits per channel: stage 1 runs into a staging cache of
 plain rows, which is packed right after it, and decode steps and evictions work on the packed rows. The staging
-rows are needed during ``prefill`` alone, so sessions may share them (``staging``).
+rows are needed during ``prefill`` alone: it makes them and gives them back to torch's allocator. Rows that the caller
+keeps (``staging``) may serve several sessions: each prefill on them waits for the one before, on whatever stream.
 """
 from __future__ import annotations
+
+import threading
 
 import torch
 
 from . import _native as N
 
 
+class _Turn:
+    """Whose prefill has a staging cache that sessions share: one at a time. `done` is recorded behind the last one's
+    packing."""
+
+    def __init__(self):
+        self.lock = threading.Lock()
+        self.done = None
+
+
 class Session:
     """`budget` holds one budget per sequence, or per sequence and layer ([B][L]); `history` and
     `compaction` select the eviction policy (see voxzip_evict_ex). `kv_bits` is 16 (rows in the descriptor's
-    dtype) or 4; `staging`, with 4, a dict of k and v [B][L][Hkv][C][D] that stage 1 may overwrite."""
+    dtype) or 4; `staging`, with 4, a dict of k and v [B][L][Hkv][C][D] that stage 1 may overwrite (the same dict for
+    every session that shares them: it holds their order too, under "turn")."""
 
     def __init__(self, desc: N.CacheDesc, budget, gamma: float, *, sink: int = 4, recent_frac: float = 0.2,
                  history: bool = True, compaction: str = "ordered", device="cuda", cache=None,
@@ -66,22 +79,45 @@ class Session:
                                        span_start, span_end, span_groups, slot_map=slot_map, anchor_k=anchor_k,
                                        anchor_v=anchor_v, workspace=self.workspace, stream=stream)
         else:
-            rows = c
+            def launch(rows):
+                N.voxzip_anchor_fuse(self.desc, k_prefill, v_prefill, in_len, audio_begin, audio_len, span_off,
+                                     span_start, span_end, span_groups, rows["k"], rows["v"], c["score"], c["pos"],
+                                     c["len"], slot_map=slot_map, anchor_k=anchor_k, anchor_v=anchor_v,
+                                     workspace=self.workspace, stream=stream)
+                if self.kv_bits == 4:
+                    N.voxzip_q4_pack(self.desc, c, 0, self.desc.layers, rows["k"], rows["v"], stream=stream)
+
             if self.kv_bits == 4:
-                if self.staging is None:
-                    new = lambda: torch.empty(self.desc._rows, dtype=self.desc.dtype, device=self.device)  # noqa: E731
-                    self.staging = dict(k=new(), v=new())
-                rows = self.staging
-            N.voxzip_anchor_fuse(self.desc, k_prefill, v_prefill, in_len, audio_begin, audio_len, span_off,
-                                 span_start, span_end, span_groups, rows["k"], rows["v"], c["score"], c["pos"],
-                                 c["len"], slot_map=slot_map, anchor_k=anchor_k, anchor_v=anchor_v,
-                                 workspace=self.workspace, stream=stream)
-            if self.kv_bits == 4:
-                N.voxzip_q4_pack(self.desc, c, 0, self.desc.layers, rows["k"], rows["v"], stream=stream)
+                self._staged(launch, stream)
+            else:
+                launch(c)
         if read_back:
             self.n_max = int(c["len"].max().item())
         else:
             self.n_max = int(k_prefill.shape[3])  # stage 1 never lengthens a prompt
+
+    def _staged(self, launch, stream):
+        """Runs launch(rows) with rows for stage 1 that nothing else uses until it is done on the GPU."""
+        if stream is not None and not hasattr(stream, "wait_event"):
+            stream = torch.cuda.ExternalStream(stream.cuda_stream)
+        with torch.cuda.stream(stream):  # memory made here is the launches' own: who gets it next is ordered behind them
+            rows = self.staging
+            if rows is None:
+                new = lambda: torch.empty(self.desc._rows, dtype=self.desc.dtype, device=self.device)  # noqa: E731
+                rows = dict(k=new(), v=new())
+            alone = self.staging is None or torch.cuda.is_current_stream_capturing()
+        if alone:  # (a graph's replays are ordered by who replays them)
+            launch(rows)
+        else:
+            turn = self.staging.setdefault("turn", _Turn())
+            with turn.lock:
+                at = stream if stream is not None else torch.cuda.current_stream()
+                if turn.done is not None:
+                    at.wait_event(turn.done)
+                try:
+                    launch(self.staging)
+                finally:
+                    turn.done = at.record_event()
 
     # stage 2 -------------------------------------------------------------------------------------
     def decode(self, q, k_new, v_new, new_pos, out, *, layer_begin=0, layer_count=None, stream=None):
