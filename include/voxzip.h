@@ -435,6 +435,14 @@ voxzip_status voxzip_q4_unpack(const voxzip_cache_desc *desc, const voxzip_q4_ca
  * n and takes part in the attention as packed. Attention, scores and errors are those of voxzip_decode_step, on the
  * values the rows stand for, at any length up to the capacity. score is 16-byte aligned.
  *
+ * max_len also selects the kernel: the tensor-core kernel keeps the logits of max_len rows (of the capacity, where
+ * max_len is 0) in the shared memory of a cluster, which holds, by head dimension and dtype,
+ *   groups of up to 8 heads   D = 128: 102912 rows bf16,  99840 fp32;  D = 64: 109056 bf16, 107520 fp32
+ *   groups of 9 to 16         D = 128:  46080 rows bf16,  43008 fp32;  D = 64:  51200 bf16,  49664 fp32
+ * Above that, and above 65535 sequences or layers of a call, a kernel without the tensor cores runs, with one CTA per
+ * unit: about 0.4 us per row of the longest unit, twenty times as long for 192 units and a hundred for 8. A short
+ * cache of a large capacity wants its max_len.
+ *
  * Range: the tensor-core products carry powers of two that keep every code exact; |q 2^e| and the scales of V must
  * lie below 2^40, and magnitudes below 2^-60 count as zero there.
  */

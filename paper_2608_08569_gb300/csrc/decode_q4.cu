@@ -21,13 +21,14 @@ struct DecodeQ4Params {
 };
 
 // One CTA per unit, a row per thread, two passes over K: the softmax's maximum and sum, then its weights. A form
-// without a limit on the length, in fp32 throughout; bound by its own arithmetic (some thirty times the time per
-// row of the tensor-core kernel), it serves lengths that one does not take: above about 100 000 rows with groups of up
-// to 8 heads, 48 000 with more (16 CTAs of 227 KB hold the logits of no more).
+// without a limit on the length, in fp32 throughout, for lengths that the tensor-core kernel does not take: those whose
+// logits 16 CTAs of 227 KB do not hold (decode_q4_plan.cuh; voxzip.h lists them). Bound by its own arithmetic: 192
+// units of 120 000 rows, G = 8, D = 128 take 48.6 ms in bf16 or fp32 (by bytes 0.5; the tensor-core kernel needs 1.9
+// for 100 000), 8 units with G = 16 40.9 ms.
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads) decode_q4_rows_kernel(const DecodeQ4Params p) {
     constexpr int J = D / kQ4Group;
-    __shared__ float qs[kMaxGroup][D];  // times 2^e, in the words' order of channels
+    __shared__ float qs[kMaxGroup][D];  // times 2^e
     __shared__ float pt[kThreads][kMaxGroup + 1];
     __shared__ float red[kThreads / 32][kMaxGroup][2];
     __shared__ float mz[kMaxGroup][2];

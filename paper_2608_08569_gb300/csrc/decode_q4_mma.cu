@@ -32,6 +32,7 @@
 
 #include <type_traits>
 
+#include "decode_q4_plan.cuh"
 #include "q4.cuh"
 
 namespace cg = cooperative_groups;
@@ -39,12 +40,9 @@ namespace cg = cooperative_groups;
 namespace voxzip {
 namespace {
 
-constexpr int kWarps = 4;
-constexpr int kThreads = kWarps * 32;
-constexpr int kTile = 32;   // tokens per stage
-constexpr int kMaxStages = 3;  // of a warp's ring: two, or three where they do not cost the SM a CTA
-constexpr int kMaxCluster = 16;
-constexpr size_t kMaxSmem = 227 * 1024;
+using namespace q4;
+static_assert(kGroup == kQ4Group, "the plan counts the format's groups");
+
 constexpr float kCarry = 0x1p84f, kUncarry = 0x1p49f;
 constexpr float kLeast = -3.402823466e38f;
 
@@ -61,34 +59,6 @@ struct MmaQ4Params {
     int32_t next_h, next_b, next_l; // how far the unit lies whose CTAs take these ones' place (next_l < 0: none)
     uint32_t inv_s, inv_slice;      // ceil(2^32 / S), ceil(2^32 / slice): quotients by __umulhi
     float gamma, scale_log2;  // scale_log2: logits in units of log 2, times kUncarry
-};
-
-template <int D, int NT, int kParts>
-struct Layout {
-    static constexpr int J = D / kQ4Group;
-    static constexpr int kGP = 8 * NT;
-    static constexpr int kCodeBytes = kTile * D / 2;
-    static constexpr int kStageBytes = kCodeBytes + kTile * J * 2;
-    static constexpr int kOStride = D + 4;  // a warp's outputs take its drained ring: [kGP][kOStride] fp32
-    static constexpr int warp_ring(int stages) { return max(stages * kStageBytes, kGP * kOStride * 4); }
-    // Offsets from the rings' end.
-    static constexpr int kStatOff = 0;
-    static constexpr int kStatFloats = 3 * kWarps * kGP;                 // m_w, z_w, f_w [kWarps][kGP]
-    static constexpr int kScOff = kStatOff + kStatFloats * 4;  // [kWarps][J][kTile] the scales of a V tile
-    static constexpr int kCOff = kScOff + kWarps * J * kTile * 4;  // [NT][J][8] what the accumulators start from
-    // q's operands [parts][NT][2 J][32] pairs, and in their place, once every CTA of the cluster has them in
-    // registers (fp32: beside them), what the cluster's CTAs send: [S][kGP] maxima and sums, [S][slice] float4 of
-    // outputs (S slices cover kGP D).
-    static constexpr int kQOff = kCOff + NT * J * 8 * 4;
-    static constexpr int kQBytes = kParts * NT * 2 * J * 32 * 8;
-    static constexpr int kMzOff = kParts == 1 ? kQOff : kQOff + kQBytes;
-    static constexpr int rx_bytes(int S) { return S * (kGP * 8 + 16) + kGP * D * 4; }
-    static_assert(kParts > 1 || rx_bytes(2) >= kQBytes, "q's operands fit");
-    // [NT][chunk_cap][8] logits, then weights
-    static constexpr int lg_off(int S) { return S > 1 ? kMzOff + rx_bytes(S) : kQOff + kQBytes; }
-    static size_t bytes(int chunk_cap, int S, int stages) {
-        return (size_t)kWarps * warp_ring(stages) + lg_off(S) + (size_t)chunk_cap * kGP * 4;
-    }
 };
 
 __device__ __forceinline__ float fast_exp2(float x) {
@@ -795,8 +765,10 @@ auto by_shape(const voxzip_cache_desc &d, F &&f) {
 
 // How many clusters of S CTAs with `smem` bytes each fit the GPU at once.
 template <typename K>
-int resident_clusters(int S, size_t smem) {
-    if (configure<K>() != cudaSuccess) return 0;
+cudaError_t resident_clusters(int S, size_t smem, int *n) {
+    *n = 0;
+    const cudaError_t set = configure<K>();
+    if (set != cudaSuccess) return set;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)S, 1024, 1);
     cfg.blockDim = dim3(kThreads, 1, 1);
@@ -808,55 +780,24 @@ int resident_clusters(int S, size_t smem) {
     attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, K::of(S), &cfg) != cudaSuccess) {
-        cudaGetLastError();
-        return 0;
-    }
-    return n;
+    const cudaError_t err = cudaOccupancyMaxActiveClusters(n, K::of(S), &cfg);
+    if (err == cudaSuccess) return err;
+    cudaGetLastError();
+    *n = 0;
+    return err == cudaErrorInvalidClusterSize ? cudaSuccess : err;  // such clusters do not fit
 }
 
-struct Plan {
-    int S, stages, chunk_cap;
-    int resident;  // clusters at once
-};
-
-// A time model of a launch, in us, fitted to back-to-back launches of forced plans (4 to 6 144 units of 100 to
-// 40 000 rows, groups of 1 to 16 heads, both head dims and types: 22 shapes, S up to 16, two to four stages). The
-// plans it picks are 0.6% slower than the best of each shape on average, 4% at worst.
-constexpr double kFixed = 3.46, kFixedNeighbour = 0.2;  // a CTA's start and end, more with each CTA on its SM
-constexpr double kExchange = 2.51;                      // the cluster's
-constexpr double kTileAlone = 1.33, kTileShared = 0.41; // a warp's tile of K and V: by latency, or by CTAs on its SM
-constexpr double kTwoStages = 0.18;                     // more per tile with a ring of two, shared by the SM's CTAs
-constexpr double kLastRound = 0.75;                     // how far a part-filled last round costs a whole one
-
-Plan plan(const voxzip_cache_desc &d, int units, int nmax) {
-    const int tiles = (nmax + kTile - 1) / kTile, sms = sm_count();
-    const double weight = (d.head_dim == 64 ? 0.70 : 1.0) * (d.dtype == VOXZIP_F32 ? 1.24 : 1.0) *
-                          (d.q_heads / d.kv_heads > 8 ? 1.55 : 1.0);
-    Plan best{0, 0, 0, 0};
-    double best_cost = 0.0;
-    for (int S : {1, 2, 3, 4, 5, 6, 8, 12, 16}) {
-        if (S > tiles) break;
-        const int cap = (tiles + S - 1) / S * kTile;
-        for (int stages = kMaxStages; stages >= 2; --stages) {
-            const size_t smem = by_shape(d, [&](auto k) { return decltype(k)::Lay::bytes(cap, S, stages); });
-            if (smem > kMaxSmem) continue;
-            const int resident = by_shape(d, [&](auto k) { return resident_clusters<decltype(k)>(S, smem); });
-            if (resident <= 0) continue;
-            const double per_sm = fmin((double)resident, (double)units) * S / sms, neighbours = fmax(1.0, per_sm);
-            const double tile = fmax(kTileAlone, kTileShared * neighbours) * weight + (stages == 2 ? kTwoStages / neighbours : 0.0);
-            const double cta = kFixed + kFixedNeighbour * neighbours + (S > 1 ? kExchange : 0.0) +
-                               tile * ((tiles + kWarps * S - 1) / (kWarps * S));
-            const double share = (double)units / resident;
-            const double cost = cta * (share <= 1.0 ? 1.0 : kLastRound * ceil(share) + (1.0 - kLastRound) * share);
-            if (best.S == 0 || cost < best_cost) {
-                best = Plan{S, stages, cap, resident};
-                best_cost = cost;
-            }
-        }
-    }
-    return best;
+cudaError_t plan(const voxzip_cache_desc &d, int units, int nmax, Plan *best) {
+    const q4::Shape shape{d.head_dim, d.dtype == VOXZIP_F32, d.q_heads / d.kv_heads > 8};
+    return q4::choose_plan(
+        shape, sm_count(), units, nmax,
+        [&](int cap, int S, int stages) {
+            return by_shape(d, [&](auto k) { return decltype(k)::Lay::bytes(cap, S, stages); });
+        },
+        [&](int S, size_t smem, int *n) {
+            return by_shape(d, [&](auto k) { return resident_clusters<decltype(k)>(S, smem, n); });
+        },
+        best);
 }
 
 }  // namespace
@@ -874,7 +815,7 @@ cudaError_t launch_decode_q4(const voxzip_cache_desc &d, const Q4View &q4, int32
     };
     thread_local Entry cache[16];
     thread_local int cache_next = 0;
-    const int G = d.q_heads / d.kv_heads, tiles = (nmax + kTile - 1) / kTile;
+    const int G = d.q_heads / d.kv_heads, tiles = (nmax - 1) / kTile + 1;
     int device = 0;
     const cudaError_t got = cudaGetDevice(&device);
     if (got != cudaSuccess) return got;
@@ -886,7 +827,8 @@ cudaError_t launch_decode_q4(const voxzip_cache_desc &d, const Q4View &q4, int32
             found = true;
         }
     if (!found) {
-        pl = plan(d, units, nmax);
+        const cudaError_t err = plan(d, units, nmax, &pl);
+        if (err != cudaSuccess) return err;  // (no plan is kept)
         cache[cache_next] = Entry{device, d.head_dim, d.dtype, G > 8, units, tiles, pl};
         cache_next = (cache_next + 1) % 16;
     }
