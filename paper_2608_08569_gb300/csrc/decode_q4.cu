@@ -49,7 +49,8 @@ __global__ void __launch_bounds__(kThreads) decode_q4_rows_kernel(const DecodeQ4
     const T *qg = static_cast<const T *>(p.q) + (act * p.Hq + (int64_t)ui.h * p.G) * D;
     const int8_t *ke = p.q4.k_exp + ui.cache_unit * D;
     for (int i = tid; i < p.G * D; i += kThreads) qs[i / D][i % D] = Elem<T>::to_f(qg[i]) * exp2_int(ke[i % D]);
-    if (warp < 2) {  // the appended row
+    auto in_cache = [&](int r) { return VOXZIP_IN_RANGE(p.status, r >= 0 && r < p.C); };  // of a row of the unit
+    if (warp < 2 && in_cache(n_old)) {  // the appended row
         const T *src = static_cast<const T *>(warp == 0 ? p.k_new : p.v_new) + (act * p.Hkv + ui.h) * D;
         float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
         if (lane < D / 4) {
@@ -64,7 +65,7 @@ __global__ void __launch_bounds__(kThreads) decode_q4_rows_kernel(const DecodeQ4
         else
             Q4Row<D, false>(x).store(p.q4.v_codes + (row_base + n_old) * (D / 2), p.q4.v_scale + (row_base + n_old) * J);
     }
-    if (tid == 0) p.pos[row_base + n_old] = p.new_pos[ui.b];
+    if (tid == 0 && in_cache(n_old)) p.pos[row_base + n_old] = p.new_pos[ui.b];
     __syncthreads();
 
     auto logits = [&](int r, float (&l)[kMaxGroup]) {
@@ -95,7 +96,7 @@ __global__ void __launch_bounds__(kThreads) decode_q4_rows_kernel(const DecodeQ4
     float m[kMaxGroup], z[kMaxGroup];
 #pragma unroll
     for (int h = 0; h < kMaxGroup; ++h) m[h] = -INFINITY, z[h] = 0.f;
-    for (int r = tid; r < n; r += kThreads) {
+    for (int r = tid; r < n && in_cache(r); r += kThreads) {
         float l[kMaxGroup];
         logits(r, l);
 #pragma unroll
@@ -134,7 +135,7 @@ __global__ void __launch_bounds__(kThreads) decode_q4_rows_kernel(const DecodeQ4
     for (int h = 0; h < kMaxGroup; ++h) o[h] = 0.f;
     for (int r0 = 0; r0 < n; r0 += kThreads) {
         const int r = r0 + tid;
-        if (r < n) {
+        if (r < n && in_cache(r)) {
             float l[kMaxGroup], add = 0.f;
             logits(r, l);
 #pragma unroll
@@ -147,7 +148,7 @@ __global__ void __launch_bounds__(kThreads) decode_q4_rows_kernel(const DecodeQ4
             *sc = r == n_old ? add : p.gamma * *sc + add;
         }
         __syncthreads();
-        for (int i = part; i < min(kThreads, n - r0); i += kParts) {
+        for (int i = part; i < min(kThreads, n - r0) && in_cache(r0 + i); i += kParts) {
             const int64_t row = row_base + r0 + i;
             const uint32_t w = reinterpret_cast<const uint16_t *>(p.q4.v_codes + row * (D / 2))[(at >> 2) * J + j];
             const float v = (float)((int)(w >> (4 * (at & 3)) & 15u) - 8) * __bfloat162float(p.q4.v_scale[row * J + j]);

@@ -151,6 +151,7 @@ __global__ void __launch_bounds__(kThreads, 4) q4_pack_kernel(const PackParams p
     const int j = tid % kLanes >> 1, half = tid & 1, r0 = first + tid / kLanes;
     const T *k = static_cast<const T *>(p.k_cache) + ui.cache_unit * p.C * D + 32 * j + 8 * half;
     const T *v = static_cast<const T *>(p.v_cache) + ui.cache_unit * p.C * D + 32 * j + 8 * half;
+    auto in_cache = [&](int r) { return VOXZIP_IN_RANGE(p.status, r >= 0 && r < p.C); };  // of a row of the unit
     auto channel = [&](int i) { return 32 * j + 8 * half + i + (i & 8); };  // of the lane's i-th value
     // Largest magnitudes: of bf16 as pairs of 16-bit integers (the order of magnitudes is that of their bits).
     constexpr int kTop = 4 * Half<T>::kVecs;
@@ -162,7 +163,7 @@ __global__ void __launch_bounds__(kThreads, 4) q4_pack_kernel(const PackParams p
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             x[u] = Half<T>{};
-            if (r + u * kRows < last) x[u].load(k + (int64_t)(r + u * kRows) * D);
+            if (r + u * kRows < last && in_cache(r + u * kRows)) x[u].load(k + (int64_t)(r + u * kRows) * D);
         }
 #pragma unroll
         for (int u = 0; u < kAhead; ++u)
@@ -222,7 +223,7 @@ __global__ void __launch_bounds__(kThreads, 4) q4_pack_kernel(const PackParams p
         for (int u = 0; u < kBoth; ++u) {
             const int r = r0 + (i0 + u) * kRows;
             a[u] = b[u] = Half<T>{};
-            if (r < last) {
+            if (r < last && in_cache(r)) {
                 a[u].load(k + (int64_t)r * D);
                 b[u].load(v + (int64_t)r * D);
             }
@@ -260,7 +261,7 @@ __global__ void __launch_bounds__(kThreads, 4) q4_pack_kernel(const PackParams p
             // Words of V pair the groups 2 i and 2 i + 1: the even one's lane takes the first two g, the odd one's the others.
             const uint32_t other = __shfl_xor_sync(0xffffffffu, j & 1 ? vw[0] : vw[1], 2);
             const uint32_t even = j & 1 ? other : vw[0], odd = j & 1 ? vw[1] : other;
-            if (r < last) {
+            if (r < last && in_cache(r)) {
                 uint32_t *kc = reinterpret_cast<uint32_t *>(p.q4.k_codes + row * (D / 2)) + half * J + j;
                 uint32_t *vc = reinterpret_cast<uint32_t *>(p.q4.v_codes + row * (D / 2)) + (2 * half + 4 * (j & 1)) * (J / 2) + (j >> 1);
                 kc[0] = kw[0];
@@ -355,7 +356,7 @@ __global__ void __launch_bounds__(kThreads, 6) q4_unpack_kernel(const UnpackPara
             const int64_t slot = r0 + u * kRows + shift;
             kw[u] = vw[u] = 0u;
             ks[u] = vs[u] = 0.f;
-            if (r0 + u * kRows < p.rows && slot >= 0 && slot < n) {
+            if (r0 + u * kRows < p.rows && slot >= 0 && slot < n && VOXZIP_IN_RANGE(p.status, slot < p.C)) {
                 kw[u] = kc[slot * (D / 8)];
                 vw[u] = vc[slot * (D / 8)];
                 ks[u] = __bfloat162float(ks0[slot * J]);
@@ -368,7 +369,7 @@ __global__ void __launch_bounds__(kThreads, 6) q4_unpack_kernel(const UnpackPara
             const uint32_t other = __shfl_xor_sync(0xffffffffu, vw[u], 4);
             const uint32_t v = j & 1 ? __byte_perm(other, vw[u], 0x7632) : __byte_perm(vw[u], other, 0x5410);
             const int r = r0 + u * kRows;
-            if (r < p.rows) {
+            if (r < p.rows && VOXZIP_IN_RANGE(p.status, r >= 0)) {
                 const float2 k2 = make_float2(ks[u], ks[u]), v2 = make_float2(vs[u], vs[u]);
                 float2 x[4];
                 eight_values<true>(kw[u], [&](int i) { return mul2(k2, f[i]); }, x);

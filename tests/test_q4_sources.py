@@ -18,3 +18,14 @@ def test_a_cluster_is_left_by_a_release():
     assert arrives == 3  # pack: one; decode: its start, and what it sends
     ptx = open(os.path.join(ROOT, "paper_2608_08569_gb300", "csrc", "ptx.cuh")).read()
     assert "barrier.cluster.arrive.release.aligned" in ptx
+
+
+def test_every_kernel_checks_its_rows_in_the_checked_build():
+    """VOXZIP_IN_RANGE stands in each kernel of the 4-bit cache, so that the checked build's runs show what they touch."""
+    kernels = [(f, m.group(1), m.start()) for f, s in SOURCES.items() for m in re.finditer(r"__global__[^;{]*?(\w+)\(const \w+ p\)", s)]
+    assert sorted(k for _, k, _ in kernels) == ["decode_q4_mma_kernel", "decode_q4_rows_kernel", "evict_q4_kernel", "q4_pack_kernel",
+                                                "q4_unpack_kernel"]
+    for f, k, at in kernels:
+        s = SOURCES[f]
+        end = min([a for g, _, a in kernels if g == f and a > at] + [s.find("cudaError_t", at)])
+        assert s.count("VOXZIP_IN_RANGE", at, end) >= 1, k
