@@ -297,9 +297,11 @@ __device__ __forceinline__ void store8(T *p, const float2 (&x)[4]) {
     }
 }
 
-// The eight channels of a word, times scale(i): a code's byte becomes 2^23 + c + 8 by one byte permutation.
-template <bool kIsK, typename S>
-__device__ __forceinline__ void eight_values(uint32_t w, S &&scale, float2 (&x)[4]) {
+// The eight channels of a word: code times scale, for K (an eighth of) it and then 2^(e + 3): neither factor nor the
+// product between is infinite or inexact, whatever the scale (one times 2^e may be, where the code is 0). A code's byte
+// becomes 2^23 + c + 8 by one byte permutation.
+template <bool kIsK>
+__device__ __forceinline__ void eight_values(uint32_t w, float2 scale, const float2 (&pow)[4], float2 (&x)[4]) {
     using O = WordOrder<kIsK>;
     const uint32_t lo = w & 0x0f0f0f0fu, hi = w >> 4 & 0x0f0f0f0fu;
     float y[8];
@@ -309,8 +311,10 @@ __device__ __forceinline__ void eight_values(uint32_t w, S &&scale, float2 (&x)[
         y[O::high(k)] = __uint_as_float(__byte_perm(hi, 0x4b000000u, 0x7540 | k));
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        x[i] = mul2(add2(make_float2(y[2 * i], y[2 * i + 1]), make_float2(-8388616.f, -8388616.f)), scale(i));
+    for (int i = 0; i < 4; ++i) {
+        x[i] = mul2(add2(make_float2(y[2 * i], y[2 * i + 1]), make_float2(-8388616.f, -8388616.f)), scale);
+        if constexpr (kIsK) x[i] = mul2(x[i], pow[i]);
+    }
 }
 
 // Row r of the output is slot first + r (from the unit's end if first < 0); zeros where there is none. A lane takes 8
@@ -337,7 +341,7 @@ __global__ void __launch_bounds__(kThreads, 6) q4_unpack_kernel(const UnpackPara
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int e = (i < 2 ? exps.x : exps.y) >> (16 * (i & 1));
-        f[i] = make_float2(exp2_int((int)(int8_t)e), exp2_int((int)(int8_t)(e >> 8)));
+        f[i] = make_float2(exp2_int((int)(int8_t)e + 3), exp2_int((int)(int8_t)(e >> 8) + 3));
     }
     const int64_t out_unit = ((int64_t)ui.b * p.layer_count + ui.l_local) * p.Hkv + ui.h;
     const int64_t shift = (int64_t)p.first + (p.first < 0 ? n : 0);
@@ -370,11 +374,10 @@ __global__ void __launch_bounds__(kThreads, 6) q4_unpack_kernel(const UnpackPara
             const uint32_t v = j & 1 ? __byte_perm(other, vw[u], 0x7632) : __byte_perm(vw[u], other, 0x5410);
             const int r = r0 + u * kRows;
             if (r < p.rows && VOXZIP_IN_RANGE(p.status, r >= 0)) {
-                const float2 k2 = make_float2(ks[u], ks[u]), v2 = make_float2(vs[u], vs[u]);
                 float2 x[4];
-                eight_values<true>(kw[u], [&](int i) { return mul2(k2, f[i]); }, x);
+                eight_values<true>(kw[u], make_float2(ks[u] * 0.125f, ks[u] * 0.125f), f, x);
                 store8(k_out + (int64_t)r * D, x);
-                eight_values<false>(v, [&](int) { return v2; }, x);
+                eight_values<false>(v, make_float2(vs[u], vs[u]), f, x);
                 store8(v_out + (int64_t)r * D, x);
             }
         }
