@@ -443,8 +443,14 @@ voxzip_status voxzip_q4_unpack(const voxzip_cache_desc *desc, const voxzip_q4_ca
  * unit: about 0.4 us per row of the longest unit, twenty times as long for 192 units and a hundred for 8. A short
  * cache of a large capacity wants its max_len.
  *
- * Range: the tensor-core products carry powers of two that keep every code exact; |q 2^e| and the scales of V must
- * lie below 2^40, and magnitudes below 2^-60 count as zero there.
+ * Range of the tensor-core kernel, whose operands carry powers of two that keep every code exact: |q 2^e| and the
+ * scales of V must lie below 2^44 (at or above it, outputs are not finite), and what |q 2^e| or a term p s of an output
+ * (p the softmax weight) has below 2^-77 may count as zero. The other kernel has the range of fp32.
+ *
+ * Channel exponents stay as voxzip_q4_pack last set them (evictions and decode steps leave them alone). A channel of
+ * K whose appended values are much larger, against the other channels, than its packed ones takes the scales of its
+ * group: after a prompt in which it lay 2^-16 below the median channel or lower, e = -16 and an ordinary value leaves
+ * the group's other channels code 0 in that row. k 2^-e above the range of fp32 is not finite: the group reads as NaN.
  */
 voxzip_status voxzip_decode_step_q4(const voxzip_cache_desc *desc, const voxzip_q4_cache *q4, int32_t layer_begin,
                                     int32_t layer_count, const void *q, const void *k_new, const void *v_new,
