@@ -30,6 +30,13 @@ class _Turn:
         self.done = None
 
 
+def _torch_stream(stream):
+    """A call's `stream` (None, or anything with a cuda_stream) for torch's own work."""
+    if stream is None or hasattr(stream, "wait_event"):
+        return stream
+    return torch.cuda.ExternalStream(stream.cuda_stream)
+
+
 class Session:
     """`budget` holds one budget per sequence, or per sequence and layer ([B][L]); `history` and
     `compaction` select the eviction policy (see voxzip_evict_ex). `kv_bits` is 16 (rows in the descriptor's
@@ -92,14 +99,14 @@ class Session:
             else:
                 launch(c)
         if read_back:
-            self.n_max = int(c["len"].max().item())
+            with torch.cuda.stream(_torch_stream(stream)):
+                self.n_max = int(c["len"].max().item())
         else:
             self.n_max = int(k_prefill.shape[3])  # stage 1 never lengthens a prompt
 
     def _staged(self, launch, stream):
         """Runs launch(rows) with rows for stage 1 that nothing else uses until it is done on the GPU."""
-        if stream is not None and not hasattr(stream, "wait_event"):
-            stream = torch.cuda.ExternalStream(stream.cuda_stream)
+        stream = _torch_stream(stream)
         with torch.cuda.stream(stream):  # memory made here is the launches' own: who gets it next is ordered behind them
             rows = self.staging
             if rows is None:

@@ -149,3 +149,18 @@ def test_sessions_on_two_streams_share_staging_rows(monkeypatch):
     for s, c in zip(got, want):
         for name, t in c.items():
             assert torch.equal(t, s.cache[name]), name
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [4, 16])
+def test_the_length_is_read_back_on_the_prefills_stream(bits):
+    """On a stream that is still busy, a read on another one would see the cache before stage 1."""
+    w, desc, prompt = _request(3)
+    want = Session(desc, w.budget, w.gamma, kv_bits=bits)
+    want.prefill(*prompt)
+    s, stream = Session(desc, w.budget, w.gamma, kv_bits=bits), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        torch.cuda._sleep(20_000_000)  # about 10 ms
+    s.prefill(*prompt, stream=stream)
+    assert s.n_max == want.n_max > 0
