@@ -80,7 +80,8 @@ class Session:
         c = self.cache
         need = N.voxzip_anchor_fuse_workspace_size(self.desc, k_prefill.shape[3], span_start.numel())
         if self.workspace is None or self.workspace.numel() < need:
-            self.workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
+            with torch.cuda.stream(_torch_stream(stream)):  # the launches' own, as it is what they use it on
+                self.workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
         if self.paged:
             N.voxzip_anchor_fuse_paged(self.desc, c, k_prefill, v_prefill, in_len, audio_begin, audio_len, span_off,
                                        span_start, span_end, span_groups, slot_map=slot_map, anchor_k=anchor_k,

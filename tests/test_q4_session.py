@@ -84,6 +84,24 @@ def test_a_plain_session_stages_nothing(log):
     assert [x[1] for x in log] == ["fuse"] and log[0][2] is s.cache["k"]
 
 
+@pytest.mark.parametrize("bits", [4, 16])
+def test_what_a_prefill_allocates_belongs_to_its_stream(log, monkeypatch, bits):
+    """torch hands a freed block to the next user of the stream that it was made on: memory of another stream may still
+    be in use there, or go to its next user while the launches run."""
+    s, a = Session(DESC, (32,), 0.9, device="cpu", kv_bits=bits), Stream("A", log)
+    at, empty, made = [None], torch.empty, []
+
+    @contextlib.contextmanager
+    def on(stream):
+        at.append(stream)
+        yield
+        at.pop()
+    monkeypatch.setattr(torch.cuda, "stream", on)
+    monkeypatch.setattr(torch, "empty", lambda *args, **kw: made.append(at[-1]) or empty(*args, **kw))
+    _prefill(s, stream=a)
+    assert made == [a] * (3 if bits == 4 else 1)  # the workspace, and staging rows of K and V
+
+
 # ----------------------------------------------------------------------------- on the GPU
 
 def _request(seed):
