@@ -9,9 +9,11 @@
 // sources lie at or above the budget and destinations below it.
 //
 // The ordered compaction moves nearly every row (the first to leave is early) and is bound by memory, as far as three
-// CTAs per SM keep it busy: 768 units of 2 333 rows down to 2 301 take 100 us (0.78 of the measured copy rate), 192 units
-// of 11 554 to 11 522 163 us (0.61: 192 CTAs on 152 SMs). Hole filling moves 32 rows of those and is bound by the
-// selection's passes: 32 and 62 us. 192 units of 189 rows to 157: 8 us.
+// CTAs per SM keep it busy: 768 units of 2 333 rows down to 2 301 take 107 us (0.73 of the measured copy rate), 192 units
+// of 11 554 to 11 522 163 us (0.60: 192 CTAs on 152 SMs). Hole filling moves 32 rows of those and is bound by the
+// selection's passes: 39 and 62 us. 192 units of 189 rows to 157: 8 us.
+// The room for scores and positions goes by the capacity, which the host knows: hole filling takes 96 us for the 768 units
+// in a capacity of 20 480 (one CTA per SM), and 99 for the 192 in one of 47 048, where they are read where they lie.
 #include <type_traits>
 
 #include "q4.cuh"
@@ -79,9 +81,8 @@ struct Cut {
     int ties;      // how many there are
 };
 
-// (No key has a bit above the digit at top_shift.)
 // The rank-th smallest (from 1) key over the j in [lo, hi) for which key_of(j, key) is true. rank is at most
-// their number.
+// their number, and no key has a bit above the digit at top_shift.
 template <int NT, typename KeyOf>
 __device__ Cut select_kth(int lo, int hi, int rank, KeyOf key_of, Scratch<NT> &s, int top_shift = 24) {
     const int tid = threadIdx.x;

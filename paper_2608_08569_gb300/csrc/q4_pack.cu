@@ -8,8 +8,8 @@
 // Reading back: a lane takes 8 channels, so that a warp's stores are whole lines (16 per lane: 255 instead of 218 us).
 //
 // Both are bound by instructions and latency rather than HBM. 768 units of 2 301 rows, D = 128, bf16: packing 283 us
-// (1.16 GB, 0.60 of the measured copy rate, 14 instructions per channel of K or V at 2.3 per cycle), reading back 218 us
-// (0.78). Asking rows into L2 ahead gained nothing for bf16 and cost fp32 a fifth.
+// (1.16 GB, 0.60 of the measured copy rate, 14 instructions per channel of K or V at 2.3 per cycle), reading back 215 us
+// (0.80); fp32 470 (0.65) and 415 us (0.73). Asking rows into L2 ahead gained nothing for bf16 and cost fp32 a fifth.
 #include <cooperative_groups.h>
 
 #include <type_traits>
