@@ -463,6 +463,122 @@ voxzip_status voxzip_evict_q4(const voxzip_cache_desc *desc, const voxzip_q4_cac
                               const voxzip_evict_policy *policy, voxzip_stream_t stream);
 
 /*
+ * A turn's prompt: rows of the model's projections, rotated, appended to a cache and attending over it. It is how a
+ * request's own prompt gets into the slabs that stage 1 reads, and how a later turn of its conversation joins the
+ * rows that compression has kept.
+ *
+ * The rows of several sequences are packed: sequence b's tokens are rows [seq_off[b], seq_off[b + 1]) of q, k and v,
+ * with 0 <= seq_off[b] <= seq_off[b + 1] <= tokens (sequences may be empty; rows of no sequence are left alone, in the
+ * outputs too). Offsets that break this set VOXZIP_DEV_BAD_SPANS; nothing is appended then, and no sequence from the
+ * first bad one on attends.
+ */
+typedef struct {
+    const void *data;     /* [layer][token][head][D]: heads D apart; 16-byte aligned */
+    int64_t token_stride; /* elements from a token to the next: at least heads * D, a multiple of 16 bytes */
+    int64_t layer_stride; /* elements from a layer to the next, a multiple of 16 bytes */
+} voxzip_rows;            /* so q, k and v may be views of one projection's output */
+
+typedef enum {
+    VOXZIP_PAIR_HALVES = 0,  /* pair i is channels i and i + R / 2 */
+    VOXZIP_PAIR_ADJACENT = 1 /* pair i is channels 2 i and 2 i + 1 */
+} voxzip_rotary_pairing;
+
+/* Rotary positions of the first R = rotary_dim channels of a head. Pair i (lo, hi) becomes
+ *   (lo cos th - hi sin th, hi cos th + lo sin th),  th = position[axis[i]] * freq[i],
+ * with th exact to 2^-60 of a turn for any int32 position, in fp32 and rounded once. Several axes (time, height and
+ * width, say) give each pair a position of its own. */
+typedef struct {
+    int32_t rotary_dim;  /* R: a multiple of 16, at most the head dimension; channels from R on stay as they are */
+    int32_t axes;        /* position axes, 1 to 255 */
+    int32_t pairing;     /* voxzip_rotary_pairing */
+    const double *freq;  /* HOST memory, [R / 2]: radians per position, magnitude at most 1e6 */
+    const uint8_t *axis; /* HOST memory, [R / 2]: the axis of each pair, below axes; NULL: all 0 */
+} voxzip_rotary_desc;
+
+/*
+ * Rotates rows of q and k, as for a decode step whose q and k_new come unrotated.
+ *   q, k       NULL, or rows of q_heads and kv_heads heads; at least one of the two
+ *   positions  [axes][tokens] device int32, the same for every layer
+ *   q_out      [layer_count][tokens][Hq][D];  k_out  [layer_count][tokens][Hkv][D]; either may be its input, if that is
+ *              dense
+ * desc gives the heads, the head dimension and the dtype. tokens may be 0.
+ */
+voxzip_status voxzip_rotary(const voxzip_cache_desc *desc, const voxzip_rotary_desc *rotary, int32_t layer_count,
+                            int32_t tokens, const voxzip_rows *q, const voxzip_rows *k, const int32_t *positions,
+                            void *q_out, void *k_out, voxzip_stream_t stream);
+
+/* Bytes of workspace voxzip_append and voxzip_append_paged need (0 if the arguments are invalid). */
+size_t voxzip_append_workspace_size(const voxzip_cache_desc *desc, int32_t layer_count);
+
+/*
+ * Appends the rows of every sequence to its units of layers [layer_begin, layer_begin + layer_count): with m tokens
+ * and a unit of length n, token i's k row, rotated, and v row go to slot n + i, with score 0 and pos = new_pos[token];
+ * len becomes n + m. q rows are rotated beside them.
+ *   rotary     NULL: k and q rows as they are (positions is not read)
+ *   q          NULL, or rows of q_heads heads; q_out [layer_count][tokens][Hq][D]
+ *   k, v       rows of kv_heads heads
+ *   positions  [axes][tokens] device int32;  new_pos [tokens] device int32
+ *   seq_off    [B + 1] device int32
+ *   max_rows   host-side bound on the tokens of one sequence, or 0; a hint, which changes no result
+ *   score, pos NULL: not kept (a prompt that stage 1 will read: its slab is a cache whose capacity is the
+ *              prefill stride); new_pos may then be NULL too
+ *   workspace  device scratch of voxzip_append_workspace_size() bytes, 256-byte aligned; contents need not be
+ *              initialised
+ * Device errors: VOXZIP_DEV_CAPACITY (a length outside [0, C], or n + m > C; the unit is skipped), BAD_SPANS.
+ */
+voxzip_status voxzip_append(const voxzip_cache_desc *desc, const voxzip_rotary_desc *rotary, int32_t layer_begin,
+                            int32_t layer_count, int32_t tokens, const voxzip_rows *q, const voxzip_rows *k,
+                            const voxzip_rows *v, const int32_t *positions, const int32_t *new_pos,
+                            const int32_t *seq_off, int32_t max_rows, void *k_cache, void *v_cache, float *score,
+                            int32_t *pos, int32_t *len, void *q_out, void *workspace, size_t workspace_bytes,
+                            voxzip_stream_t stream);
+
+/* voxzip_append on a paged cache, in the descriptor's dtype: a unit takes the pages of its new rows and of the next
+   append's slot, or, with VOXZIP_DEV_CAPACITY, none and is skipped. A page index outside the pool sets
+   VOXZIP_DEV_CAPACITY too; its rows are not written. */
+voxzip_status voxzip_append_paged(const voxzip_cache_desc *desc, const voxzip_paged_cache *paged,
+                                  const voxzip_rotary_desc *rotary, int32_t layer_begin, int32_t layer_count,
+                                  int32_t tokens, const voxzip_rows *q, const voxzip_rows *k, const voxzip_rows *v,
+                                  const int32_t *positions, const int32_t *new_pos, const int32_t *seq_off,
+                                  int32_t max_rows, float *score, int32_t *pos, int32_t *len, void *q_out,
+                                  void *workspace, size_t workspace_bytes, voxzip_stream_t stream);
+
+/* Bytes of workspace voxzip_prompt_attention and its paged form need: 0 for a call whose rows fill the GPU (and if the
+   arguments are invalid); otherwise the parts of the keys that CTAs share out, before they are joined. */
+size_t voxzip_prompt_attention_workspace_size(const voxzip_cache_desc *desc, int32_t layer_count, int32_t tokens,
+                                              int32_t max_rows, int32_t max_len);
+
+/*
+ * Causal attention of the rows appended last: with m tokens of a sequence and a unit of length n (theirs included),
+ * token i's queries see slots [0, n - m + i] of their kv-head's unit, all kept rows and the turn's own up to it:
+ *   out = softmax(scale * q K^T) V.
+ * A token that sees no slot (n - m + i < 0) gets 0. What lies in slots that a token does not see, infinities and NaN
+ * too, has no part in its result. Scores do not change: they follow the decode steps.
+ *   q          rows of q_heads heads, rotated;  out [layer_count][tokens][Hq][D]
+ *   seq_off    [B + 1] device int32;  len [B][L][Hkv] device int32, read
+ *   sm_scale   logit scale; <= 0 selects 1/sqrt(D)
+ *   max_rows   host-side bound on the tokens of one sequence, or 0 (tokens);  max_len on the length of a unit, or 0
+ *              (the capacity). Hints for the launch: others change which CTAs share the keys, not what is computed
+ *   workspace  device scratch of voxzip_prompt_attention_workspace_size() bytes for the same arguments, 256-byte
+ *              aligned; NULL where that is 0
+ * Requires D in {64, 128}, G <= 16. Device errors: VOXZIP_DEV_CAPACITY (a length outside [0, C]; the unit's rows of
+ * out are not written), BAD_SPANS.
+ */
+voxzip_status voxzip_prompt_attention(const voxzip_cache_desc *desc, int32_t layer_begin, int32_t layer_count,
+                                      int32_t tokens, const voxzip_rows *q, const int32_t *seq_off,
+                                      const void *k_cache, const void *v_cache, const int32_t *len, float sm_scale,
+                                      int32_t max_rows, int32_t max_len, void *out, void *workspace,
+                                      size_t workspace_bytes, voxzip_stream_t stream);
+
+/* voxzip_prompt_attention on a paged cache, in the descriptor's dtype. A page index outside the pool sets
+   VOXZIP_DEV_CAPACITY; its rows count as zeros. */
+voxzip_status voxzip_prompt_attention_paged(const voxzip_cache_desc *desc, const voxzip_paged_cache *paged,
+                                            int32_t layer_begin, int32_t layer_count, int32_t tokens,
+                                            const voxzip_rows *q, const int32_t *seq_off, const int32_t *len,
+                                            float sm_scale, int32_t max_rows, int32_t max_len, void *out,
+                                            void *workspace, size_t workspace_bytes, voxzip_stream_t stream);
+
+/*
  * Waits for `stream`, then returns the device status word of the current device in *bits
  * (VOXZIP_DEV_* flags accumulated by earlier calls) and clears it.
  */

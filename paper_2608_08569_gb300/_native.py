@@ -128,6 +128,74 @@ class _Q4(ctypes.Structure):
                 ("v_scale", ctypes.c_void_p), ("k_exp", ctypes.c_void_p)]
 
 
+class _Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("layer_stride", ctypes.c_int64)]
+
+
+class _RotaryDesc(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("axes", ctypes.c_int32), ("pairing", ctypes.c_int32),
+                ("freq", ctypes.POINTER(ctypes.c_double)), ("axis", ctypes.POINTER(ctypes.c_uint8))]
+
+
+VOXZIP_PAIR_HALVES, VOXZIP_PAIR_ADJACENT = 0, 1
+_PAIRINGS = {"halves": VOXZIP_PAIR_HALVES, "adjacent": VOXZIP_PAIR_ADJACENT}
+
+
+@dataclass(frozen=True)
+class RotaryDesc:
+    """Rotary positions of a head's first 2 * len(freqs) channels: pair i turns by position[axes[i]] * freqs[i]
+    radians. A pair is channels (i, i + R / 2) with pairing="halves", (2 i, 2 i + 1) with "adjacent". `axes` holds the
+    position axis of each pair; empty, all pairs follow axis 0. (Build the usual ones with RotaryDesc.make.)"""
+    freqs: tuple
+    axes: tuple = ()
+    pairing: str = "halves"
+
+    @staticmethod
+    def make(rotary_dim: int, theta: float = 10000.0, sections=None, in_turns: bool = False,
+             pairing: str = "halves") -> "RotaryDesc":
+        """Frequencies theta^(-2 i / rotary_dim). `sections` gives the pairs of each position axis: one block after
+        the other, or with in_turns=True axis a > 0 takes the pairs i = a, a + A, ... (A axes) up to its number of
+        them and axis 0 the others."""
+        half = rotary_dim // 2
+        freqs = tuple(float(theta) ** (-2.0 * i / rotary_dim) for i in range(half))
+        if sections is None:
+            return RotaryDesc(freqs, (), pairing)
+        sec = [int(x) for x in sections]
+        if sum(sec) != half or min(sec) < 0:
+            raise ValueError(f"sections {tuple(sec)} do not add up to {half} pairs")
+        A = len(sec)
+        if in_turns:
+            axes = tuple(i % A if i % A and i < A * sec[i % A] else 0 for i in range(half))
+            if any(axes.count(a) != n for a, n in enumerate(sec)):
+                raise ValueError(f"sections {tuple(sec)} cannot be taken in turns")
+        else:
+            axes = tuple(a for a, n in enumerate(sec) for _ in range(n))
+        return RotaryDesc(freqs, axes, pairing)
+
+    @property
+    def rotary_dim(self) -> int:
+        return 2 * len(self.freqs)
+
+    @functools.cached_property
+    def num_axes(self) -> int:
+        return max(self.axes, default=0) + 1
+
+    @functools.cached_property
+    def _c(self):
+        if self.pairing not in _PAIRINGS:
+            raise ValueError("pairing must be 'halves' or 'adjacent'")
+        n = len(self.freqs)
+        if self.axes and (len(self.axes) != n or min(self.axes) < 0 or max(self.axes) > 254):
+            raise ValueError("axes must hold an axis from 0 to 254 for each of the freqs")
+        freq = (ctypes.c_double * max(n, 1))(*self.freqs)
+        axis = (ctypes.c_uint8 * n)(*self.axes) if self.axes else None
+        return _RotaryDesc(2 * n, self.num_axes, _PAIRINGS[self.pairing], freq, axis)
+
+    def __getstate__(self):  # as CacheDesc: the fields alone
+        return {k: v for k, v in self.__dict__.items()
+                if not isinstance(getattr(type(self), k, None), functools.cached_property)}
+
+
 PAGE_TOKENS = 64
 Q4_CAPACITY_MULTIPLE, Q4_GROUP = 4, 32
 
@@ -181,6 +249,20 @@ def lib() -> ctypes.CDLL:
             L.voxzip_decode_step_q4.argtypes = [_DP, _QP, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _f32, _f32,
                                                 _i32, _vp, _vp]
             L.voxzip_evict_q4.argtypes = [_DP, _QP, _i32, _i32, _vp, _vp, _vp, _vp, ctypes.POINTER(_EvictPolicy), _vp]
+            _RP, _TP = ctypes.POINTER(_Rows), ctypes.POINTER(_RotaryDesc)
+            L.voxzip_rotary.argtypes = [_DP, _TP, _i32, _i32, _RP, _RP, _vp, _vp, _vp, _vp]
+            L.voxzip_append_workspace_size.argtypes = [_DP, _i32]
+            L.voxzip_append_workspace_size.restype = _sz
+            L.voxzip_append.argtypes = [_DP, _TP, _i32, _i32, _i32, _RP, _RP, _RP, _vp, _vp, _vp, _i32, _vp, _vp, _vp,
+                                        _vp, _vp, _vp, _vp, _sz, _vp]
+            L.voxzip_append_paged.argtypes = [_DP, _PP, _TP, _i32, _i32, _i32, _RP, _RP, _RP, _vp, _vp, _vp, _i32, _vp,
+                                              _vp, _vp, _vp, _vp, _sz, _vp]
+            L.voxzip_prompt_attention_workspace_size.argtypes = [_DP, _i32, _i32, _i32, _i32]
+            L.voxzip_prompt_attention_workspace_size.restype = _sz
+            L.voxzip_prompt_attention.argtypes = [_DP, _i32, _i32, _i32, _RP, _vp, _vp, _vp, _vp, _f32, _i32, _i32,
+                                                  _vp, _vp, _sz, _vp]
+            L.voxzip_prompt_attention_paged.argtypes = [_DP, _PP, _i32, _i32, _i32, _RP, _vp, _vp, _f32, _i32, _i32,
+                                                        _vp, _vp, _sz, _vp]
             L.voxzip_selftest_bounded_wait.argtypes = [ctypes.c_uint32, _vp]
             L.voxzip_selftest_bounded_wait.restype = _i32
             L.voxzip_stream_read.argtypes = [_vp, _sz, _vp, _vp]
@@ -197,7 +279,8 @@ def lib() -> ctypes.CDLL:
             for f in (L.voxzip_anchor_fuse, L.voxzip_decode_step, L.voxzip_evict, L.voxzip_get_status,
                       L.voxzip_segments_to_spans, L.voxzip_embed_fuse, L.voxzip_evict_ex, L.voxzip_paged_init,
                       L.voxzip_anchor_fuse_paged, L.voxzip_decode_step_paged, L.voxzip_evict_paged, L.voxzip_q4_pack,
-                      L.voxzip_q4_unpack, L.voxzip_decode_step_q4, L.voxzip_evict_q4):
+                      L.voxzip_q4_unpack, L.voxzip_decode_step_q4, L.voxzip_evict_q4, L.voxzip_rotary, L.voxzip_append,
+                      L.voxzip_append_paged, L.voxzip_prompt_attention, L.voxzip_prompt_attention_paged):
                 f.restype = _i32
             _lib = L
     return _lib
@@ -695,6 +778,182 @@ def voxzip_evict_q4(desc: CacheDesc, qc, layer_begin: int, layer_count: int, bud
     _check("voxzip_evict_q4", lib().voxzip_evict_q4(
         ctypes.byref(desc._c), ctypes.byref(qs), int(layer_begin), int(layer_count), _ptr(qc["score"]),
         _ptr(qc["pos"]), _ptr(qc["len"]), _ptr(budget), ctypes.byref(pol), _stream(stream)))
+
+
+def _rows(t, name: str, desc: CacheDesc, heads: int, like=None):
+    """Checks rows [layers][tokens][heads][D] (heads dense, tokens and layers at any stride of whole 16-byte vectors)
+    and returns their C struct; `like` is (layers, tokens)."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dtype != desc.dtype:
+        raise ValueError(f"{name}: dtype {t.dtype}, expected {desc.dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be on a CUDA device")
+    if t.dim() != 4 or t.shape[2] != heads or t.shape[3] != desc.head_dim or (like and tuple(t.shape[:2]) != like):
+        n = like or ("layers", "tokens")
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {(*n, heads, desc.head_dim)}")
+    L, T = t.shape[:2]
+    sl, st, sh, sd = t.stride()
+    D, vec = desc.head_dim, 16 // t.element_size()
+    if T and L:
+        if sd != 1 or (heads > 1 and sh != D) or (T > 1 and (st % vec or st < heads * D)) or (L > 1 and (sl % vec or sl < 1)) or \
+                t.data_ptr() % 16:
+            raise ValueError(f"{name}: strides {tuple(t.stride())}: heads must be dense, tokens apart, and every token's "
+                             "rows aligned to 16 bytes")
+    return _Rows(t.data_ptr(), st, sl)
+
+
+def _positions(positions, rotary: RotaryDesc, tokens: int) -> None:
+    axes = rotary.num_axes
+    if positions is not None and isinstance(positions, torch.Tensor) and positions.dim() == 1 and axes == 1:
+        _need(positions, "positions", torch.int32, (tokens,))
+    else:
+        if isinstance(positions, torch.Tensor) and positions.dim() == 2 and positions.shape[0] > axes:
+            axes = positions.shape[0]  # a model's axes that no pair follows
+        _need(positions, "positions", torch.int32, (axes, tokens))
+
+
+def _scratch(workspace, need: int, device, stream):
+    """The caller's workspace, or one that belongs to the stream of the launches."""
+    if workspace is not None:
+        _need(workspace, "workspace", torch.uint8)
+        return workspace.data_ptr(), workspace.numel(), workspace
+    if need == 0:
+        return None, 0, None
+    if stream is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    else:
+        at = stream if hasattr(stream, "wait_event") else torch.cuda.ExternalStream(stream.cuda_stream)
+        with torch.cuda.stream(at):
+            workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    return workspace.data_ptr(), need, workspace
+
+
+def voxzip_rotary(desc: CacheDesc, rotary: RotaryDesc, positions, *, q=None, k=None, q_out=None, k_out=None,
+                  stream=None) -> None:
+    """Rotates rows q [layers][tokens][Hq][D] and k [layers][tokens][Hkv][D] (either may be None) into q_out and k_out,
+    which may be the inputs. positions is [axes][tokens] (or [tokens] for one axis), the same for every layer."""
+    if q is None and k is None:
+        raise ValueError("voxzip_rotary needs q or k")
+    qr = None if q is None else _rows(q, "q", desc, desc.q_heads)
+    L, T = (k if q is None else q).shape[:2]
+    kr = None if k is None else _rows(k, "k", desc, desc.kv_heads, (L, T))
+    if q is not None:
+        _need(q_out, "q_out", desc.dtype, (L, T, desc.q_heads, desc.head_dim))
+    if k is not None:
+        _need(k_out, "k_out", desc.dtype, (L, T, desc.kv_heads, desc.head_dim))
+    _positions(positions, rotary, T)
+    if L == 0:
+        return
+    _check("voxzip_rotary", lib().voxzip_rotary(
+        ctypes.byref(desc._c), ctypes.byref(rotary._c), L, T, qr and ctypes.byref(qr), kr and ctypes.byref(kr),
+        positions.data_ptr(), _ptr(q_out), _ptr(k_out), _stream(stream)))
+
+
+def voxzip_append_workspace_size(desc: CacheDesc, layer_count: int) -> int:
+    return int(lib().voxzip_append_workspace_size(ctypes.byref(desc._c), int(layer_count)))
+
+
+def _append_args(desc: CacheDesc, layer_count: int, k, v, new_pos, seq_off, rotary, positions, q, q_out, pos_kept: bool):
+    kr = _rows(k, "k", desc, desc.kv_heads)
+    L, T = k.shape[:2]
+    if L != layer_count:
+        raise ValueError(f"k: {L} layers, expected {layer_count}")
+    vr = _rows(v, "v", desc, desc.kv_heads, (L, T))
+    _need(seq_off, "seq_off", torch.int32, (desc.batch + 1,))
+    if pos_kept or new_pos is not None:
+        _need(new_pos, "new_pos", torch.int32, (T,))
+    qr = None
+    if q is not None:
+        qr = _rows(q, "q", desc, desc.q_heads, (L, T))
+        _need(q_out, "q_out", desc.dtype, (L, T, desc.q_heads, desc.head_dim))
+    if rotary is not None:
+        _positions(positions, rotary, T)
+    else:
+        positions = None
+    return T, qr, kr, vr, positions
+
+
+def voxzip_append(desc: CacheDesc, layer_begin: int, layer_count: int, k, v, new_pos, seq_off, k_cache, v_cache, score,
+                  pos, len_, *, rotary: RotaryDesc | None = None, positions=None, q=None, q_out=None, max_rows: int = 0,
+                  workspace=None, stream=None) -> None:
+    """Appends packed rows k and v [layer_count][tokens][Hkv][D] (sequence b's are tokens [seq_off[b], seq_off[b + 1]))
+    to the units of layers [layer_begin, layer_begin + layer_count), k rotated on the way; q, if given, is rotated into
+    q_out. score and pos may be None (a slab that stage 1 will read); rotary=None appends rows as they are."""
+    T, qr, kr, vr, positions = _append_args(desc, layer_count, k, v, new_pos, seq_off, rotary, positions, q, q_out, pos is not None)
+    _need(k_cache, "k_cache", desc.dtype, desc._rows)
+    _need(v_cache, "v_cache", desc.dtype, desc._rows)
+    if score is not None:
+        _need(score, "score", torch.float32, desc._slots)
+    if pos is not None:
+        _need(pos, "pos", torch.int32, desc._slots)
+    _need(len_, "len", torch.int32, desc._units)
+    at, size, _keep = _scratch(workspace, voxzip_append_workspace_size(desc, layer_count), k_cache.device, stream)
+    _check("voxzip_append", lib().voxzip_append(
+        ctypes.byref(desc._c), rotary and ctypes.byref(rotary._c), int(layer_begin), int(layer_count), T,
+        qr and ctypes.byref(qr), ctypes.byref(kr), ctypes.byref(vr), _ptr(positions), _ptr(new_pos), seq_off.data_ptr(),
+        int(max_rows), k_cache.data_ptr(), v_cache.data_ptr(), _ptr(score), _ptr(pos), len_.data_ptr(), _ptr(q_out),
+        at, size, _stream(stream)))
+
+
+def voxzip_append_paged(desc: CacheDesc, pc, layer_begin: int, layer_count: int, k, v, new_pos, seq_off, *,
+                        rotary: RotaryDesc | None = None, positions=None, q=None, q_out=None, max_rows: int = 0,
+                        workspace=None, stream=None) -> None:
+    """voxzip_append on a paged cache: each unit takes the pages that its new rows need."""
+    T, qr, kr, vr, positions = _append_args(desc, layer_count, k, v, new_pos, seq_off, rotary, positions, q, q_out, True)
+    _check_dense_state(desc, pc["score"], pc["pos"], pc["len"])
+    ps = _paged_struct(desc, pc)
+    at, size, _keep = _scratch(workspace, voxzip_append_workspace_size(desc, layer_count), pc["k_pool"].device, stream)
+    _check("voxzip_append_paged", lib().voxzip_append_paged(
+        ctypes.byref(desc._c), ctypes.byref(ps), rotary and ctypes.byref(rotary._c), int(layer_begin), int(layer_count), T,
+        qr and ctypes.byref(qr), ctypes.byref(kr), ctypes.byref(vr), _ptr(positions), _ptr(new_pos), seq_off.data_ptr(),
+        int(max_rows), pc["score"].data_ptr(), pc["pos"].data_ptr(), pc["len"].data_ptr(), _ptr(q_out), at, size,
+        _stream(stream)))
+
+
+def voxzip_prompt_attention_workspace_size(desc: CacheDesc, layer_count: int, tokens: int, max_rows: int = 0,
+                                           max_len: int = 0) -> int:
+    return int(lib().voxzip_prompt_attention_workspace_size(ctypes.byref(desc._c), int(layer_count), int(tokens),
+                                                            int(max_rows), int(max_len)))
+
+
+def _attention_args(desc: CacheDesc, layer_count: int, q, seq_off, out, max_rows, max_len, workspace, stream):
+    qr = _rows(q, "q", desc, desc.q_heads)
+    L, T = q.shape[:2]
+    if L != layer_count:
+        raise ValueError(f"q: {L} layers, expected {layer_count}")
+    _need(seq_off, "seq_off", torch.int32, (desc.batch + 1,))
+    _need(out, "out", desc.dtype, (L, T, desc.q_heads, desc.head_dim))
+    need = voxzip_prompt_attention_workspace_size(desc, L, T, max_rows, max_len) if T else 0
+    return T, qr, _scratch(workspace, need, out.device, stream)
+
+
+def voxzip_prompt_attention(desc: CacheDesc, layer_begin: int, layer_count: int, q, seq_off, k_cache, v_cache, len_, out, *,
+                            sm_scale: float = 0.0, max_rows: int = 0, max_len: int = 0, workspace=None,
+                            stream=None) -> None:
+    """Causal attention of the rows appended last: token i of a sequence's m sees slots [0, n - m + i] of its units of
+    length n. q and out are [layer_count][tokens][Hq][D]; max_rows and max_len are hints for the launch."""
+    T, qr, (at, size, _keep) = _attention_args(desc, layer_count, q, seq_off, out, max_rows, max_len, workspace, stream)
+    _need(k_cache, "k_cache", desc.dtype, desc._rows)
+    _need(v_cache, "v_cache", desc.dtype, desc._rows)
+    _need(len_, "len", torch.int32, desc._units)
+    _check("voxzip_prompt_attention", lib().voxzip_prompt_attention(
+        ctypes.byref(desc._c), int(layer_begin), int(layer_count), T, ctypes.byref(qr), seq_off.data_ptr(),
+        k_cache.data_ptr(), v_cache.data_ptr(), len_.data_ptr(), float(sm_scale), int(max_rows), int(max_len),
+        out.data_ptr(), at, size, _stream(stream)))
+
+
+def voxzip_prompt_attention_paged(desc: CacheDesc, pc, layer_begin: int, layer_count: int, q, seq_off, out, *,
+                                  sm_scale: float = 0.0, max_rows: int = 0, max_len: int = 0, workspace=None,
+                                  stream=None) -> None:
+    """voxzip_prompt_attention on a paged cache."""
+    T, qr, (at, size, _keep) = _attention_args(desc, layer_count, q, seq_off, out, max_rows, max_len, workspace, stream)
+    _need(pc["len"], "len", torch.int32, desc._units)
+    ps = _paged_struct(desc, pc)
+    _check("voxzip_prompt_attention_paged", lib().voxzip_prompt_attention_paged(
+        ctypes.byref(desc._c), ctypes.byref(ps), int(layer_begin), int(layer_count), T, ctypes.byref(qr),
+        seq_off.data_ptr(), pc["len"].data_ptr(), float(sm_scale), int(max_rows), int(max_len), out.data_ptr(), at, size,
+        _stream(stream)))
 
 
 def voxzip_selftest_bounded_wait(limit: int = 1000, stream=None) -> None:

@@ -1,0 +1,127 @@
+// A turn's prompt: packed rows of several sequences, rotated, appended to a cache and attending over it. Shared by
+// rotary.cu, prompt_attn.cu, prompt_attn_mma.cu and the C ABI (api_prompt.cu).
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "common.cuh"
+#include "paged.cuh"
+#include "voxzip.h"
+
+namespace voxzip {
+
+constexpr int kMaxPairs = 64;  // rotated pairs of a head (D <= 128)
+
+// A rotation as the kernels take it, by value. A frequency is a fraction of a turn per position in 64-bit fixed
+// point, so position * frequency is exact modulo a turn for any 32-bit position.
+struct RotaryTable {
+    uint64_t turns[kMaxPairs];
+    uint8_t axis[kMaxPairs];
+    int32_t half;      // pairs
+    int32_t adjacent;  // pairs are channels (2 i, 2 i + 1), not (i, i + half)
+};
+
+// Rows [layer][token][head][D] of a packed tensor; strides in elements.
+struct RowsView {
+    const void *data;
+    int64_t token_stride, layer_stride;
+};
+
+struct CacheRows {  // where a unit's rows lie: dense slabs (pv.table null) or page pools
+    void *k, *v;
+    PageView pv;
+    int64_t pool_rows;  // rows of k and v: every row index is below it
+};
+
+cudaError_t launch_rotary(const voxzip_cache_desc &d, const RotaryTable &table, int32_t layer_count, int32_t tokens,
+                          RowsView q, RowsView k, const int32_t *positions, void *q_out, void *k_out,
+                          cudaStream_t stream);
+
+size_t append_workspace_bytes(const voxzip_cache_desc &d, int32_t layer_count);
+cudaError_t launch_append(const voxzip_cache_desc &d, const RotaryTable *table, int32_t layer_begin,
+                          int32_t layer_count, RowsView q, RowsView k, RowsView v, const int32_t *positions,
+                          const int32_t *new_pos, const int32_t *seq_off, int32_t tokens, int32_t max_rows,
+                          const CacheRows &cache, float *score, int32_t *pos, int32_t *len, void *q_out,
+                          void *workspace, int32_t *status, cudaStream_t stream);
+
+// The attention of packed rows over their units. Rows of a tile are (token, head of the group) pairs, head fastest:
+// the G query heads of a kv-head share its K and V tiles, whatever G is.
+struct PromptAttn {
+    RowsView q;
+    const int32_t *seq_off;
+    const int32_t *len;
+    CacheRows cache;
+    void *out;
+    float *part_o;   // [splits][layer_count * T * Hq][D], of splits > 1
+    float2 *part_ml; // [splits][layer_count * T * Hq]: running maximum (in units of log2) and sum
+    int32_t *status;
+    float scale_log2;  // logit scale times log2(e)
+    int32_t B, L, Hq, Hkv, G, C, T;
+    int32_t layer_begin, layer_count;
+    int32_t tile_tokens;  // tokens per CTA
+    int32_t tiles;        // bound on the CTAs of all sequences
+    int32_t splits;
+    int64_t kv_rows;  // rows of the K and V tensors (checked builds)
+};
+
+// A CTA's place: tile `x` of those of all sequences, in packed order, the last tile of a sequence first (it sees the
+// most keys, and CTAs start in order).
+struct TileAt {
+    int32_t b, t0, rows, before;  // sequence, first packed token, tokens of this tile, its first token's index in the sequence
+    int32_t m;                    // the sequence's tokens
+};
+
+// One warp, all lanes. False where x lies behind the last tile or the offsets are malformed up to it.
+__device__ __forceinline__ bool find_tile(const int32_t *seq_off, int32_t B, int32_t T, int32_t per, int32_t x,
+                                          int32_t *status, TileAt &at) {
+    const int lane = threadIdx.x & 31;
+    int32_t first = 0;
+    for (int32_t base = 0; base < B; base += 32) {
+        const int32_t b = base + lane;
+        const int32_t o0 = b < B ? seq_off[b] : 0, o1 = b < B ? seq_off[b + 1] : 0;
+        const bool bad = b < B && (o0 < 0 || o1 < o0 || o1 > T);
+        if (__ballot_sync(0xffffffffu, bad)) {
+            if (lane == 0) raise_status(status, VOXZIP_DEV_BAD_SPANS);
+            return false;
+        }
+        const int32_t n = (o1 - o0) / per + ((o1 - o0) % per != 0);
+        int32_t sum = n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int32_t up = __shfl_up_sync(0xffffffffu, sum, o);
+            if (lane >= o) sum += up;
+        }
+        const unsigned past = __ballot_sync(0xffffffffu, x < first + sum);
+        if (past) {
+            const int src = __ffs(past) - 1;
+            const int32_t idx = __shfl_sync(0xffffffffu, n - 1 - (x - (first + sum - n)), src);
+            const int32_t s0 = __shfl_sync(0xffffffffu, o0, src), s1 = __shfl_sync(0xffffffffu, o1, src);
+            at.b = base + src;
+            at.m = s1 - s0;
+            at.before = idx * per;
+            at.t0 = s0 + at.before;
+            at.rows = min(per, at.m - at.before);
+            return true;
+        }
+        first += __shfl_sync(0xffffffffu, sum, 31);
+    }
+    return false;
+}
+
+// CTAs of a launch: every sequence has ceil(m / per) tiles, so all of them at most T / per + B.
+inline int64_t tile_bound(int64_t tokens, int64_t B, int per) { return tokens / per + (B < tokens ? B : tokens); }
+
+struct PromptPlan {
+    int32_t splits;
+    size_t workspace;
+};
+PromptPlan prompt_plan(const voxzip_cache_desc &d, int32_t layer_count, int32_t tokens, int32_t max_rows,
+                       int32_t max_len);
+cudaError_t launch_prompt_attention(const voxzip_cache_desc &d, int32_t layer_begin, int32_t layer_count, RowsView q,
+                                    const int32_t *seq_off, int32_t tokens, const CacheRows &cache,
+                                    const int32_t *len, float sm_scale, int32_t max_rows, int32_t max_len, void *out,
+                                    void *workspace, int32_t *status, cudaStream_t stream);
+
+}  // namespace voxzip

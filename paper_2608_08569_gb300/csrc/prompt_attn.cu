@@ -1,0 +1,350 @@
+// Causal attention of a prompt's packed rows over their units' caches: launch planning, the kernel of fp32 rows and the
+// join of split launches. bf16 rows go to the tensor cores (prompt_attn_mma.cu).
+//
+//   row i of m in a unit of n rows:  o = sum_j w_j v_j / sum_j w_j,  w_j = 2^(c q.k_j - max),  j <= n - m + i
+//
+// One pass over K and V with the running maximum and sum in registers. A tile's 128 rows are (token, head of the group)
+// pairs, so the G heads of a kv-head read its K and V once, and few tokens still fill a tile.
+#include <algorithm>
+
+#include "evict_policy.cuh"  // once_per_device
+#include "prompt.cuh"
+#include "ptx.cuh"
+
+namespace voxzip {
+namespace {
+
+constexpr int kSms = 152;
+constexpr int kRows = 128, kKeys = 64;
+
+template <int D> struct Smem {
+    static constexpr int kQ = D + 4, kK = D + 4, kP = kRows + 4;  // row lengths: 4 words on, the next row's banks
+    float q[kRows * kQ];
+    float k[kKeys * kK];
+    float v[kKeys * D];
+    float p[kKeys * kP];
+    TileAt at;
+    int ok;
+};
+
+// Cache row of slot s, or -1 where its page is not in the pool.
+__device__ __forceinline__ int64_t cache_row(const PromptAttn &p, int64_t cu, int32_t s) {
+    if (!p.cache.pv.table) return cu * p.C + s;
+    const int64_t r = paged_row(p.cache.pv, cu, s);
+    return r >= 0 && r < p.cache.pool_rows ? r : -1;
+}
+
+// Stores row `at` ([layer][token][head]) of the result, or of this CTA's split.
+template <typename T, int N>
+__device__ __forceinline__ void store_row(const PromptAttn &p, int64_t at, int d, const float (&o)[N], float inv,
+                                          bool split, int s, int D) {
+    if (split) {
+        float *to = p.part_o + ((int64_t)s * p.layer_count * p.T * p.Hq + at) * D + d;
+#pragma unroll
+        for (int i = 0; i < N; ++i) to[i] = o[i];
+    } else {
+        T *to = static_cast<T *>(p.out) + at * D + d;
+#pragma unroll
+        for (int i = 0; i < N; ++i) to[i] = Elem<T>::from_f(o[i] * inv);
+    }
+}
+
+// 256 threads as 16 x 16: thread (ty, tx) has the logits of rows ty + 16 i and keys tx + 16 j, and of the output the
+// same rows' channels 4 tx (and 64 + 4 tx). Fused multiply-adds bound it: per four channels 128 of them meet twelve
+// 16-byte reads of shared memory.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) prompt_rows_kernel(const PromptAttn p) {
+    extern __shared__ __align__(16) uint8_t raw[];
+    Smem<D> &sm = *reinterpret_cast<Smem<D> *>(raw);
+    const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+    const int h = blockIdx.y % p.Hkv, l = blockIdx.y / p.Hkv, s = blockIdx.z;
+    ptx::grid_dependency_wait();
+    if (tid < 32) {
+        TileAt at;
+        const bool ok = find_tile(p.seq_off, p.B, p.T, p.tile_tokens, blockIdx.x, p.status, at);
+        if (tid == 0) {
+            sm.ok = ok;
+            if (ok) sm.at = at;
+        }
+    }
+    __syncthreads();
+    if (!sm.ok) return;
+    const TileAt at = sm.at;
+    const int64_t cu = ((int64_t)at.b * p.L + p.layer_begin + l) * p.Hkv + h;
+    const int32_t n = p.len[cu];
+    if (n < 0 || n > p.C) {
+        if (tid == 0) raise_status(p.status, VOXZIP_DEV_CAPACITY);
+        return;
+    }
+    const int rows = at.rows * p.G;
+    const int32_t first = n - at.m + at.before + 1;  // keys that the tile's first token sees (none if < 1)
+    const int32_t most = max(0, first + at.rows - 1);
+    // this split's keys
+    const int32_t tiles = (most + kKeys - 1) / kKeys, per = (tiles + p.splits - 1) / p.splits;
+    const int32_t j0 = min(tiles, s * per), j1 = min(tiles, j0 + per);
+
+    for (int i = tid; i < kRows * (D / 4); i += 256) {
+        const int r = i / (D / 4), d = i % (D / 4) * 4;
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (r < rows)
+            x = load4(static_cast<const T *>(p.q.data) + l * p.q.layer_stride +
+                      (int64_t)(at.t0 + r / p.G) * p.q.token_stride + (int64_t)(h * p.G + r % p.G) * D + d);
+        *reinterpret_cast<float4 *>(&sm.q[r * Smem<D>::kQ + d]) = x;
+    }
+    int32_t lim[8];  // keys that each of this thread's rows sees
+    float mx[8], sum[8], o[8][D / 16];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        lim[i] = first + (ty + 16 * i) / p.G;
+        mx[i] = -INFINITY;
+        sum[i] = 0.f;
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d) o[i][d] = 0.f;
+    }
+    for (int32_t j = j0; j < j1; ++j) {
+        const int32_t key0 = j * kKeys;
+        __syncthreads();
+        for (int i = tid; i < kKeys * (D / 4); i += 256) {
+            const int r = i / (D / 4), d = i % (D / 4) * 4;
+            float4 k = make_float4(0.f, 0.f, 0.f, 0.f), v = k;
+            if (key0 + r < most) {
+                const int64_t row = cache_row(p, cu, key0 + r);
+                if (row < 0) {
+                    if (d == 0) raise_status(p.status, VOXZIP_DEV_CAPACITY);
+                } else if (VOXZIP_IN_RANGE(p.status, row < p.kv_rows)) {
+                    k = load4(static_cast<const T *>(p.cache.k) + row * D + d);
+                    v = load4(static_cast<const T *>(p.cache.v) + row * D + d);
+                }
+            }
+            *reinterpret_cast<float4 *>(&sm.k[r * Smem<D>::kK + d]) = k;
+            *reinterpret_cast<float4 *>(&sm.v[r * D + d]) = v;
+        }
+        __syncthreads();
+        float x[8][4] = {};
+#pragma unroll 4
+        for (int d = 0; d < D; d += 4) {
+            float4 q[8], k[4];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) q[i] = *reinterpret_cast<const float4 *>(&sm.q[(ty + 16 * i) * Smem<D>::kQ + d]);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) k[c] = *reinterpret_cast<const float4 *>(&sm.k[(tx + 16 * c) * Smem<D>::kK + d]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    x[i][c] = fmaf(q[i].x, k[c].x, x[i][c]);
+                    x[i][c] = fmaf(q[i].y, k[c].y, x[i][c]);
+                    x[i][c] = fmaf(q[i].z, k[c].z, x[i][c]);
+                    x[i][c] = fmaf(q[i].w, k[c].w, x[i][c]);
+                }
+        }
+        const bool masked = key0 + kKeys > first;  // some row does not see all of this tile
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float top = -INFINITY;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                x[i][c] *= p.scale_log2;
+                if (masked && key0 + tx + 16 * c >= lim[i]) x[i][c] = -INFINITY;
+                top = fmaxf(top, x[i][c]);
+            }
+#pragma unroll
+            for (int w = 1; w < 16; w <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
+            const float was = mx[i], now = fmaxf(was, top);
+            const float ref = now == -INFINITY ? 0.f : now;  // a row that has seen no key yet
+            const float keep = exp2f(was - ref);
+            mx[i] = now;
+            sum[i] *= keep;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                x[i][c] = exp2f(x[i][c] - ref);
+                sum[i] += x[i][c];
+            }
+#pragma unroll
+            for (int d = 0; d < D / 16; ++d) o[i][d] *= keep;
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            float4 *to = reinterpret_cast<float4 *>(&sm.p[(tx + 16 * c) * Smem<D>::kP + ty * 8]);
+            to[0] = make_float4(x[0][c], x[1][c], x[2][c], x[3][c]);
+            to[1] = make_float4(x[4][c], x[5][c], x[6][c], x[7][c]);
+        }
+        __syncthreads();
+        auto accumulate = [&](auto guard) {
+#pragma unroll 4
+            for (int key = 0; key < kKeys; ++key) {
+                const float4 *pr = reinterpret_cast<const float4 *>(&sm.p[key * Smem<D>::kP + ty * 8]);
+                const float4 pa = pr[0], pb = pr[1];
+                const float w[8] = {pa.x, pa.y, pa.z, pa.w, pb.x, pb.y, pb.z, pb.w};
+                float v[D / 16];
+#pragma unroll
+                for (int c = 0; c < D / 64; ++c) {
+                    const float4 t = *reinterpret_cast<const float4 *>(&sm.v[key * D + 64 * c + 4 * tx]);
+                    v[4 * c] = t.x, v[4 * c + 1] = t.y, v[4 * c + 2] = t.z, v[4 * c + 3] = t.w;
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const bool unseen = decltype(guard)::value && key0 + key >= lim[i];
+#pragma unroll
+                    for (int d = 0; d < D / 16; ++d)  // 0 times an infinity behind the mask is not 0
+                        o[i][d] = fmaf(w[i], unseen ? 0.f : v[d], o[i][d]);
+                }
+            }
+        };
+        if (masked)
+            accumulate(std::true_type{});
+        else
+            accumulate(std::false_type{});
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+#pragma unroll
+        for (int w = 1; w < 16; w <<= 1) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], w);
+        const int r = ty + 16 * i;
+        if (r >= rows) continue;
+        const int64_t row = ((int64_t)l * p.T + at.t0 + r / p.G) * p.Hq + h * p.G + r % p.G;
+        const float inv = lim[i] <= 0 ? 0.f : 1.f / sum[i];  // a row that sees nothing is 0
+        if (p.splits > 1 && tx == 0)
+            p.part_ml[(int64_t)s * p.layer_count * p.T * p.Hq + row] = make_float2(mx[i], sum[i]);
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c) {
+            const float part[4] = {o[i][4 * c], o[i][4 * c + 1], o[i][4 * c + 2], o[i][4 * c + 3]};
+            store_row<T>(p, row, 64 * c + 4 * tx, part, inv, p.splits > 1, s, D);
+        }
+    }
+}
+
+// Joins the splits: out = sum_s o_s 2^(m_s - m) / sum_s l_s 2^(m_s - m), m the greatest m_s. A warp per row.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) prompt_join_kernel(const PromptAttn p) {
+    ptx::grid_dependency_wait();
+    const int lane = threadIdx.x & 31;
+    const int64_t rows = (int64_t)p.layer_count * p.T * p.Hq;
+    const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (row >= rows) return;
+    // rows of no sequence, or of one whose unit was skipped, were not written
+    const int32_t t = (int32_t)(row / p.Hq % p.T);
+    const int l = (int)(row / p.Hq / p.T), h = (int)(row % p.Hq) / p.G;
+    int32_t b = -1;
+    for (int32_t base = 0; base < p.B; base += 32) {
+        const int32_t c = base + lane;
+        const int32_t o0 = c < p.B ? p.seq_off[c] : 0, o1 = c < p.B ? p.seq_off[c + 1] : 0;
+        if (__any_sync(0xffffffffu, c < p.B && (o0 < 0 || o1 < o0 || o1 > p.T))) return;
+        const unsigned mine = __ballot_sync(0xffffffffu, c < p.B && o0 <= t && t < o1);
+        if (mine) {
+            b = base + __ffs(mine) - 1;
+            break;
+        }
+    }
+    if (b < 0) return;
+    const int32_t n = p.len[((int64_t)b * p.L + p.layer_begin + l) * p.Hkv + h];
+    if (n < 0 || n > p.C) return;
+    const bool none = n - p.seq_off[b + 1] + t + 1 <= 0;
+    float m = -INFINITY;
+    for (int s = lane; s < p.splits; s += 32) m = fmaxf(m, p.part_ml[s * rows + row].x);
+#pragma unroll
+    for (int w = 16; w > 0; w >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, w));
+    if (m == -INFINITY) m = 0.f;
+    float sum = 0.f, o[D / 32] = {};
+    for (int s = 0; s < p.splits; ++s) {
+        const float2 ml = p.part_ml[s * rows + row];
+        if (ml.x == -INFINITY && ml.y == 0.f) continue;  // it has no key of this row
+        const float w = exp2f(ml.x - m);
+        sum = fmaf(ml.y, w, sum);
+        const float *from = p.part_o + (s * rows + row) * D + lane * (D / 32);
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d) o[d] = fmaf(from[d], w, o[d]);
+    }
+    const float inv = none ? 0.f : 1.f / sum;
+    T *to = static_cast<T *>(p.out) + row * D + lane * (D / 32);
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) to[d] = Elem<T>::from_f(none ? 0.f : o[d] * inv);
+}
+
+cudaLaunchConfig_t config(dim3 grid, int threads, size_t smem, cudaStream_t stream, cudaLaunchAttribute *attr) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cfg;
+}
+
+template <typename T, int D>
+cudaError_t launch_rows(const PromptAttn &p, cudaStream_t stream) {
+    static std::atomic<uint64_t> done{0};
+    cudaError_t e = once_per_device(done, [] {
+        return cudaFuncSetAttribute(prompt_rows_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                    (int)sizeof(Smem<D>));
+    });
+    if (e != cudaSuccess) return e;
+    cudaLaunchAttribute attr[1];
+    const dim3 grid(p.tiles, p.Hkv * p.layer_count, p.splits);
+    cudaLaunchConfig_t cfg = config(grid, 256, sizeof(Smem<D>), stream, attr);
+    e = cudaLaunchKernelEx(&cfg, prompt_rows_kernel<T, D>, p);
+    if (e != cudaSuccess || p.splits == 1) return e;
+    const int64_t rows = (int64_t)p.layer_count * p.T * p.Hq;
+    cfg = config(dim3((unsigned)((rows + 7) / 8)), 256, 0, stream, attr);
+    return cudaLaunchKernelEx(&cfg, prompt_join_kernel<T, D>, p);
+}
+
+}  // namespace
+
+PromptPlan prompt_plan(const voxzip_cache_desc &d, int32_t layer_count, int32_t tokens, int32_t max_rows,
+                       int32_t max_len) {
+    const int G = d.q_heads / d.kv_heads;
+    const int per = kRows / G;
+    if (max_rows <= 0 || max_rows > tokens) max_rows = tokens;
+    if (max_len <= 0 || max_len > d.capacity) max_len = d.capacity;
+    // CTAs of an even launch, and keys that one walks through; a split wants four tiles of them to itself.
+    const int64_t ctas = std::max<int64_t>(1, (int64_t)tokens / per + (tokens % per != 0)) * d.kv_heads * layer_count;
+    const int64_t key_tiles = (max_len + kKeys - 1) / kKeys;
+    PromptPlan plan;
+    plan.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(kSms / ctas, key_tiles / 4));
+    const size_t rows = (size_t)layer_count * tokens * d.q_heads;
+    plan.workspace = plan.splits == 1 ? 0 : plan.splits * rows * (d.head_dim * sizeof(float) + sizeof(float2));
+    plan.workspace = (plan.workspace + 255) / 256 * 256;
+    return plan;
+}
+
+cudaError_t launch_prompt_attention(const voxzip_cache_desc &d, int32_t layer_begin, int32_t layer_count, RowsView q,
+                                    const int32_t *seq_off, int32_t tokens, const CacheRows &cache,
+                                    const int32_t *len, float sm_scale, int32_t max_rows, int32_t max_len, void *out,
+                                    void *workspace, int32_t *status, cudaStream_t stream) {
+    const PromptPlan plan = prompt_plan(d, layer_count, tokens, max_rows, max_len);
+    PromptAttn p = {};
+    p.q = q;
+    p.seq_off = seq_off;
+    p.len = len;
+    p.cache = cache;
+    p.out = out;
+    p.status = status;
+    p.scale_log2 = (sm_scale > 0.f ? sm_scale : 1.f / sqrtf((float)d.head_dim)) * 1.4426950408889634f;
+    p.B = d.batch;
+    p.L = d.layers;
+    p.Hq = d.q_heads;
+    p.Hkv = d.kv_heads;
+    p.G = d.q_heads / d.kv_heads;
+    p.C = d.capacity;
+    p.T = tokens;
+    p.layer_begin = layer_begin;
+    p.layer_count = layer_count;
+    p.splits = plan.splits;
+    p.kv_rows = cache.pool_rows;
+    if (plan.splits > 1) {
+        const size_t rows = (size_t)layer_count * tokens * d.q_heads * plan.splits;
+        p.part_o = static_cast<float *>(workspace);
+        p.part_ml = reinterpret_cast<float2 *>(p.part_o + rows * d.head_dim);
+    }
+    p.tile_tokens = kRows / p.G;
+    p.tiles = (int32_t)tile_bound(tokens, d.batch, p.tile_tokens);
+    if (d.dtype == VOXZIP_BF16)
+        return d.head_dim == 128 ? launch_rows<__nv_bfloat16, 128>(p, stream) : launch_rows<__nv_bfloat16, 64>(p, stream);
+    return d.head_dim == 128 ? launch_rows<float, 128>(p, stream) : launch_rows<float, 64>(p, stream);
+}
+
+}  // namespace voxzip

@@ -1,0 +1,387 @@
+// Rotary positions and the append of a prompt's rows.
+//
+//   th = position[axis_i] freq_i;   lo' = lo cos th - hi sin th,   hi' = hi cos th + lo sin th
+//
+// of pairs i < R / 2 of a head's first R channels, in fp32 and rounded once. A warp takes a token of a layer: it
+// computes the token's angles once (each lane two of them) for all heads, and streams the heads' rows past them, q to
+// q_out, k and v to the cache rows behind the unit's own. Bound by memory: each row is read and written once.
+#include <algorithm>
+
+#include "evict_policy.cuh"  // sm_count
+#include "prompt.cuh"
+#include "ptx.cuh"
+
+namespace voxzip {
+namespace {
+
+constexpr int kWarps = 4;
+
+struct RowsParams {
+    RotaryTable rot;  // rot.half = 0: rows as they are
+    RowsView q, k, v;
+    void *q_out, *k_out;  // k_out: rotated rows as they lie in k (no cache)
+    const int32_t *positions;  // [axes][T]
+    const int32_t *seq_off, *new_pos, *start;
+    CacheRows cache;
+    float *score;
+    int32_t *pos, *status;
+    int32_t T, B, L, Hq, Hkv, C, D;
+    int32_t layer_begin, layer_count;
+    int32_t heads;        // heads of a token: Hq (if q) + Hkv + Hkv (if a cache)
+    int32_t warp_heads;   // heads that one warp takes
+    int32_t chunks;       // warps per token
+};
+
+// sin and cos of a fraction of a turn. The nearest quarter-turn is taken off in integers, so the argument of the
+// functions is small and exact to 2^-27 of a turn.
+__device__ __forceinline__ float2 turn_cos_sin(uint64_t turns) {
+    const int32_t t = (int32_t)(turns >> 32);  // [-1/2, 1/2) turns
+    const uint32_t quarter = ((uint32_t)t + (1u << 29)) >> 30;
+    const int32_t rest = (int32_t)((uint32_t)t - (quarter << 30));  // [-1/8, 1/8) turns
+    float s, c;
+    sincospif((float)rest * 4.656612873077393e-10f, &s, &c);  // 2^-31: half-turns
+    const float2 r0 = (quarter & 1) ? make_float2(-s, c) : make_float2(c, s);
+    return (quarter & 2) ? make_float2(-r0.x, -r0.y) : r0;
+}
+
+template <typename T> struct Vec;  // 16 bytes of a row
+template <> struct Vec<float> {
+    static constexpr int N = 4;
+    static __device__ __forceinline__ void get(const uint4 &u, float (&x)[4]) {
+        x[0] = __uint_as_float(u.x), x[1] = __uint_as_float(u.y), x[2] = __uint_as_float(u.z), x[3] = __uint_as_float(u.w);
+    }
+    static __device__ __forceinline__ uint4 put(const float (&x)[4]) {
+        return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+    }
+};
+template <> struct Vec<__nv_bfloat16> {
+    static constexpr int N = 8;
+    static __device__ __forceinline__ void get(const uint4 &u, float (&x)[8]) {
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = __uint_as_float(w[i] << 16);
+            x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    }
+    static __device__ __forceinline__ uint4 put(const float (&x)[8]) {
+        return make_uint4(ptx::pack_bf16(x[0], x[1]), ptx::pack_bf16(x[2], x[3]), ptx::pack_bf16(x[4], x[5]),
+                          ptx::pack_bf16(x[6], x[7]));
+    }
+};
+
+// The sequence that packed token t belongs to, -1 for none. All lanes of a warp; 32 candidates per round.
+__device__ __forceinline__ int32_t sequence_of(const int32_t *off, int32_t B, int32_t t) {
+    const int lane = threadIdx.x & 31;
+    int32_t lo = 0, n = B + 1;  // the last entry at or below t is in [lo - 1, lo + n)
+    while (n > 0) {
+        const int32_t step = (n + 31) / 32, at = lo + lane * step;
+        const int c = __popc(__ballot_sync(0xffffffffu, lane * step < n && off[min(at, B)] <= t));
+        if (c == 0) break;
+        const int32_t next = lo + (c - 1) * step + 1;
+        n = min(lo + n, lo + c * step) - next;
+        lo = next;
+    }
+    const int32_t b = lo - 1;
+    return b >= 0 && b < B && off[b] <= t && t < off[b + 1] ? b : -1;
+}
+
+template <typename T, int D, bool kCache>
+__global__ void __launch_bounds__(32 * kWarps) rows_kernel(const RowsParams p) {
+    using V = Vec<T>;
+    constexpr int kItems = D / V::N / 2;  // pairs of vectors in a row
+    constexpr int kLanes = 32 / kItems;   // heads that a warp has in hand at once
+    __shared__ float2 angles[kWarps][kMaxPairs];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t item = (int64_t)blockIdx.x * kWarps + warp;
+    ptx::grid_dependency_wait();
+    const int64_t total = (int64_t)p.layer_count * p.T * p.chunks;
+    if (item >= total) return;
+    const int chunk = (int)(item % p.chunks);
+    const int32_t t = (int32_t)(item / p.chunks % p.T);
+    const int l = (int)(item / p.chunks / p.T);
+
+    int32_t b = 0, row = 0;
+    if (kCache) {
+        b = sequence_of(p.seq_off, p.B, t);
+        if (b < 0) return;  // behind the last sequence: left as it is
+        row = t - p.seq_off[b];
+    }
+    const int half = p.rot.half;
+    for (int i = lane; i < half; i += 32)
+        angles[warp][i] =
+            turn_cos_sin((uint64_t)(int64_t)p.positions[(int64_t)p.rot.axis[i] * p.T + t] * p.rot.turns[i]);
+    __syncwarp();
+
+    // This lane's two vectors of a row, in units of vectors, and whether they are rotated.
+    const int j = lane % kItems, sub = lane / kItems;
+    const int rot_items = half / V::N;
+    const bool rotated = j < rot_items;
+    const int va = rotated ? j : 2 * rot_items + 2 * (j - rot_items);
+    const int vb = rotated ? j + rot_items : va + 1;
+    // cos and sin of the pairs of the two vectors: of pairs side by side each vector has its own half as many
+    float2 cs[V::N];
+#pragma unroll
+    for (int i = 0; i < V::N; ++i) {
+        const int pair = !p.rot.adjacent ? j * V::N + i
+                         : i < V::N / 2  ? va * (V::N / 2) + i
+                                         : vb * (V::N / 2) + i - V::N / 2;
+        cs[i] = rotated ? angles[warp][pair] : make_float2(1.f, 0.f);
+    }
+    const int32_t new_pos = kCache && p.new_pos ? p.new_pos[t] : 0;
+
+    const int Hq = p.q.data ? p.Hq : 0;
+    const int h_end = min(p.heads, (chunk + 1) * p.warp_heads);
+#pragma unroll 2
+    for (int head = chunk * p.warp_heads + sub; head < h_end; head += kLanes) {
+        const bool is_q = head < Hq, is_v = head >= Hq + p.Hkv;
+        const int h = is_q ? head : is_v ? head - Hq - p.Hkv : head - Hq;
+        const RowsView &src = is_q ? p.q : is_v ? p.v : p.k;
+        const uint4 *from = reinterpret_cast<const uint4 *>(static_cast<const T *>(src.data) + l * src.layer_stride +
+                                                            t * src.token_stride + (int64_t)h * D);
+        uint4 a = from[va], c = from[vb];
+        if (rotated && !is_v) {
+            float x[V::N], y[V::N];
+            V::get(a, x);
+            V::get(c, y);
+            if (!p.rot.adjacent) {
+#pragma unroll
+                for (int i = 0; i < V::N; ++i) {
+                    const float lo = x[i], hi = y[i];
+                    x[i] = lo * cs[i].x - hi * cs[i].y;
+                    y[i] = hi * cs[i].x + lo * cs[i].y;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < V::N / 2; ++i) {
+                    float lo = x[2 * i], hi = x[2 * i + 1];
+                    const float2 u = cs[i], w = cs[V::N / 2 + i];
+                    x[2 * i] = lo * u.x - hi * u.y;
+                    x[2 * i + 1] = hi * u.x + lo * u.y;
+                    lo = y[2 * i], hi = y[2 * i + 1];
+                    y[2 * i] = lo * w.x - hi * w.y;
+                    y[2 * i + 1] = hi * w.x + lo * w.y;
+                }
+            }
+            a = V::put(x);
+            c = V::put(y);
+        }
+        T *to;
+        if (is_q) {
+            to = static_cast<T *>(p.q_out) + (((int64_t)l * p.T + t) * p.Hq + h) * D;
+        } else if (!kCache) {
+            to = static_cast<T *>(p.k_out) + (((int64_t)l * p.T + t) * p.Hkv + h) * D;
+        } else {
+            const int64_t cu = ((int64_t)b * p.L + p.layer_begin + l) * p.Hkv + h;
+            const int32_t at = p.start[((int64_t)l * p.B + b) * p.Hkv + h];
+            if (at < 0) continue;  // the unit is skipped
+            const int32_t slot = at + row;
+            const int64_t r = p.cache.pv.table ? paged_row(p.cache.pv, cu, slot) : cu * p.C + slot;
+            if (p.cache.pv.table && (r < 0 || r >= p.cache.pool_rows)) {  // a page that the pool does not have
+                raise_status(p.status, VOXZIP_DEV_CAPACITY);
+                continue;
+            }
+            if (!VOXZIP_IN_RANGE(p.status, slot < p.C && r >= 0 && r < p.cache.pool_rows)) continue;
+            to = static_cast<T *>(is_v ? p.cache.v : p.cache.k) + r * D;
+            if (!is_v && j == 0) {
+                if (p.score) p.score[cu * p.C + slot] = 0.f;
+                if (p.pos) p.pos[cu * p.C + slot] = new_pos;
+            }
+        }
+        reinterpret_cast<uint4 *>(to)[va] = a;
+        reinterpret_cast<uint4 *>(to)[vb] = c;
+    }
+}
+
+struct PlanParams {
+    const int32_t *seq_off;
+    PageView pv;
+    int32_t *len, *start, *status;
+    int32_t B, L, Hkv, C, T, layer_begin, units;
+};
+
+// Takes `want` pages off the free stack, all or none: the stack index of the first, or -1.
+__device__ __forceinline__ int32_t take_pages(const PageView &pv, int32_t want) {
+    int32_t have = *reinterpret_cast<volatile int32_t *>(pv.free_count);
+    while (have >= want) {  // a failed exchange means that another unit took its pages: at most one per unit
+        const int32_t was = atomicCAS(pv.free_count, have, have - want);
+        if (was == have) return have - want;
+        have = was;
+    }
+    return -1;
+}
+
+// A warp per unit: where its rows go (start, -1 where it is skipped), the pages that they need, and its new length.
+__global__ void __launch_bounds__(128) append_plan_kernel(const PlanParams p) {
+    ptx::grid_dependency_wait();
+    ptx::launch_dependents();
+    const int lane = threadIdx.x & 31;
+    const int32_t u = blockIdx.x * 4 + (threadIdx.x >> 5);
+    if (u >= p.units) return;
+    const UnitIdx ui = unit_of(u, p.B, p.L, p.Hkv, p.layer_begin);
+    bool bad = false;
+    for (int32_t base = 0; base < p.B; base += 32) {
+        const int32_t b = base + lane;
+        const int32_t o0 = b < p.B ? p.seq_off[b] : 0, o1 = b < p.B ? p.seq_off[b + 1] : 0;
+        bad |= o0 < 0 || o1 < o0 || o1 > p.T;
+    }
+    bad = __any_sync(0xffffffffu, bad);
+    const int32_t m = bad ? 0 : p.seq_off[ui.b + 1] - p.seq_off[ui.b];
+    const int32_t n = p.len[ui.cache_unit];
+    uint32_t error = bad ? VOXZIP_DEV_BAD_SPANS : 0;
+    if (!bad && (n < 0 || n > p.C || m > p.C - n)) error = VOXZIP_DEV_CAPACITY;
+    if (!error && p.pv.table) {
+        // pages of slots [n, n + m), and of n + m (the next append's), that the unit does not hold
+        int32_t *table = p.pv.table + ui.cache_unit * p.pv.max_pages;
+        const int32_t p0 = n / kPageTokens, p1 = min(p.pv.max_pages, (n + m) / kPageTokens + 1);
+        const int32_t must = m > 0 ? (n + m - 1) / kPageTokens + 1 : p0;  // pages below it are needed now
+        int32_t missing = 0, needed = 0;
+        for (int32_t base = p0; base < p1; base += 32) {
+            const bool none = base + lane < p1 && table[base + lane] < 0;
+            missing += __popc(__ballot_sync(0xffffffffu, none));
+            needed += __popc(__ballot_sync(0xffffffffu, none && base + lane < must));
+        }
+        int32_t at = -1, got = missing;
+        if (lane == 0 && missing > 0) {
+            at = take_pages(p.pv, missing);
+            if (at < 0 && needed < missing) {
+                got = needed;
+                at = needed > 0 ? take_pages(p.pv, needed) : 0;
+            }
+        }
+        at = __shfl_sync(0xffffffffu, at, 0);
+        got = __shfl_sync(0xffffffffu, got, 0);
+        if (missing > 0 && at < 0) {
+            error = VOXZIP_DEV_CAPACITY;
+        } else {
+            int32_t done = 0;  // the highest stack entry first, as take_page does
+            for (int32_t base = p0; base < p1 && done < got; base += 32) {
+                const bool none = base + lane < p1 && table[base + lane] < 0;
+                const unsigned who = __ballot_sync(0xffffffffu, none);
+                const int32_t i = done + __popc(who & ((1u << lane) - 1u));
+                if (none && i < got) table[base + lane] = p.pv.free_pages[at + got - 1 - i];
+                done += __popc(who);
+            }
+        }
+    }
+    if (lane == 0) {
+        if (error) raise_status(p.status, error);
+        p.start[u] = error ? -1 : n;
+        if (!error && m > 0) p.len[ui.cache_unit] = n + m;
+    }
+}
+
+template <typename T>
+cudaError_t launch_rows(const RowsParams &p, bool cache, cudaStream_t stream) {
+    cudaLaunchConfig_t cfg = {};
+    const int64_t warps = (int64_t)p.layer_count * p.T * p.chunks;
+    cfg.gridDim = dim3((unsigned)((warps + kWarps - 1) / kWarps));
+    cfg.blockDim = dim3(32 * kWarps);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (p.D == 128)
+        return cache ? cudaLaunchKernelEx(&cfg, rows_kernel<T, 128, true>, p)
+                     : cudaLaunchKernelEx(&cfg, rows_kernel<T, 128, false>, p);
+    return cache ? cudaLaunchKernelEx(&cfg, rows_kernel<T, 64, true>, p)
+                 : cudaLaunchKernelEx(&cfg, rows_kernel<T, 64, false>, p);
+}
+
+cudaError_t launch_rows(const voxzip_cache_desc &d, RowsParams &p, bool cache, cudaStream_t stream) {
+    p.D = d.head_dim;
+    p.Hq = d.q_heads;
+    p.Hkv = d.kv_heads;
+    // A warp takes all heads of a token, unless there are too few tokens to fill the SMs: then fewer, as long as it
+    // has one round of them (a warp has 32 / (D / 2 / vector) heads in hand at once).
+    const int vec = d.dtype == VOXZIP_BF16 ? 8 : 4;
+    const int round = 32 / (d.head_dim / vec / 2);
+    const int64_t tokens = (int64_t)p.layer_count * p.T;
+    const int64_t want = (int64_t)sm_count() * 16;
+    const int most = (p.heads + round - 1) / round;
+    p.chunks = (int)std::min<int64_t>(most, std::max<int64_t>(1, (want + tokens - 1) / tokens));
+    p.warp_heads = (p.heads + p.chunks - 1) / p.chunks;
+    p.warp_heads = (p.warp_heads + round - 1) / round * round;
+    p.chunks = (p.heads + p.warp_heads - 1) / p.warp_heads;
+    return d.dtype == VOXZIP_BF16 ? launch_rows<__nv_bfloat16>(p, cache, stream) : launch_rows<float>(p, cache, stream);
+}
+
+}  // namespace
+
+cudaError_t launch_rotary(const voxzip_cache_desc &d, const RotaryTable &table, int32_t layer_count, int32_t tokens,
+                          RowsView q, RowsView k, const int32_t *positions, void *q_out, void *k_out,
+                          cudaStream_t stream) {
+    RowsParams p = {};
+    p.rot = table;
+    p.q = q;
+    p.k = k;
+    p.q_out = q_out;
+    p.k_out = k_out;
+    p.positions = positions;
+    p.T = tokens;
+    p.layer_count = layer_count;
+    p.heads = (q.data ? d.q_heads : 0) + (k.data ? d.kv_heads : 0);
+    return launch_rows(d, p, false, stream);
+}
+
+size_t append_workspace_bytes(const voxzip_cache_desc &d, int32_t layer_count) {
+    return ((size_t)d.batch * layer_count * d.kv_heads * sizeof(int32_t) + 255) / 256 * 256;
+}
+
+cudaError_t launch_append(const voxzip_cache_desc &d, const RotaryTable *table, int32_t layer_begin,
+                          int32_t layer_count, RowsView q, RowsView k, RowsView v, const int32_t *positions,
+                          const int32_t *new_pos, const int32_t *seq_off, int32_t tokens, int32_t max_rows,
+                          const CacheRows &cache, float *score, int32_t *pos, int32_t *len, void *q_out,
+                          void *workspace, int32_t *status, cudaStream_t stream) {
+    (void)max_rows;
+    PlanParams pp = {};
+    pp.seq_off = seq_off;
+    pp.pv = cache.pv;
+    pp.len = len;
+    pp.start = static_cast<int32_t *>(workspace);
+    pp.status = status;
+    pp.B = d.batch;
+    pp.L = d.layers;
+    pp.Hkv = d.kv_heads;
+    pp.C = d.capacity;
+    pp.T = tokens;
+    pp.layer_begin = layer_begin;
+    pp.units = d.batch * layer_count * d.kv_heads;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((pp.units + 3) / 4);
+    cfg.blockDim = dim3(128);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    cudaError_t e = cudaLaunchKernelEx(&cfg, append_plan_kernel, pp);
+    if (e != cudaSuccess) return e;
+    RowsParams p = {};
+    if (table) p.rot = *table;
+    p.q = q;
+    p.k = k;
+    p.v = v;
+    p.q_out = q_out;
+    p.positions = positions;
+    p.seq_off = seq_off;
+    p.new_pos = new_pos;
+    p.start = pp.start;
+    p.cache = cache;
+    p.score = score;
+    p.pos = pos;
+    p.status = status;
+    p.T = tokens;
+    p.B = d.batch;
+    p.L = d.layers;
+    p.C = d.capacity;
+    p.layer_begin = layer_begin;
+    p.layer_count = layer_count;
+    p.heads = (q.data ? d.q_heads : 0) + 2 * d.kv_heads;
+    return launch_rows(d, p, true, stream);
+}
+
+}  // namespace voxzip
