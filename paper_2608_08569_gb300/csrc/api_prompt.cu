@@ -130,6 +130,8 @@ voxzip_status attention(const voxzip_cache_desc &d, const CacheRows &cache, int3
     if (!q || !rows_ok(d, q, d.q_heads, tokens, layer_count) || !out || !aligned(out, 16)) return VOXZIP_EINVAL;
     if (d.q_heads / d.kv_heads > voxzip::kMaxGroup) return VOXZIP_EUNSUPPORTED;
     if (!counts_fit(d, layer_count, tokens)) return VOXZIP_EUNSUPPORTED;
+    // a copy of a bf16 tile names its row by 32 bits
+    if (d.dtype == VOXZIP_BF16 && cache.pool_rows > INT32_MAX) return VOXZIP_EUNSUPPORTED;
     const size_t need = voxzip::prompt_plan(d, layer_count, tokens, max_rows, max_len).workspace;
     if (need > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < need)) return VOXZIP_EINVAL;
     int32_t *status = nullptr;

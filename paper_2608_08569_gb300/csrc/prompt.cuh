@@ -113,8 +113,10 @@ __device__ __forceinline__ bool find_tile(const int32_t *seq_off, int32_t B, int
 // CTAs of a launch: every sequence has ceil(m / per) tiles, so all of them at most T / per + B.
 inline int64_t tile_bound(int64_t tokens, int64_t B, int per) { return tokens / per + (B < tokens ? B : tokens); }
 
+cudaError_t launch_prompt_mma(const PromptAttn &p, int D, cudaStream_t stream);
+
 struct PromptPlan {
-    int32_t splits;
+    int32_t splits, tile_tokens;
     size_t workspace;
 };
 PromptPlan prompt_plan(const voxzip_cache_desc &d, int32_t layer_count, int32_t tokens, int32_t max_rows,

@@ -52,9 +52,10 @@ __device__ __forceinline__ void store_row(const PromptAttn &p, int64_t at, int d
 // 256 threads as 16 x 16: thread (ty, tx) has the logits of rows ty + 16 i and keys tx + 16 j, and of the output the
 // same rows' channels 4 tx (and 64 + 4 tx). Fused multiply-adds bound it: per four channels 128 of them meet twelve
 // 16-byte reads of shared memory.
-template <typename T, int D>
+template <int D>
 __global__ void __launch_bounds__(256) prompt_rows_kernel(const PromptAttn p) {
     extern __shared__ __align__(16) uint8_t raw[];
+    using T = float;
     Smem<D> &sm = *reinterpret_cast<Smem<D> *>(raw);
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
     const int h = blockIdx.y % p.Hkv, l = blockIdx.y / p.Hkv, s = blockIdx.z;
@@ -274,37 +275,40 @@ cudaLaunchConfig_t config(dim3 grid, int threads, size_t smem, cudaStream_t stre
     return cfg;
 }
 
-template <typename T, int D>
-cudaError_t launch_rows(const PromptAttn &p, cudaStream_t stream) {
+template <typename T, int D> cudaError_t launch_join(const PromptAttn &p, cudaStream_t stream) {
+    const int64_t rows = (int64_t)p.layer_count * p.T * p.Hq;
+    cudaLaunchAttribute attr[1];
+    cudaLaunchConfig_t cfg = config(dim3((unsigned)((rows + 7) / 8)), 256, 0, stream, attr);
+    return cudaLaunchKernelEx(&cfg, prompt_join_kernel<T, D>, p);
+}
+
+template <int D> cudaError_t launch_rows(const PromptAttn &p, cudaStream_t stream) {
     static std::atomic<uint64_t> done{0};
     cudaError_t e = once_per_device(done, [] {
-        return cudaFuncSetAttribute(prompt_rows_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                    (int)sizeof(Smem<D>));
+        return cudaFuncSetAttribute(prompt_rows_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem<D>));
     });
     if (e != cudaSuccess) return e;
     cudaLaunchAttribute attr[1];
-    const dim3 grid(p.tiles, p.Hkv * p.layer_count, p.splits);
-    cudaLaunchConfig_t cfg = config(grid, 256, sizeof(Smem<D>), stream, attr);
-    e = cudaLaunchKernelEx(&cfg, prompt_rows_kernel<T, D>, p);
-    if (e != cudaSuccess || p.splits == 1) return e;
-    const int64_t rows = (int64_t)p.layer_count * p.T * p.Hq;
-    cfg = config(dim3((unsigned)((rows + 7) / 8)), 256, 0, stream, attr);
-    return cudaLaunchKernelEx(&cfg, prompt_join_kernel<T, D>, p);
+    cudaLaunchConfig_t cfg = config(dim3(p.tiles, p.Hkv * p.layer_count, p.splits), 256, sizeof(Smem<D>), stream, attr);
+    e = cudaLaunchKernelEx(&cfg, prompt_rows_kernel<D>, p);
+    return e != cudaSuccess || p.splits == 1 ? e : launch_join<float, D>(p, stream);
 }
 
 }  // namespace
 
 PromptPlan prompt_plan(const voxzip_cache_desc &d, int32_t layer_count, int32_t tokens, int32_t max_rows,
                        int32_t max_len) {
+    // Rows and keys of a CTA's tiles; a split wants a few tiles of keys to itself.
     const int G = d.q_heads / d.kv_heads;
-    const int per = kRows / G;
+    const bool mma = d.dtype == VOXZIP_BF16;
+    const int keys = mma ? 128 : kKeys, least = mma ? 2 : 4;
+    PromptPlan plan;
+    plan.tile_tokens = mma ? 2 * (128 / G) : kRows / G;
     if (max_rows <= 0 || max_rows > tokens) max_rows = tokens;
     if (max_len <= 0 || max_len > d.capacity) max_len = d.capacity;
-    // CTAs of an even launch, and keys that one walks through; a split wants four tiles of them to itself.
-    const int64_t ctas = std::max<int64_t>(1, (int64_t)tokens / per + (tokens % per != 0)) * d.kv_heads * layer_count;
-    const int64_t key_tiles = (max_len + kKeys - 1) / kKeys;
-    PromptPlan plan;
-    plan.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(kSms / ctas, key_tiles / 4));
+    const int64_t ctas = tile_bound(tokens, d.batch, plan.tile_tokens) * d.kv_heads * layer_count;
+    const int64_t key_tiles = (max_len + keys - 1) / keys;
+    plan.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(kSms / std::max<int64_t>(1, ctas), key_tiles / least));
     const size_t rows = (size_t)layer_count * tokens * d.q_heads;
     plan.workspace = plan.splits == 1 ? 0 : plan.splits * rows * (d.head_dim * sizeof(float) + sizeof(float2));
     plan.workspace = (plan.workspace + 255) / 256 * 256;
@@ -340,11 +344,15 @@ cudaError_t launch_prompt_attention(const voxzip_cache_desc &d, int32_t layer_be
         p.part_o = static_cast<float *>(workspace);
         p.part_ml = reinterpret_cast<float2 *>(p.part_o + rows * d.head_dim);
     }
-    p.tile_tokens = kRows / p.G;
+    p.tile_tokens = plan.tile_tokens;
     p.tiles = (int32_t)tile_bound(tokens, d.batch, p.tile_tokens);
-    if (d.dtype == VOXZIP_BF16)
-        return d.head_dim == 128 ? launch_rows<__nv_bfloat16, 128>(p, stream) : launch_rows<__nv_bfloat16, 64>(p, stream);
-    return d.head_dim == 128 ? launch_rows<float, 128>(p, stream) : launch_rows<float, 64>(p, stream);
+    if (d.dtype == VOXZIP_BF16) {
+        const cudaError_t e = launch_prompt_mma(p, d.head_dim, stream);
+        return e != cudaSuccess || p.splits == 1 ? e
+               : d.head_dim == 128               ? launch_join<__nv_bfloat16, 128>(p, stream)
+                                                 : launch_join<__nv_bfloat16, 64>(p, stream);
+    }
+    return d.head_dim == 128 ? launch_rows<128>(p, stream) : launch_rows<64>(p, stream);
 }
 
 }  // namespace voxzip

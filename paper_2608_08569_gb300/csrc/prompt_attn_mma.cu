@@ -1,0 +1,483 @@
+// Causal attention of a prompt's packed bf16 rows on the tensor cores (the mathematics: prompt_attn.cu).
+//
+// A CTA has 256 rows ((token, head of the group) pairs) of a unit as two tiles of 128, which take turns on the tensor
+// cores: while a warpgroup turns one tile's logits into weights, the other tile's products run.
+//   S_t = Q_t K_j'           128 x 128, fp32, tensor memory
+//   P_t = 2^(c S_t - m - 8)  bf16, over S_t's columns; rounding it costs 2^-8 of each weight, as much as the output's
+//   O_t += P_t V_j           128 x D, fp32, tensor memory
+// m is a row's reference, not its running maximum: it moves (and O_t with it) only when the maximum has grown by more
+// than 2^8 over it, so weights stay at most 1 and nearly every tile leaves O_t to the tensor cores alone.
+// Warps 0-3 and 4-7: a tile's weights, a row per thread. Warp 8: matrix instructions. Warp 9: tile copies into a ring of
+// K and V tiles. Warp 10: what the mask hides of V.
+#include <algorithm>
+
+#include "evict_policy.cuh"  // once_per_device
+#include "prompt.cuh"
+#include "ptx.cuh"
+#include "tcgen05.cuh"
+#include "tmap.cuh"
+
+namespace voxzip {
+namespace {
+
+constexpr int kTile = 128;       // rows of a tile, keys of a tile
+constexpr int kThreads = 11 * 32;
+constexpr uint32_t kPolls = 1u << 20;
+constexpr float kSlack = 8.f;    // growth of a row's maximum that its reference lets pass (log2)
+
+template <int D> struct Cfg {
+    static constexpr int kHalves = D / 64;                    // copies of 64 channels
+    static constexpr int kHalfBytes = kTile * 128;            // one of them
+    static constexpr int kTileBytes = kHalves * kHalfBytes;   // a Q, K or V tile
+    static constexpr int kStages = D == 128 ? 5 : 6;
+    static constexpr int kBytes = 2 * kTileBytes + kStages * kTileBytes;
+    static constexpr uint32_t kColO = 256;                    // S_0, S_1: columns 0 and 128
+    static constexpr uint32_t kColumns = 512;
+};
+
+template <int D> struct Shared {
+    uint64_t q_full, full[Cfg<D>::kStages], empty[Cfg<D>::kStages], s_full[2], p_full[2], o_full[2], sent[4], clean[4], drained;
+    TileAt at;
+    uint32_t tmem;
+    int ok, dead, dirty;
+};
+
+template <int D> constexpr size_t smem_bytes() { return 1024 + Cfg<D>::kBytes + sizeof(Shared<D>); }
+
+// A bounded wait; once one has given up in a CTA, all do.
+template <int D> __device__ __forceinline__ bool wait(Shared<D> &sh, uint64_t *bar, uint32_t parity) {
+    for (uint32_t i = 0; i < kPolls; ++i) {
+        if (ptx::mbar_try_wait(bar, parity)) return true;
+        if (*reinterpret_cast<volatile int *>(&sh.dead)) return false;
+    }
+    *reinterpret_cast<volatile int *>(&sh.dead) = 1;
+    return false;
+}
+
+// The same by all lanes of a warp, which stay together whatever each of them saw.
+template <int D> __device__ __forceinline__ bool wait_warp(Shared<D> &sh, uint64_t *bar, uint32_t parity) {
+    return __all_sync(0xffffffffu, wait(sh, bar, parity));
+}
+
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+__device__ __forceinline__ void tma_load_4d(void *dst, const CUtensorMap *map, int x, int y, int z, int w, uint64_t *bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+        ::"r"(ptx::smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(ptx::smem_u32(bar))
+        : "memory");
+}
+
+// What a CTA works on.
+struct Work {
+    int32_t first;       // keys that its first token sees (may be < 1)
+    int32_t most;        // keys that its last one sees
+    int32_t j0, end[2];  // key tiles [j0, end[t]) of row tile t
+    int64_t cu;          // cache unit
+};
+
+template <int D, bool kPaged>
+__global__ void __launch_bounds__(kThreads, 1)
+prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                  const __grid_constant__ CUtensorMap map_v, const __grid_constant__ PromptAttn p) {
+    using C = Cfg<D>;
+    extern __shared__ uint8_t raw[];
+    uint8_t *tiles = raw + (1024 - (ptx::smem_u32(raw) & 1023)) % 1024;
+    Shared<D> &sh = *reinterpret_cast<Shared<D> *>(tiles + C::kBytes);
+    uint8_t *q_smem = tiles, *ring = tiles + 2 * C::kTileBytes;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int h = blockIdx.y % p.Hkv, l = blockIdx.y / p.Hkv, split = blockIdx.z;
+
+    if (threadIdx.x == 0) {
+        ptx::mbar_init(&sh.q_full, 1);
+        for (int i = 0; i < C::kStages; ++i) ptx::mbar_init(&sh.full[i], 1), ptx::mbar_init(&sh.empty[i], 1);
+        for (int t = 0; t < 2; ++t)
+            ptx::mbar_init(&sh.s_full[t], 1), ptx::mbar_init(&sh.p_full[t], 4), ptx::mbar_init(&sh.o_full[t], 1);
+        for (int i = 0; i < 4; ++i) ptx::mbar_init(&sh.sent[i], 1), ptx::mbar_init(&sh.clean[i], 1);
+        ptx::mbar_init(&sh.drained, 1);
+        ptx::fence_mbar_init();
+        sh.dead = 0;
+        sh.dirty = 0;
+    }
+    if (warp == 8) tc::alloc(&sh.tmem, C::kColumns);
+    if (warp == 9 && lane == 0) {
+        ptx::prefetch_tmap(&map_q);
+        ptx::prefetch_tmap(&map_k);
+        ptx::prefetch_tmap(&map_v);
+    }
+    ptx::grid_dependency_wait();
+    if (warp == 0) {
+        TileAt at;
+        const bool found = find_tile(p.seq_off, p.B, p.T, p.tile_tokens, blockIdx.x, p.status, at);
+        if (lane == 0) {
+            sh.ok = found;
+            if (found) sh.at = at;
+        }
+    }
+    tc::fence_before();
+    __syncthreads();
+    tc::fence_after();
+    const uint32_t tmem = sh.tmem;
+    bool ok = sh.ok;
+    const TileAt at = sh.at;
+    Work w = {};
+    const int tile_tokens = kTile / p.G;
+    if (ok) {
+        w.cu = ((int64_t)at.b * p.L + p.layer_begin + l) * p.Hkv + h;
+        const int32_t n = p.len[w.cu];
+        if (n < 0 || n > p.C) {
+            if (threadIdx.x == 0) raise_status(p.status, VOXZIP_DEV_CAPACITY);
+            ok = false;
+        } else {
+            w.first = n - at.m + at.before + 1;
+            w.most = max(0, w.first + at.rows - 1);
+            // the keys of this split, of those that the CTA's last token sees; row tile 0 ends with its own last token's
+            const int32_t total = (w.most + kTile - 1) / kTile, per = (total + p.splits - 1) / p.splits;
+            w.j0 = min(total, split * per);
+            const int32_t j1 = min(total, w.j0 + per);
+            const int32_t most0 = max(0, w.first + min(tile_tokens, at.rows) - 1);
+            w.end[0] = max(w.j0, min(j1, (most0 + kTile - 1) / kTile));
+            w.end[1] = at.rows > tile_tokens ? j1 : w.j0;
+        }
+    }
+    const int32_t end = max(w.end[0], w.end[1]);
+    const int32_t masked0 = max(0, w.first) / kTile;  // from this key tile on some row does not see all keys
+
+    if (!ok) {
+        // nothing to do
+    } else if (warp == 9) {
+        // ------------------------------------------------------------ copies
+        bool live = true;
+        int issued = 0;
+        if (lane == 0 && end > w.j0) {
+            const uint32_t bytes = p.G * tile_tokens * 128 * C::kHalves;
+            const int both = at.rows > tile_tokens ? 2 : 1;
+            ptx::mbar_arrive_expect_tx(&sh.q_full, bytes * both);
+            for (int t = 0; t < both; ++t)
+                for (int c = 0; c < C::kHalves; ++c)
+                    tma_load_4d(q_smem + t * C::kTileBytes + c * C::kHalfBytes, &map_q, 64 * c, h * p.G,
+                                at.t0 + t * tile_tokens, l, &sh.q_full);
+        }
+        int32_t pages = 0, pages_at = INT32_MIN;  // this lane's of 32 consecutive page indices
+        for (int32_t j = w.j0; j < end && live; ++j) {
+            int32_t row[2];
+            if constexpr (kPaged) {
+                constexpr int kPages = kTile / kPageTokens;
+                const int32_t first_page = j * kPages;
+                if (first_page >= pages_at + 32 || pages_at == INT32_MIN) {
+                    pages_at = first_page;
+                    const int32_t at_page = first_page + lane;
+                    pages = -1;
+                    if (at_page * kPageTokens < w.most) {
+                        pages = p.cache.pv.table[w.cu * p.cache.pv.max_pages + at_page];
+                        if (pages < 0 || (int64_t)pages * kPageTokens >= p.cache.pool_rows) {
+                            raise_status(p.status, VOXZIP_DEV_CAPACITY);
+                            pages = -1;
+                        }
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < kPages; ++i) {
+                    const int32_t page = __shfl_sync(0xffffffffu, pages, first_page - pages_at + i);
+                    row[i] = page < 0 ? (int32_t)p.cache.pool_rows : page * kPageTokens;  // outside: zeros
+                }
+            } else {
+                row[0] = (int32_t)(w.cu * p.C + (int64_t)j * kTile);
+                row[1] = row[0] + kTile / 2;
+                (void)VOXZIP_IN_RANGE(p.status, row[0] >= 0 && row[0] < p.kv_rows);
+            }
+            if (lane == 0) {
+                for (int kv = 0; kv < 2 && live; ++kv) {
+                    const int slot = issued % C::kStages;
+                    live = issued < C::kStages || wait(sh, &sh.empty[slot], (issued / C::kStages & 1) ^ 1);
+                    if (!live) break;
+                    const CUtensorMap *map = kv ? &map_v : &map_k;
+                    uint8_t *to = ring + slot * C::kTileBytes;
+                    ptx::mbar_arrive_expect_tx(&sh.full[slot], C::kTileBytes);
+                    for (int c = 0; c < C::kHalves; ++c) {
+                        ptx::tma_load_2d(to + c * C::kHalfBytes, map, 64 * c, row[0], &sh.full[slot]);
+                        if (kPaged)
+                            ptx::tma_load_2d(to + c * C::kHalfBytes + C::kHalfBytes / 2, map, 64 * c, row[1], &sh.full[slot]);
+                    }
+                    ++issued;
+                    if (kv && j >= masked0) ptx::mbar_arrive(&sh.sent[j - max(w.j0, masked0)]);
+                }
+            }
+            live = __shfl_sync(0xffffffffu, live, 0);
+        }
+        if (lane == 0 && !live)  // a wait gave up: no copy is left in flight behind this CTA
+            for (int i = max(0, issued - C::kStages); i < issued; ++i)
+                ptx::mbar_wait_bounded(&sh.full[i % C::kStages], i / C::kStages & 1, kPolls);
+    } else if (warp == 8) {
+        // ------------------------------------------------------------ matrix instructions
+        if (lane == 0 && end > w.j0) {
+            constexpr uint32_t kInstS = tc::instruction(kTile, false), kInstO = tc::instruction(D, true);
+            int used = 0;  // tiles of the ring
+            bool live = wait(sh, &sh.q_full, 0);
+            const uint32_t q_at = ptx::smem_u32(q_smem), ring_at = ptx::smem_u32(ring);
+            auto logits = [&](int t, int slot) {
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k) {
+                    const uint32_t off = k / 4 * C::kHalfBytes + k % 4 * 32;
+                    tc::mma(tmem + t * kTile, tc::operand(q_at + t * C::kTileBytes + off, 0),
+                            tc::operand(ring_at + slot * C::kTileBytes + off, 0), kInstS, k > 0);
+                }
+                tc::commit(&sh.s_full[t]);
+            };
+            if (live && (live = wait(sh, &sh.full[0], 0))) {
+                tc::fence_after();
+                for (int t = 0; t < 2; ++t)
+                    if (w.j0 < w.end[t]) logits(t, 0);
+                tc::commit(&sh.empty[0]);
+                used = 1;
+            }
+            for (int32_t j = w.j0; j < end && live; ++j) {
+                const int v_slot = used % C::kStages, v_phase = used / C::kStages & 1;
+                const int k_slot = (used + 1) % C::kStages, k_phase = (used + 1) / C::kStages & 1;
+                const bool next = j + 1 < end;
+                live = wait(sh, &sh.full[v_slot], v_phase);
+                if (live && j >= masked0) live = wait(sh, &sh.clean[j - max(w.j0, masked0)], 0);
+                if (live && next) live = wait(sh, &sh.full[k_slot], k_phase);
+                if (!live) break;
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    if (j < w.end[t]) {
+                        live = live && wait(sh, &sh.p_full[t], (j - w.j0) & 1);
+                        if (!live) break;
+                        tc::fence_after();
+#pragma unroll
+                        for (int k = 0; k < kTile / 16; ++k)
+                            tc::mma_ta(tmem + C::kColO + t * D, tmem + t * kTile + k * 8,
+                                       tc::operand(ring_at + v_slot * C::kTileBytes + k * 16 * 128, C::kHalfBytes), kInstO,
+                                       j > w.j0 || k > 0);
+                        if (j + 1 == w.end[t]) tc::commit(&sh.o_full[t]);
+                    }
+                    if (t == 1) tc::commit(&sh.empty[v_slot]);
+                    if (j + 1 < w.end[t]) logits(t, k_slot);
+                }
+                if (live && next) tc::commit(&sh.empty[k_slot]);
+                used += 2;
+            }
+            if (!live) {  // a wait gave up: what was issued ends before the tensor memory goes
+                tc::commit(&sh.drained);
+                ptx::mbar_wait_bounded(&sh.drained, 0, kPolls);
+                raise_status(p.status, VOXZIP_DEV_TIMEOUT);
+            }
+        }
+    } else if (warp == 10) {
+        // ------------------------------------------------------------ V behind the mask
+        // A weight of 0 times an infinity or a NaN would be NaN in rows that do not see the key. Rows that nobody sees
+        // become 0. In rows that some see such elements do, and join the result at the end.
+        for (int32_t j = max(w.j0, masked0); j < end; ++j) {
+            const int i = 2 * (j - w.j0) + 1, slot = i % C::kStages;
+            // only once its copy is asked for is a phase of the slot's barrier this tile's
+            if (!wait_warp(sh, &sh.sent[j - max(w.j0, masked0)], 0)) break;
+            if (!wait_warp(sh, &sh.full[slot], i / C::kStages & 1)) break;
+            uint8_t *tile = ring + slot * C::kTileBytes;
+            const int32_t key0 = j * kTile;
+            const int r0 = max(0, w.first - key0), r1 = min(kTile, max(0, w.most - key0));
+            bool found = false;
+            for (int i = r0 * 8 + lane; i < kTile * 8; i += 32) {
+#pragma unroll
+                for (int c = 0; c < C::kHalves; ++c) {
+                    uint4 *at16 = reinterpret_cast<uint4 *>(tile + c * C::kHalfBytes) + i;
+                    if (i >= r1 * 8) {
+                        *at16 = make_uint4(0, 0, 0, 0);
+                        continue;
+                    }
+                    uint4 u = *at16;
+                    uint32_t *x = &u.x;
+                    bool bad = false;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if ((x[e] & 0x7f80u) == 0x7f80u) x[e] &= 0xffff0000u, bad = true;
+                        if ((x[e] & 0x7f800000u) == 0x7f800000u) x[e] &= 0x0000ffffu, bad = true;
+                    }
+                    if (bad) *at16 = u;
+                    found |= bad;
+                }
+            }
+            if (__any_sync(0xffffffffu, found) && lane == 0) *reinterpret_cast<volatile int *>(&sh.dirty) = 1;
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(&sh.clean[j - max(w.j0, masked0)]);
+        }
+    } else {
+        // ------------------------------------------------------------ weights, a row per thread
+        const int t = warp >> 2, r = threadIdx.x & (kTile - 1);
+        const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // this warp's 32 lanes
+        const uint32_t s_at = tmem + lanes + t * kTile, o_at = tmem + lanes + C::kColO + t * D;
+        const int32_t token = t * tile_tokens + r / p.G;
+        const int32_t lim = w.first + token;  // keys that the row sees
+        float m = -INFINITY, sum = 0.f;
+        bool live = true;
+        for (int32_t j = w.j0; j < w.end[t]; ++j) {
+            const uint32_t phase = (j - w.j0) & 1;
+            if (!(live = wait_warp(sh, &sh.s_full[t], phase))) break;
+            tc::fence_after();
+            float x[4][32];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) tc::ld32(s_at + 32 * c, x[c]);
+            tc::wait_ld();
+            if (j >= masked0) {
+                const int32_t seen = lim - j * kTile;
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        if (32 * c + i >= seen) x[c][i] = -INFINITY;
+            }
+            float top = -INFINITY;
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                for (int i = 0; i < 32; ++i) top = fmaxf(top, x[c][i]);
+            top *= p.scale_log2;
+            const bool grown = top > m + kSlack;
+            if (__any_sync(0xffffffffu, grown)) {
+                const float keep = grown ? ex2(m - top) : 1.f;  // a row does not depend on its neighbours
+                if (grown) m = top;
+                sum *= keep;
+                if (j > w.j0) {  // the products of the tiles before are done: the logits' commit came after theirs
+                    float o[32];
+#pragma unroll
+                    for (int c = 0; c < D / 32; ++c) {
+                        tc::ld32(o_at + 32 * c, o);
+                        tc::wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) o[i] *= keep;
+                        tc::st32(o_at + 32 * c, reinterpret_cast<uint32_t(&)[32]>(o));
+                    }
+                }
+            }
+            const float ref = m == -INFINITY ? 0.f : -m - kSlack;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                uint32_t u[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float a = ex2(fmaf(x[c][2 * i], p.scale_log2, ref));
+                    const float b = ex2(fmaf(x[c][2 * i + 1], p.scale_log2, ref));
+                    sum += a + b;
+                    u[i] = ptx::pack_bf16(a, b);
+                }
+                tc::st16(s_at + 16 * c, u);
+            }
+            tc::wait_st();
+            tc::fence_before();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(&sh.p_full[t]);
+        }
+        // ------------------------------------------------------------ results
+        const bool any = w.end[t] > w.j0;
+        if (live && any) live = wait_warp(sh, &sh.o_full[t], 0);
+        tc::fence_after();
+        const bool mine = live && token < at.rows && r < tile_tokens * p.G;
+        const int64_t row = ((int64_t)l * p.T + at.t0 + token) * p.Hq + h * p.G + r % p.G;
+        const bool none = !any || lim <= 0;
+        const float inv = none ? 0.f : 1.f / sum;
+        const bool dirty = *reinterpret_cast<volatile int *>(&sh.dirty);
+        const int64_t all = (int64_t)p.layer_count * p.T * p.Hq;
+        if (mine && p.splits > 1)
+            p.part_ml[split * all + row] = make_float2(!any || m == -INFINITY ? -INFINITY : m + kSlack, any ? sum : 0.f);
+        if (live && any) {
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c) {
+                float o[32];
+                tc::ld32(o_at + 32 * c, o);
+                tc::wait_ld();
+                if (!mine) continue;
+                if (p.splits == 1)
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) o[i] = none ? 0.f : o[i] * inv;
+                if (dirty) {  // the elements of V that warp 10 took out, for the rows that see them
+                    const int32_t k0 = max(max(0, w.first), w.j0 * kTile), k1 = min(lim, w.end[t] * kTile);
+                    for (int32_t key = k0; key < k1; ++key) {
+                        const int64_t at_row = kPaged ? paged_row(p.cache.pv, w.cu, key) : w.cu * p.C + key;
+                        if (at_row < 0 || at_row >= p.kv_rows) continue;
+                        const __nv_bfloat16 *v = static_cast<const __nv_bfloat16 *>(p.cache.v) + at_row * D + 32 * c;
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) {
+                            const float e = __bfloat162float(v[i]);
+                            if (!isfinite(e)) o[i] += e;
+                        }
+                    }
+                }
+                if (p.splits > 1) {
+                    float4 *to = reinterpret_cast<float4 *>(p.part_o + (split * all + row) * D + 32 * c);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) to[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                } else {
+                    uint4 *to = reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) + row * D + 32 * c);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        to[i] = make_uint4(ptx::pack_bf16(o[8 * i], o[8 * i + 1]), ptx::pack_bf16(o[8 * i + 2], o[8 * i + 3]),
+                                           ptx::pack_bf16(o[8 * i + 4], o[8 * i + 5]), ptx::pack_bf16(o[8 * i + 6], o[8 * i + 7]));
+                }
+            }
+        } else if (mine && p.splits == 1) {
+            uint4 *to = reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) + row * D);
+            for (int i = 0; i < D / 8; ++i) to[i] = make_uint4(0, 0, 0, 0);
+        }
+    }
+    tc::fence_before();
+    __syncthreads();
+    tc::fence_after();
+    __syncwarp();
+    if (warp == 8) tc::dealloc(tmem, C::kColumns);
+}
+
+bool encode(CUtensorMap *map, const void *base, int rank, const cuuint64_t *dims, const cuuint64_t *strides,
+            const cuuint32_t *box) {
+    auto enc = tensor_map_encoder();
+    const cuuint32_t ones[4] = {1, 1, 1, 1};
+    return enc && enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void *>(base), dims, strides, box, ones,
+                      CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D, bool kPaged> cudaError_t launch(const PromptAttn &p, cudaStream_t stream) {
+    static std::atomic<uint64_t> done{0};
+    cudaError_t e = once_per_device(done, [] {
+        return cudaFuncSetAttribute(prompt_mma_kernel<D, kPaged>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                    (int)smem_bytes<D>());
+    });
+    if (e != cudaSuccess) return e;
+    CUtensorMap mq, mk, mv;
+    // a stride that no second token or layer uses may be anything: the map gets a valid one
+    const int64_t ts = p.T > 1 ? p.q.token_stride : (int64_t)p.Hq * D;
+    const int64_t ls = p.layer_count > 1 ? p.q.layer_stride : ts * p.T;
+    const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)p.Hq, (cuuint64_t)p.T, (cuuint64_t)p.layer_count};
+    const cuuint64_t strides[3] = {(cuuint64_t)D * 2, (cuuint64_t)ts * 2, (cuuint64_t)ls * 2};
+    const cuuint32_t box[4] = {64, (cuuint32_t)p.G, (cuuint32_t)(kTile / p.G), 1};
+    if (!encode(&mq, p.q.data, 4, dims, strides, box)) return cudaErrorInvalidValue;
+    const int rows = kPaged ? kPageTokens : kTile;
+    if (!make_cache_map(&mk, p.cache.k, p.cache.pool_rows, D, rows) ||
+        !make_cache_map(&mv, p.cache.v, p.cache.pool_rows, D, rows))
+        return cudaErrorInvalidValue;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(p.tiles, p.Hkv * p.layer_count, p.splits);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem_bytes<D>();
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, prompt_mma_kernel<D, kPaged>, mq, mk, mv, p);
+}
+
+}  // namespace
+
+cudaError_t launch_prompt_mma(const PromptAttn &p, int D, cudaStream_t stream) {
+    const bool paged = p.cache.pv.table != nullptr;
+    if (D == 128) return paged ? launch<128, true>(p, stream) : launch<128, false>(p, stream);
+    return paged ? launch<64, true>(p, stream) : launch<64, false>(p, stream);
+}
+
+}  // namespace voxzip
