@@ -7,8 +7,9 @@
 //   O_t += P_t V_j           128 x D, fp32, tensor memory
 // m is a row's reference, not its running maximum: it moves (and O_t with it) only when the maximum has grown by more
 // than 2^8 over it, so weights stay at most 1 and nearly every tile leaves O_t to the tensor cores alone.
-// Warps 0-3 and 4-7: a tile's weights, a row per thread. Warp 8: matrix instructions. Warp 9: tile copies into a ring of
-// K and V tiles. Warp 10: what the mask hides of V.
+// Warps 0-3 and 4-7: a tile's weights, a row per thread. Warps 8 and 11: a tile's matrix instructions (one thread for
+// both would wait for one tile's weights while the other's lie ready). Warp 9: tile copies into a ring of K and V tiles.
+// Warp 10: what the mask hides of V.
 #include <algorithm>
 
 #include "evict_policy.cuh"  // once_per_device
@@ -21,8 +22,8 @@ namespace voxzip {
 namespace {
 
 constexpr int kTile = 128;       // rows of a tile, keys of a tile
-constexpr int kThreads = 11 * 32;
-constexpr uint32_t kPolls = 1u << 20;
+constexpr int kThreads = 12 * 32;
+constexpr uint32_t kPolls = 1u << 15, kSuspendNs = 100000;  // of a wait: three seconds at most
 constexpr float kSlack = 8.f;    // growth of a row's maximum that its reference lets pass (log2)
 
 template <int D> struct Cfg {
@@ -36,7 +37,7 @@ template <int D> struct Cfg {
 };
 
 template <int D> struct Shared {
-    uint64_t q_full, full[Cfg<D>::kStages], empty[Cfg<D>::kStages], s_full[2], p_full[2], o_full[2], sent[4], clean[4], drained;
+    uint64_t q_full, full[Cfg<D>::kStages], empty[Cfg<D>::kStages], s_full[2], p_full[2][2], o_full[2], sent[4], clean[4], drained[2];
     TileAt at;
     uint32_t tmem;
     int ok, dead, dirty;
@@ -47,7 +48,7 @@ template <int D> constexpr size_t smem_bytes() { return 1024 + Cfg<D>::kBytes + 
 // A bounded wait; once one has given up in a CTA, all do.
 template <int D> __device__ __forceinline__ bool wait(Shared<D> &sh, uint64_t *bar, uint32_t parity) {
     for (uint32_t i = 0; i < kPolls; ++i) {
-        if (ptx::mbar_try_wait(bar, parity)) return true;
+        if (ptx::mbar_try_wait_for(bar, parity, kSuspendNs)) return true;
         if (*reinterpret_cast<volatile int *>(&sh.dead)) return false;
     }
     *reinterpret_cast<volatile int *>(&sh.dead) = 1;
@@ -65,6 +66,27 @@ __device__ __forceinline__ float ex2(float x) {
     return y;
 }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float y;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+    return y;
+}
+// (a0, a1) b + c and (a0, a1) + (b0, b1), two at a time.
+__device__ __forceinline__ float2 fma2(float a0, float a1, float b, float c) {
+    float2 y;
+    asm("{\n\t.reg .b64 u, v, w;\n\tmov.b64 u, {%2, %3};\n\tmov.b64 v, {%4, %4};\n\tmov.b64 w, {%5, %5};\n\t"
+        "fma.rn.f32x2 u, u, v, w;\n\tmov.b64 {%0, %1}, u;\n\t}"
+        : "=f"(y.x), "=f"(y.y)
+        : "f"(a0), "f"(a1), "f"(b), "f"(c));
+    return y;
+}
+__device__ __forceinline__ void add2(float2 &a, float b0, float b1) {
+    asm("{\n\t.reg .b64 u, v;\n\tmov.b64 u, {%0, %1};\n\tmov.b64 v, {%2, %3};\n\tadd.rn.f32x2 u, u, v;\n\t"
+        "mov.b64 {%0, %1}, u;\n\t}"
+        : "+f"(a.x), "+f"(a.y)
+        : "f"(b0), "f"(b1));
+}
+
 __device__ __forceinline__ void tma_load_4d(void *dst, const CUtensorMap *map, int x, int y, int z, int w, uint64_t *bar) {
     asm volatile(
         "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
@@ -76,7 +98,7 @@ __device__ __forceinline__ void tma_load_4d(void *dst, const CUtensorMap *map, i
 struct Work {
     int32_t first;       // keys that its first token sees (may be < 1)
     int32_t most;        // keys that its last one sees
-    int32_t j0, end[2];  // key tiles [j0, end[t]) of row tile t
+    int32_t j0, end0, end1;  // key tiles [j0, end0) and [j0, end1) of the two row tiles
     int64_t cu;          // cache unit
 };
 
@@ -94,11 +116,11 @@ prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
 
     if (threadIdx.x == 0) {
         ptx::mbar_init(&sh.q_full, 1);
-        for (int i = 0; i < C::kStages; ++i) ptx::mbar_init(&sh.full[i], 1), ptx::mbar_init(&sh.empty[i], 1);
+        for (int i = 0; i < C::kStages; ++i) ptx::mbar_init(&sh.full[i], 1), ptx::mbar_init(&sh.empty[i], 2);
         for (int t = 0; t < 2; ++t)
-            ptx::mbar_init(&sh.s_full[t], 1), ptx::mbar_init(&sh.p_full[t], 4), ptx::mbar_init(&sh.o_full[t], 1);
+            ptx::mbar_init(&sh.s_full[t], 1), ptx::mbar_init(&sh.p_full[t][0], 4), ptx::mbar_init(&sh.p_full[t][1], 4), ptx::mbar_init(&sh.o_full[t], 1);
         for (int i = 0; i < 4; ++i) ptx::mbar_init(&sh.sent[i], 1), ptx::mbar_init(&sh.clean[i], 1);
-        ptx::mbar_init(&sh.drained, 1);
+        ptx::mbar_init(&sh.drained[0], 1), ptx::mbar_init(&sh.drained[1], 1);
         ptx::fence_mbar_init();
         sh.dead = 0;
         sh.dirty = 0;
@@ -140,11 +162,11 @@ prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
             w.j0 = min(total, split * per);
             const int32_t j1 = min(total, w.j0 + per);
             const int32_t most0 = max(0, w.first + min(tile_tokens, at.rows) - 1);
-            w.end[0] = max(w.j0, min(j1, (most0 + kTile - 1) / kTile));
-            w.end[1] = at.rows > tile_tokens ? j1 : w.j0;
+            w.end0 = max(w.j0, min(j1, (most0 + kTile - 1) / kTile));
+            w.end1 = at.rows > tile_tokens ? j1 : w.j0;
         }
     }
-    const int32_t end = max(w.end[0], w.end[1]);
+    const int32_t end = max(w.end0, w.end1);
     const int32_t masked0 = max(0, w.first) / kTile;  // from this key tile on some row does not see all keys
 
     if (!ok) {
@@ -212,59 +234,65 @@ prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         if (lane == 0 && !live)  // a wait gave up: no copy is left in flight behind this CTA
             for (int i = max(0, issued - C::kStages); i < issued; ++i)
                 ptx::mbar_wait_bounded(&sh.full[i % C::kStages], i / C::kStages & 1, kPolls);
-    } else if (warp == 8) {
-        // ------------------------------------------------------------ matrix instructions
+    } else if (warp == 8 || warp == 11) {
+        // ------------------------------------------------------------ matrix instructions, a thread per row tile
+        const int t = warp == 11;
+        const int32_t t_end = t ? w.end1 : w.end0;
         if (lane == 0 && end > w.j0) {
             constexpr uint32_t kInstS = tc::instruction(kTile, false), kInstO = tc::instruction(D, true);
-            int used = 0;  // tiles of the ring
+            const uint32_t q_at = ptx::smem_u32(q_smem) + t * C::kTileBytes, ring_at = ptx::smem_u32(ring);
+            const uint32_t s_at = tmem + t * kTile, o_at = tmem + C::kColO + t * D;
             bool live = wait(sh, &sh.q_full, 0);
-            const uint32_t q_at = ptx::smem_u32(q_smem), ring_at = ptx::smem_u32(ring);
-            auto logits = [&](int t, int slot) {
-#pragma unroll
-                for (int k = 0; k < D / 16; ++k) {
-                    const uint32_t off = k / 4 * C::kHalfBytes + k % 4 * 32;
-                    tc::mma(tmem + t * kTile, tc::operand(q_at + t * C::kTileBytes + off, 0),
-                            tc::operand(ring_at + slot * C::kTileBytes + off, 0), kInstS, k > 0);
-                }
-                tc::commit(&sh.s_full[t]);
+            int slot = 0, phase = 0;  // of the ring's next tile
+            auto next = [&] {
+                if (++slot == C::kStages) slot = 0, phase ^= 1;
             };
-            if (live && (live = wait(sh, &sh.full[0], 0))) {
-                tc::fence_after();
-                for (int t = 0; t < 2; ++t)
-                    if (w.j0 < w.end[t]) logits(t, 0);
-                tc::commit(&sh.empty[0]);
-                used = 1;
-            }
-            for (int32_t j = w.j0; j < end && live; ++j) {
-                const int v_slot = used % C::kStages, v_phase = used / C::kStages & 1;
-                const int k_slot = (used + 1) % C::kStages, k_phase = (used + 1) / C::kStages & 1;
-                const bool next = j + 1 < end;
-                live = wait(sh, &sh.full[v_slot], v_phase);
-                if (live && j >= masked0) live = wait(sh, &sh.clean[j - max(w.j0, masked0)], 0);
-                if (live && next) live = wait(sh, &sh.full[k_slot], k_phase);
-                if (!live) break;
+            // The logits of key tile j, once it is there. A tile of the ring that this thread has no use for is given
+            // back only when it has come: before that, the barrier's phase is that of its last use.
+            auto logits = [&](int32_t j) {
+                if (!(live = live && wait(sh, &sh.full[slot], phase))) return;
+                if (j < t_end) {
+                    tc::fence_after();
+                    const uint32_t k_at = ring_at + slot * C::kTileBytes;
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    if (j < w.end[t]) {
-                        live = live && wait(sh, &sh.p_full[t], (j - w.j0) & 1);
-                        if (!live) break;
+                    for (int k = 0; k < D / 16; ++k) {
+                        const uint32_t off = k / 4 * C::kHalfBytes + k % 4 * 32;
+                        tc::mma(s_at, tc::operand(q_at + off, 0), tc::operand(k_at + off, 0), kInstS, k > 0);
+                    }
+                    tc::commit(&sh.s_full[t]);
+                    tc::commit(&sh.empty[slot]);
+                } else {
+                    ptx::mbar_arrive(&sh.empty[slot]);
+                }
+                next();
+            };
+            logits(w.j0);
+            for (int32_t j = w.j0; j < end && live; ++j) {
+                live = wait(sh, &sh.full[slot], phase);
+                if (live && j >= masked0) live = wait(sh, &sh.clean[j - max(w.j0, masked0)], 0);
+                if (live && j < t_end) {
+                    const uint32_t v_at = ring_at + slot * C::kTileBytes;
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {  // of the keys, as their weights come
+                        if (!(live = live && wait(sh, &sh.p_full[t][half], (j - w.j0) & 1))) break;
                         tc::fence_after();
 #pragma unroll
-                        for (int k = 0; k < kTile / 16; ++k)
-                            tc::mma_ta(tmem + C::kColO + t * D, tmem + t * kTile + k * 8,
-                                       tc::operand(ring_at + v_slot * C::kTileBytes + k * 16 * 128, C::kHalfBytes), kInstO,
+                        for (int k = 4 * half; k < 4 * half + 4; ++k)
+                            tc::mma_ta(o_at, s_at + k * 8, tc::operand(v_at + k * 16 * 128, C::kHalfBytes), kInstO,
                                        j > w.j0 || k > 0);
-                        if (j + 1 == w.end[t]) tc::commit(&sh.o_full[t]);
                     }
-                    if (t == 1) tc::commit(&sh.empty[v_slot]);
-                    if (j + 1 < w.end[t]) logits(t, k_slot);
+                    if (!live) break;
+                    if (j + 1 == t_end) tc::commit(&sh.o_full[t]);
+                    tc::commit(&sh.empty[slot]);
+                } else if (live) {
+                    ptx::mbar_arrive(&sh.empty[slot]);
                 }
-                if (live && next) tc::commit(&sh.empty[k_slot]);
-                used += 2;
+                next();
+                if (live && j + 1 < end) logits(j + 1);
             }
             if (!live) {  // a wait gave up: what was issued ends before the tensor memory goes
-                tc::commit(&sh.drained);
-                ptx::mbar_wait_bounded(&sh.drained, 0, kPolls);
+                tc::commit(&sh.drained[t]);
+                ptx::mbar_wait_bounded(&sh.drained[t], 0, kPolls);
                 raise_status(p.status, VOXZIP_DEV_TIMEOUT);
             }
         }
@@ -313,9 +341,10 @@ prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         const uint32_t s_at = tmem + lanes + t * kTile, o_at = tmem + lanes + C::kColO + t * D;
         const int32_t token = t * tile_tokens + r / p.G;
         const int32_t lim = w.first + token;  // keys that the row sees
+        const int32_t t_end = t ? w.end1 : w.end0;
         float m = -INFINITY, sum = 0.f;
         bool live = true;
-        for (int32_t j = w.j0; j < w.end[t]; ++j) {
+        for (int32_t j = w.j0; j < t_end; ++j) {
             const uint32_t phase = (j - w.j0) & 1;
             if (!(live = wait_warp(sh, &sh.s_full[t], phase))) break;
             tc::fence_after();
@@ -331,49 +360,55 @@ prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     for (int i = 0; i < 32; ++i)
                         if (32 * c + i >= seen) x[c][i] = -INFINITY;
             }
-            float top = -INFINITY;
+            float tops[4];
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
+            for (int c = 0; c < 4; ++c) {
+                tops[c] = fmaxf(x[c][0], x[c][1]);
 #pragma unroll
-                for (int i = 0; i < 32; ++i) top = fmaxf(top, x[c][i]);
-            top *= p.scale_log2;
+                for (int i = 2; i < 32; i += 2) tops[c] = max3(tops[c], x[c][i], x[c][i + 1]);
+            }
+            const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * p.scale_log2;
             const bool grown = top > m + kSlack;
             if (__any_sync(0xffffffffu, grown)) {
                 const float keep = grown ? ex2(m - top) : 1.f;  // a row does not depend on its neighbours
                 if (grown) m = top;
                 sum *= keep;
                 if (j > w.j0) {  // the products of the tiles before are done: the logits' commit came after theirs
-                    float o[32];
-#pragma unroll
-                    for (int c = 0; c < D / 32; ++c) {
-                        tc::ld32(o_at + 32 * c, o);
+                    float o[16];
+#pragma unroll 1
+                    for (int c = 0; c < D / 16; ++c) {
+                        tc::ld16(o_at + 16 * c, o);
                         tc::wait_ld();
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) o[i] *= keep;
-                        tc::st32(o_at + 32 * c, reinterpret_cast<uint32_t(&)[32]>(o));
+                        for (int i = 0; i < 16; ++i) o[i] *= keep;
+                        tc::st16(o_at + 16 * c, reinterpret_cast<uint32_t(&)[16]>(o));
                     }
                 }
             }
             const float ref = m == -INFINITY ? 0.f : -m - kSlack;
+            float2 s2[2] = {};
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 uint32_t u[16];
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const float a = ex2(fmaf(x[c][2 * i], p.scale_log2, ref));
-                    const float b = ex2(fmaf(x[c][2 * i + 1], p.scale_log2, ref));
-                    sum += a + b;
+                    const float2 e = fma2(x[c][2 * i], x[c][2 * i + 1], p.scale_log2, ref);
+                    const float a = ex2(e.x), b = ex2(e.y);
+                    add2(s2[i & 1], a, b);
                     u[i] = ptx::pack_bf16(a, b);
                 }
                 tc::st16(s_at + 16 * c, u);
+                if (c & 1) {  // half of the keys
+                    tc::wait_st();
+                    tc::fence_before();
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(&sh.p_full[t][c >> 1]);
+                }
             }
-            tc::wait_st();
-            tc::fence_before();
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(&sh.p_full[t]);
+            sum += (s2[0].x + s2[0].y) + (s2[1].x + s2[1].y);
         }
         // ------------------------------------------------------------ results
-        const bool any = w.end[t] > w.j0;
+        const bool any = t_end > w.j0;
         if (live && any) live = wait_warp(sh, &sh.o_full[t], 0);
         tc::fence_after();
         const bool mine = live && token < at.rows && r < tile_tokens * p.G;
@@ -395,7 +430,7 @@ prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
 #pragma unroll
                     for (int i = 0; i < 32; ++i) o[i] = none ? 0.f : o[i] * inv;
                 if (dirty) {  // the elements of V that warp 10 took out, for the rows that see them
-                    const int32_t k0 = max(max(0, w.first), w.j0 * kTile), k1 = min(lim, w.end[t] * kTile);
+                    const int32_t k0 = max(max(0, w.first), w.j0 * kTile), k1 = min(lim, t_end * kTile);
                     for (int32_t key = k0; key < k1; ++key) {
                         const int64_t at_row = kPaged ? paged_row(p.cache.pv, w.cu, key) : w.cu * p.C + key;
                         if (at_row < 0 || at_row >= p.kv_rows) continue;
