@@ -7,9 +7,10 @@
 //   O_t += P_t V_j           128 x D, fp32, tensor memory
 // m is a row's reference, not its running maximum: it moves (and O_t with it) only when the maximum has grown by more
 // than 2^8 over it, so weights stay at most 1 and nearly every tile leaves O_t to the tensor cores alone.
-// Warps 0-3 and 4-7: a tile's weights, a row per thread. Warps 8 and 11: a tile's matrix instructions (one thread for
-// both would wait for one tile's weights while the other's lie ready). Warp 9: tile copies into a ring of K and V tiles.
-// Warp 10: what the mask hides of V.
+// Warps 0-7 and 8-15: a tile's weights, half a row of them per thread (a thread per row took 1500 cycles of a tile's turn,
+// which the other tile's 1000 cycles of products cannot hide). Warps 16 and 19: a tile's matrix instructions (one warp for
+// both would wait for one tile's weights while the other's lie ready). Warp 17: tile copies into a ring of K and V tiles.
+// Warp 18: what the mask hides of V.
 #include <algorithm>
 
 #include "evict_policy.cuh"  // once_per_device
@@ -22,8 +23,9 @@ namespace voxzip {
 namespace {
 
 constexpr int kTile = 128;       // rows of a tile, keys of a tile
-constexpr int kThreads = 12 * 32;
-constexpr uint32_t kPolls = 1u << 15, kSuspendNs = 100000;  // of a wait: three seconds at most
+constexpr int kMatrixWarp = 16, kCopyWarp = 17, kMaskWarp = 18, kMatrixWarp1 = 19;
+constexpr int kThreads = 20 * 32;
+constexpr uint32_t kPolls = 1u << 20;
 constexpr float kSlack = 8.f;    // growth of a row's maximum that its reference lets pass (log2)
 
 template <int D> struct Cfg {
@@ -37,18 +39,22 @@ template <int D> struct Cfg {
 };
 
 template <int D> struct Shared {
-    uint64_t q_full, full[Cfg<D>::kStages], empty[Cfg<D>::kStages], s_full[2], p_full[2][2], o_full[2], sent[4], clean[4], drained[2];
+    uint64_t q_full, full[Cfg<D>::kStages], empty[Cfg<D>::kStages], s_full[2], p_full[2], o_full[2], sent[4], clean[4], drained[2];
+    float half[2][2][kTile];  // what the two threads of a row tell each other
+    int gone[2][2][4];        // whether a wait of a weights' warp has given up
     TileAt at;
     uint32_t tmem;
     int ok, dead, dirty;
 };
 
-template <int D> constexpr size_t smem_bytes() { return 1024 + Cfg<D>::kBytes + sizeof(Shared<D>); }
+// The tiles start on a multiple of 1024 behind Shared; a CTA's memory does too, but for what the compiler puts first.
+template <int D> constexpr size_t smem_bytes() { return 3072 + Cfg<D>::kBytes; }
+static_assert(sizeof(Shared<128>) <= 2560 && smem_bytes<128>() <= 232448, "what an SM has");
 
 // A bounded wait; once one has given up in a CTA, all do.
 template <int D> __device__ __forceinline__ bool wait(Shared<D> &sh, uint64_t *bar, uint32_t parity) {
     for (uint32_t i = 0; i < kPolls; ++i) {
-        if (ptx::mbar_try_wait_for(bar, parity, kSuspendNs)) return true;
+        if (ptx::mbar_try_wait(bar, parity)) return true;
         if (*reinterpret_cast<volatile int *>(&sh.dead)) return false;
     }
     *reinterpret_cast<volatile int *>(&sh.dead) = 1;
@@ -59,6 +65,9 @@ template <int D> __device__ __forceinline__ bool wait(Shared<D> &sh, uint64_t *b
 template <int D> __device__ __forceinline__ bool wait_warp(Shared<D> &sh, uint64_t *bar, uint32_t parity) {
     return __all_sync(0xffffffffu, wait(sh, bar, parity));
 }
+
+// A barrier of two warps; both come, whatever their waits said.
+__device__ __forceinline__ void pair_barrier(int id) { asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory"); }
 
 __device__ __forceinline__ float ex2(float x) {
     float y;
@@ -107,26 +116,32 @@ __global__ void __launch_bounds__(kThreads, 1)
 prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                   const __grid_constant__ CUtensorMap map_v, const __grid_constant__ PromptAttn p) {
     using C = Cfg<D>;
-    extern __shared__ uint8_t raw[];
-    uint8_t *tiles = raw + (1024 - (ptx::smem_u32(raw) & 1023)) % 1024;
-    Shared<D> &sh = *reinterpret_cast<Shared<D> *>(tiles + C::kBytes);
+    extern __shared__ __align__(16) uint8_t raw[];
+    Shared<D> &sh = *reinterpret_cast<Shared<D> *>(raw);
+    const uint32_t front = (sizeof(Shared<D>) + ptx::smem_u32(raw) + 1023) / 1024 * 1024 - ptx::smem_u32(raw);
+    if (front + C::kBytes > smem_bytes<D>()) {  // (never: the memory in front of raw is a multiple of 1024)
+        raise_status(p.status, VOXZIP_DEV_TIMEOUT);
+        return;
+    }
+    uint8_t *tiles = raw + front;
     uint8_t *q_smem = tiles, *ring = tiles + 2 * C::kTileBytes;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;  // uniform for the compiler too
     const int h = blockIdx.y % p.Hkv, l = blockIdx.y / p.Hkv, split = blockIdx.z;
 
     if (threadIdx.x == 0) {
         ptx::mbar_init(&sh.q_full, 1);
         for (int i = 0; i < C::kStages; ++i) ptx::mbar_init(&sh.full[i], 1), ptx::mbar_init(&sh.empty[i], 2);
         for (int t = 0; t < 2; ++t)
-            ptx::mbar_init(&sh.s_full[t], 1), ptx::mbar_init(&sh.p_full[t][0], 4), ptx::mbar_init(&sh.p_full[t][1], 4), ptx::mbar_init(&sh.o_full[t], 1);
+            ptx::mbar_init(&sh.s_full[t], 1), ptx::mbar_init(&sh.p_full[t], 8), ptx::mbar_init(&sh.o_full[t], 1);
         for (int i = 0; i < 4; ++i) ptx::mbar_init(&sh.sent[i], 1), ptx::mbar_init(&sh.clean[i], 1);
         ptx::mbar_init(&sh.drained[0], 1), ptx::mbar_init(&sh.drained[1], 1);
         ptx::fence_mbar_init();
         sh.dead = 0;
+        for (int i = 0; i < 16; ++i) (&sh.gone[0][0][0])[i] = 0;
         sh.dirty = 0;
     }
-    if (warp == 8) tc::alloc(&sh.tmem, C::kColumns);
-    if (warp == 9 && lane == 0) {
+    if (warp == kMatrixWarp) tc::alloc(&sh.tmem, C::kColumns);
+    if (warp == kCopyWarp && lane == 0) {
         ptx::prefetch_tmap(&map_q);
         ptx::prefetch_tmap(&map_k);
         ptx::prefetch_tmap(&map_v);
@@ -143,7 +158,7 @@ prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
     tc::fence_before();
     __syncthreads();
     tc::fence_after();
-    const uint32_t tmem = sh.tmem;
+    const uint32_t tmem = __shfl_sync(0xffffffffu, sh.tmem, 0);
     bool ok = sh.ok;
     const TileAt at = sh.at;
     Work w = {};
@@ -171,7 +186,7 @@ prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
 
     if (!ok) {
         // nothing to do
-    } else if (warp == 9) {
+    } else if (warp == kCopyWarp) {
         // ------------------------------------------------------------ copies
         bool live = true;
         int issued = 0;
@@ -234,61 +249,64 @@ prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         if (lane == 0 && !live)  // a wait gave up: no copy is left in flight behind this CTA
             for (int i = max(0, issued - C::kStages); i < issued; ++i)
                 ptx::mbar_wait_bounded(&sh.full[i % C::kStages], i / C::kStages & 1, kPolls);
-    } else if (warp == 8 || warp == 11) {
+    } else if (warp == kMatrixWarp || warp == kMatrixWarp1) {
         // ------------------------------------------------------------ matrix instructions, a thread per row tile
-        const int t = warp == 11;
+        const int t = warp == kMatrixWarp1;
         const int32_t t_end = t ? w.end1 : w.end0;
-        if (lane == 0 && end > w.j0) {
+        if (end > w.j0) {
             constexpr uint32_t kInstS = tc::instruction(kTile, false), kInstO = tc::instruction(D, true);
             const uint32_t q_at = ptx::smem_u32(q_smem) + t * C::kTileBytes, ring_at = ptx::smem_u32(ring);
             const uint32_t s_at = tmem + t * kTile, o_at = tmem + C::kColO + t * D;
-            bool live = wait(sh, &sh.q_full, 0);
             int slot = 0, phase = 0;  // of the ring's next tile
-            auto next = [&] {
-                if (++slot == C::kStages) slot = 0, phase ^= 1;
-            };
-            // The logits of key tile j, once it is there. A tile of the ring that this thread has no use for is given
-            // back only when it has come: before that, the barrier's phase is that of its last use.
-            auto logits = [&](int32_t j) {
-                if (!(live = live && wait(sh, &sh.full[slot], phase))) return;
-                if (j < t_end) {
-                    tc::fence_after();
-                    const uint32_t k_at = ring_at + slot * C::kTileBytes;
+            auto logits = [&](int k_slot) {
+                const uint32_t k_at = ring_at + k_slot * C::kTileBytes;
 #pragma unroll
-                    for (int k = 0; k < D / 16; ++k) {
-                        const uint32_t off = k / 4 * C::kHalfBytes + k % 4 * 32;
-                        tc::mma(s_at, tc::operand(q_at + off, 0), tc::operand(k_at + off, 0), kInstS, k > 0);
-                    }
-                    tc::commit(&sh.s_full[t]);
-                    tc::commit(&sh.empty[slot]);
-                } else {
-                    ptx::mbar_arrive(&sh.empty[slot]);
+                for (int k = 0; k < D / 16; ++k) {
+                    const uint32_t off = k / 4 * C::kHalfBytes + k % 4 * 32;
+                    tc::mma(s_at, tc::operand(q_at + off, 0), tc::operand(k_at + off, 0), kInstS, k > 0);
                 }
-                next();
+                tc::commit(&sh.s_full[t]);
             };
-            logits(w.j0);
+            // Gives a tile of the ring back. One that this warp has no use for goes back only when it has come: before
+            // that, the barrier's phase is that of its last use.
+            auto release = [&](int at_slot, bool used) {
+                if (used)
+                    tc::commit(&sh.empty[at_slot]);
+                else if (lane == 0)
+                    ptx::mbar_arrive(&sh.empty[at_slot]);
+            };
+            bool live = wait_warp(sh, &sh.q_full, 0) && wait_warp(sh, &sh.full[0], 0);
+            if (live) {
+                tc::fence_after();
+                if (w.j0 < t_end) logits(0);
+                release(0, w.j0 < t_end);
+                slot = 1;
+            }
             for (int32_t j = w.j0; j < end && live; ++j) {
-                live = wait(sh, &sh.full[slot], phase);
-                if (live && j >= masked0) live = wait(sh, &sh.clean[j - max(w.j0, masked0)], 0);
-                if (live && j < t_end) {
-                    const uint32_t v_at = ring_at + slot * C::kTileBytes;
-#pragma unroll
-                    for (int half = 0; half < 2; ++half) {  // of the keys, as their weights come
-                        if (!(live = live && wait(sh, &sh.p_full[t][half], (j - w.j0) & 1))) break;
-                        tc::fence_after();
-#pragma unroll
-                        for (int k = 4 * half; k < 4 * half + 4; ++k)
-                            tc::mma_ta(o_at, s_at + k * 8, tc::operand(v_at + k * 16 * 128, C::kHalfBytes), kInstO,
-                                       j > w.j0 || k > 0);
-                    }
-                    if (!live) break;
-                    if (j + 1 == t_end) tc::commit(&sh.o_full[t]);
-                    tc::commit(&sh.empty[slot]);
-                } else if (live) {
-                    ptx::mbar_arrive(&sh.empty[slot]);
+                // V of this key tile and K of the next, before the weights: their copies are long done
+                const int v_slot = slot;
+                live = wait_warp(sh, &sh.full[slot], phase);
+                if (++slot == C::kStages) slot = 0, phase ^= 1;
+                const int k_slot = slot;
+                if (live && j + 1 < end) {
+                    live = wait_warp(sh, &sh.full[slot], phase);
+                    if (++slot == C::kStages) slot = 0, phase ^= 1;
                 }
-                next();
-                if (live && j + 1 < end) logits(j + 1);
+                if (live && j >= masked0) live = wait_warp(sh, &sh.clean[j - max(w.j0, masked0)], 0);
+                if (live && j < t_end) {
+                    if (!(live = wait_warp(sh, &sh.p_full[t], (j - w.j0) & 1))) break;
+                    tc::fence_after();
+                    const uint32_t v_at = ring_at + v_slot * C::kTileBytes;
+#pragma unroll
+                    for (int k = 0; k < kTile / 16; ++k)
+                        tc::mma_ta(o_at, s_at + k * 8, tc::operand(v_at + k * 16 * 128, C::kHalfBytes), kInstO,
+                                   j > w.j0 || k > 0);
+                    if (j + 1 < t_end) logits(k_slot);
+                    if (j + 1 == t_end) tc::commit(&sh.o_full[t]);
+                }
+                if (!live) break;
+                release(v_slot, j < t_end);
+                if (j + 1 < end) release(k_slot, j + 1 < t_end);
             }
             if (!live) {  // a wait gave up: what was issued ends before the tensor memory goes
                 tc::commit(&sh.drained[t]);
@@ -296,7 +314,7 @@ prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 raise_status(p.status, VOXZIP_DEV_TIMEOUT);
             }
         }
-    } else if (warp == 10) {
+    } else if (warp == kMaskWarp) {
         // ------------------------------------------------------------ V behind the mask
         // A weight of 0 times an infinity or a NaN would be NaN in rows that do not see the key. Rows that nobody sees
         // become 0. In rows that some see such elements do, and join the result at the end.
@@ -335,27 +353,29 @@ prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
             if (lane == 0) ptx::mbar_arrive(&sh.clean[j - max(w.j0, masked0)]);
         }
     } else {
-        // ------------------------------------------------------------ weights, a row per thread
-        const int t = warp >> 2, r = threadIdx.x & (kTile - 1);
+        // ------------------------------------------------------------ weights, half a row per thread
+        const int t = warp >> 3, hf = warp >> 2 & 1, r = threadIdx.x & (kTile - 1);
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // this warp's 32 lanes
-        const uint32_t s_at = tmem + lanes + t * kTile, o_at = tmem + lanes + C::kColO + t * D;
+        const uint32_t s_at = tmem + lanes + t * kTile + hf * 64, p_at = tmem + lanes + t * kTile + hf * 32;
+        constexpr int kCols = D / 2;  // this thread's of the output
+        const uint32_t o_at = tmem + lanes + C::kColO + t * D + hf * kCols;
+        const int pair = 1 + t * 4 + (warp & 3);  // the barrier of the two warps that have the same rows
         const int32_t token = t * tile_tokens + r / p.G;
         const int32_t lim = w.first + token;  // keys that the row sees
         const int32_t t_end = t ? w.end1 : w.end0;
         float m = -INFINITY, sum = 0.f;
         bool live = true;
         for (int32_t j = w.j0; j < t_end; ++j) {
-            const uint32_t phase = (j - w.j0) & 1;
-            if (!(live = wait_warp(sh, &sh.s_full[t], phase))) break;
+            live = wait_warp(sh, &sh.s_full[t], (j - w.j0) & 1);
             tc::fence_after();
-            float x[4][32];
+            float x[2][32];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) tc::ld32(s_at + 32 * c, x[c]);
+            for (int c = 0; c < 2; ++c) tc::ld32(s_at + 32 * c, x[c]);
             tc::wait_ld();
             if (j >= masked0) {
-                const int32_t seen = lim - j * kTile;
+                const int32_t seen = lim - j * kTile - hf * 64;
 #pragma unroll
-                for (int c = 0; c < 4; ++c)
+                for (int c = 0; c < 2; ++c)
 #pragma unroll
                     for (int i = 0; i < 32; ++i)
                         if (32 * c + i >= seen) x[c][i] = -INFINITY;
@@ -363,32 +383,40 @@ prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
             float tops[4];
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-                tops[c] = fmaxf(x[c][0], x[c][1]);
+                tops[c] = fmaxf(x[c >> 1][16 * (c & 1)], x[c >> 1][16 * (c & 1) + 1]);
 #pragma unroll
-                for (int i = 2; i < 32; i += 2) tops[c] = max3(tops[c], x[c][i], x[c][i + 1]);
+                for (int i = 2; i < 16; i += 2)
+                    tops[c] = max3(tops[c], x[c >> 1][16 * (c & 1) + i], x[c >> 1][16 * (c & 1) + i + 1]);
             }
-            const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * p.scale_log2;
+            float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * p.scale_log2;
+            sh.half[t][hf][r] = top;
+            if (!live) sh.gone[t][hf][warp & 3] = 1;
+            pair_barrier(pair);
+            top = fmaxf(top, sh.half[t][hf ^ 1][r]);
+            // A warp whose wait gave up comes as far as this, so that the two leave together.
+            live = live && !*reinterpret_cast<volatile int *>(&sh.gone[t][hf ^ 1][warp & 3]);
+            if (!live) break;
             const bool grown = top > m + kSlack;
-            if (__any_sync(0xffffffffu, grown)) {
+            if (__any_sync(0xffffffffu, grown)) {  // in both warps, or in neither
                 const float keep = grown ? ex2(m - top) : 1.f;  // a row does not depend on its neighbours
                 if (grown) m = top;
                 sum *= keep;
                 if (j > w.j0) {  // the products of the tiles before are done: the logits' commit came after theirs
                     float o[16];
 #pragma unroll 1
-                    for (int c = 0; c < D / 16; ++c) {
-                        tc::ld16(o_at + 16 * c, o);
+                    for (int c = 0; c < kCols; c += 16) {
+                        tc::ld16(o_at + c, o);
                         tc::wait_ld();
 #pragma unroll
                         for (int i = 0; i < 16; ++i) o[i] *= keep;
-                        tc::st16(o_at + 16 * c, reinterpret_cast<uint32_t(&)[16]>(o));
+                        tc::st16(o_at + c, reinterpret_cast<uint32_t(&)[16]>(o));
                     }
                 }
             }
             const float ref = m == -INFINITY ? 0.f : -m - kSlack;
             float2 s2[2] = {};
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
+            for (int c = 0; c < 2; ++c) {
                 uint32_t u[16];
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
@@ -397,19 +425,22 @@ prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     add2(s2[i & 1], a, b);
                     u[i] = ptx::pack_bf16(a, b);
                 }
-                tc::st16(s_at + 16 * c, u);
-                if (c & 1) {  // half of the keys
-                    tc::wait_st();
-                    tc::fence_before();
-                    __syncwarp();
-                    if (lane == 0) ptx::mbar_arrive(&sh.p_full[t][c >> 1]);
-                }
+                tc::st16(p_at + 16 * c, u);
             }
+            tc::wait_st();
+            tc::fence_before();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(&sh.p_full[t]);
             sum += (s2[0].x + s2[0].y) + (s2[1].x + s2[1].y);
         }
         // ------------------------------------------------------------ results
         const bool any = t_end > w.j0;
-        if (live && any) live = wait_warp(sh, &sh.o_full[t], 0);
+        if (any && live) {
+            live = wait_warp(sh, &sh.o_full[t], 0);
+            sh.half[t][hf][r] = sum;
+            pair_barrier(pair);
+            sum += sh.half[t][hf ^ 1][r];
+        }
         tc::fence_after();
         const bool mine = live && token < at.rows && r < tile_tokens * p.G;
         const int64_t row = ((int64_t)l * p.T + at.t0 + token) * p.Hq + h * p.G + r % p.G;
@@ -417,24 +448,25 @@ prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         const float inv = none ? 0.f : 1.f / sum;
         const bool dirty = *reinterpret_cast<volatile int *>(&sh.dirty);
         const int64_t all = (int64_t)p.layer_count * p.T * p.Hq;
-        if (mine && p.splits > 1)
+        if (mine && p.splits > 1 && hf == 0)
             p.part_ml[split * all + row] = make_float2(!any || m == -INFINITY ? -INFINITY : m + kSlack, any ? sum : 0.f);
         if (live && any) {
 #pragma unroll
-            for (int c = 0; c < D / 32; ++c) {
+            for (int c = 0; c < kCols / 32; ++c) {
                 float o[32];
                 tc::ld32(o_at + 32 * c, o);
                 tc::wait_ld();
                 if (!mine) continue;
+                const int col = hf * kCols + 32 * c;
                 if (p.splits == 1)
 #pragma unroll
                     for (int i = 0; i < 32; ++i) o[i] = none ? 0.f : o[i] * inv;
-                if (dirty) {  // the elements of V that warp 10 took out, for the rows that see them
+                if (dirty) {  // the elements of V that the mask warp took out, for the rows that see them
                     const int32_t k0 = max(max(0, w.first), w.j0 * kTile), k1 = min(lim, t_end * kTile);
                     for (int32_t key = k0; key < k1; ++key) {
                         const int64_t at_row = kPaged ? paged_row(p.cache.pv, w.cu, key) : w.cu * p.C + key;
                         if (at_row < 0 || at_row >= p.kv_rows) continue;
-                        const __nv_bfloat16 *v = static_cast<const __nv_bfloat16 *>(p.cache.v) + at_row * D + 32 * c;
+                        const __nv_bfloat16 *v = static_cast<const __nv_bfloat16 *>(p.cache.v) + at_row * D + col;
 #pragma unroll
                         for (int i = 0; i < 32; ++i) {
                             const float e = __bfloat162float(v[i]);
@@ -443,11 +475,11 @@ prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     }
                 }
                 if (p.splits > 1) {
-                    float4 *to = reinterpret_cast<float4 *>(p.part_o + (split * all + row) * D + 32 * c);
+                    float4 *to = reinterpret_cast<float4 *>(p.part_o + (split * all + row) * D + col);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) to[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
                 } else {
-                    uint4 *to = reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) + row * D + 32 * c);
+                    uint4 *to = reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) + row * D + col);
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
                         to[i] = make_uint4(ptx::pack_bf16(o[8 * i], o[8 * i + 1]), ptx::pack_bf16(o[8 * i + 2], o[8 * i + 3]),
@@ -455,15 +487,15 @@ prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 }
             }
         } else if (mine && p.splits == 1) {
-            uint4 *to = reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) + row * D);
-            for (int i = 0; i < D / 8; ++i) to[i] = make_uint4(0, 0, 0, 0);
+            uint4 *to = reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) + row * D + hf * kCols);
+            for (int i = 0; i < kCols / 8; ++i) to[i] = make_uint4(0, 0, 0, 0);
         }
     }
     tc::fence_before();
     __syncthreads();
     tc::fence_after();
     __syncwarp();
-    if (warp == 8) tc::dealloc(tmem, C::kColumns);
+    if (warp == kMatrixWarp) tc::dealloc(tmem, C::kColumns);
 }
 
 bool encode(CUtensorMap *map, const void *base, int rank, const cuuint64_t *dims, const cuuint64_t *strides,

@@ -72,27 +72,31 @@ __host__ __device__ constexpr uint32_t instruction(int n, bool b_n_major) {
     return 1u << 4 | 1u << 7 | 1u << 10 | (b_n_major ? 1u << 16 : 0u) | (uint32_t)(n / 8) << 17 | (128u / 16) << 24;
 }
 
-// ---------------------------------------------------------------- matrix instructions (one thread)
+// ---------------------------------------------------------------- matrix instructions
+// Called by a whole warp, whose elected lane issues them (the same one each time). Operands of a warp-uniform call live
+// in uniform registers; under a branch on the lane each of them would be moved there first, at 20 cycles an instruction.
 // d (128 x n, tensor memory) = a (128 x 16, shared memory) b (16 x n) + (add ? d : 0).
 __device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t inst, bool add) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "{\n\t.reg .pred p, e;\n\tsetp.ne.b32 p, %4, 0;\n\telect.sync _|e, 0xffffffff;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
         "l"(a), "l"(b), "r"(inst), "r"((uint32_t)add)
         : "memory");
 }
 // The same with a in tensor memory: column i of it holds elements 2 i and 2 i + 1 of each lane's row.
 __device__ __forceinline__ void mma_ta(uint32_t d, uint32_t a, uint64_t b, uint32_t inst, bool add) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+        "{\n\t.reg .pred p, e;\n\tsetp.ne.b32 p, %4, 0;\n\telect.sync _|e, 0xffffffff;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
         "r"(a), "l"(b), "r"(inst), "r"((uint32_t)add)
         : "memory");
 }
-// `bar` gets an arrival when every matrix instruction that this thread has issued is done.
+// `bar` gets an arrival when every matrix instruction that the elected lane has issued is done.
 __device__ __forceinline__ void commit(uint64_t *bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(ptx::smem_u32(bar))
-                 : "memory");
+    asm volatile(
+        "{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
+        "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(ptx::smem_u32(bar))
+        : "memory");
 }
 
 }  // namespace tc
