@@ -507,8 +507,10 @@ voxzip_status voxzip_rotary(const voxzip_cache_desc *desc, const voxzip_rotary_d
                             int32_t tokens, const voxzip_rows *q, const voxzip_rows *k, const int32_t *positions,
                             void *q_out, void *k_out, voxzip_stream_t stream);
 
-/* Bytes of workspace voxzip_append and voxzip_append_paged need (0 if the arguments are invalid). */
-size_t voxzip_append_workspace_size(const voxzip_cache_desc *desc, int32_t layer_count);
+/* Bytes of workspace voxzip_append and voxzip_append_paged need: 0 where max_rows (or tokens) says that every sequence
+   is short (and if the arguments are invalid). */
+size_t voxzip_append_workspace_size(const voxzip_cache_desc *desc, int32_t layer_count, int32_t tokens,
+                                    int32_t max_rows);
 
 /*
  * Appends the rows of every sequence to its units of layers [layer_begin, layer_begin + layer_count): with m tokens
@@ -522,8 +524,8 @@ size_t voxzip_append_workspace_size(const voxzip_cache_desc *desc, int32_t layer
  *   max_rows   host-side bound on the tokens of one sequence, or 0; a hint, which changes no result
  *   score, pos NULL: not kept (a prompt that stage 1 will read: its slab is a cache whose capacity is the
  *              prefill stride); new_pos may then be NULL too
- *   workspace  device scratch of voxzip_append_workspace_size() bytes, 256-byte aligned; contents need not be
- *              initialised
+ *   workspace  device scratch of voxzip_append_workspace_size() bytes for the same arguments, 256-byte aligned; contents
+ *              need not be initialised; NULL where that is 0
  * Device errors: VOXZIP_DEV_CAPACITY (a length outside [0, C], or n + m > C; the unit is skipped), BAD_SPANS.
  */
 voxzip_status voxzip_append(const voxzip_cache_desc *desc, const voxzip_rotary_desc *rotary, int32_t layer_begin,

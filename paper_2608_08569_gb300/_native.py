@@ -81,6 +81,11 @@ class CacheDesc:
         return self._units + (self.head_dim,)
 
     @functools.cached_property
+    def _vec(self):
+        """Elements of 16 bytes."""
+        return 8 if self.dtype is torch.bfloat16 else 4
+
+    @functools.cached_property
     def _c(self):
         """The binding's own C struct (never handed out: c_struct makes a new one)."""
         return self.c_struct()
@@ -251,7 +256,7 @@ def lib() -> ctypes.CDLL:
             L.voxzip_evict_q4.argtypes = [_DP, _QP, _i32, _i32, _vp, _vp, _vp, _vp, ctypes.POINTER(_EvictPolicy), _vp]
             _RP, _TP = ctypes.POINTER(_Rows), ctypes.POINTER(_RotaryDesc)
             L.voxzip_rotary.argtypes = [_DP, _TP, _i32, _i32, _RP, _RP, _vp, _vp, _vp, _vp]
-            L.voxzip_append_workspace_size.argtypes = [_DP, _i32]
+            L.voxzip_append_workspace_size.argtypes = [_DP, _i32, _i32, _i32]
             L.voxzip_append_workspace_size.restype = _sz
             L.voxzip_append.argtypes = [_DP, _TP, _i32, _i32, _i32, _RP, _RP, _RP, _vp, _vp, _vp, _i32, _vp, _vp, _vp,
                                         _vp, _vp, _vp, _vp, _sz, _vp]
@@ -364,14 +369,24 @@ def allocate_paged_cache(desc: CacheDesc, pages: int, device="cuda", stream=None
 
 
 def _paged_struct(desc: CacheDesc, pc) -> _Paged:
-    mp = desc.capacity // PAGE_TOKENS
-    _need(pc["k_pool"], "k_pool", desc.dtype, (pc["pages"], PAGE_TOKENS, desc.head_dim))
-    _need(pc["v_pool"], "v_pool", desc.dtype, (pc["pages"], PAGE_TOKENS, desc.head_dim))
-    _need(pc["page_table"], "page_table", torch.int32, (desc.batch, desc.layers, desc.kv_heads, mp))
-    _need(pc["free_pages"], "free_pages", torch.int32, (pc["pages"],))
-    _need(pc["free_count"], "free_count", torch.int32, (1,))
-    return _Paged(pc["k_pool"].data_ptr(), pc["v_pool"].data_ptr(), pc["page_table"].data_ptr(),
-                  pc["free_pages"].data_ptr(), pc["free_count"].data_ptr(), int(pc["pages"]), mp)
+    mp, pages = desc.capacity // PAGE_TOKENS, pc["pages"]
+    kp, vp, pt, fp, fc = pc["k_pool"], pc["v_pool"], pc["page_table"], pc["free_pages"], pc["free_count"]
+    pool = (pages, PAGE_TOKENS, desc.head_dim)
+    try:  # one pass over what must hold, as in _need
+        ok = (kp.dtype is desc.dtype and vp.dtype is desc.dtype and pt.dtype is torch.int32 and fp.dtype is torch.int32 and
+              fc.dtype is torch.int32 and kp.is_cuda and vp.is_cuda and pt.is_cuda and fp.is_cuda and fc.is_cuda and
+              kp.is_contiguous() and vp.is_contiguous() and pt.is_contiguous() and fp.is_contiguous() and
+              kp.shape == pool and vp.shape == pool and pt.shape == desc._units + (mp,) and fp.shape == (pages,) and
+              fc.shape == (1,))
+    except AttributeError:
+        ok = False
+    if not ok:
+        _need(kp, "k_pool", desc.dtype, pool)
+        _need(vp, "v_pool", desc.dtype, pool)
+        _need(pt, "page_table", torch.int32, (desc.batch, desc.layers, desc.kv_heads, mp))
+        _need(fp, "free_pages", torch.int32, (pages,))
+        _need(fc, "free_count", torch.int32, (1,))
+    return _Paged(kp.data_ptr(), vp.data_ptr(), pt.data_ptr(), fp.data_ptr(), fc.data_ptr(), int(pages), mp)
 
 
 def _check_dense_state(desc: CacheDesc, score, pos, len_) -> None:
@@ -783,18 +798,28 @@ def voxzip_evict_q4(desc: CacheDesc, qc, layer_begin: int, layer_count: int, bud
 def _rows(t, name: str, desc: CacheDesc, heads: int, like=None):
     """Checks rows [layers][tokens][heads][D] (heads dense, tokens and layers at any stride of whole 16-byte vectors)
     and returns their C struct; `like` is (layers, tokens)."""
+    D = desc.head_dim
+    try:  # one pass over what holds for most calls, as in _need
+        sl, st, sh, sd = t.stride()
+        at, vec = t.data_ptr(), desc._vec
+        if (t.dtype is desc.dtype and t.is_cuda and sd == 1 and sh == D and st >= heads * D and sl >= 1 and
+                not (st % vec or sl % vec or at & 15) and t.shape[2:] == (heads, D) and
+                (like is None or t.shape[:2] == like)):
+            return _Rows(at, st, sl)
+    except (AttributeError, ValueError, RuntimeError):
+        pass
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if t.dtype != desc.dtype:
         raise ValueError(f"{name}: dtype {t.dtype}, expected {desc.dtype}")
     if not t.is_cuda:
         raise ValueError(f"{name} must be on a CUDA device")
-    if t.dim() != 4 or t.shape[2] != heads or t.shape[3] != desc.head_dim or (like and tuple(t.shape[:2]) != like):
+    if t.dim() != 4 or tuple(t.shape[2:]) != (heads, D) or (like and tuple(t.shape[:2]) != tuple(like)):
         n = like or ("layers", "tokens")
-        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {(*n, heads, desc.head_dim)}")
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {(*n, heads, D)}")
     L, T = t.shape[:2]
     sl, st, sh, sd = t.stride()
-    D, vec = desc.head_dim, 16 // t.element_size()
+    vec = 16 // t.element_size()
     if T and L:
         if sd != 1 or (heads > 1 and sh != D) or (T > 1 and (st % vec or st < heads * D)) or (L > 1 and (sl % vec or sl < 1)) or \
                 t.data_ptr() % 16:
@@ -850,8 +875,8 @@ def voxzip_rotary(desc: CacheDesc, rotary: RotaryDesc, positions, *, q=None, k=N
         positions.data_ptr(), _ptr(q_out), _ptr(k_out), _stream(stream)))
 
 
-def voxzip_append_workspace_size(desc: CacheDesc, layer_count: int) -> int:
-    return int(lib().voxzip_append_workspace_size(ctypes.byref(desc._c), int(layer_count)))
+def voxzip_append_workspace_size(desc: CacheDesc, layer_count: int, tokens: int, max_rows: int = 0) -> int:
+    return int(lib().voxzip_append_workspace_size(ctypes.byref(desc._c), int(layer_count), int(tokens), int(max_rows)))
 
 
 def _append_args(desc: CacheDesc, layer_count: int, k, v, new_pos, seq_off, rotary, positions, q, q_out, pos_kept: bool):
@@ -888,7 +913,7 @@ def voxzip_append(desc: CacheDesc, layer_begin: int, layer_count: int, k, v, new
     if pos is not None:
         _need(pos, "pos", torch.int32, desc._slots)
     _need(len_, "len", torch.int32, desc._units)
-    at, size, _keep = _scratch(workspace, voxzip_append_workspace_size(desc, layer_count), k_cache.device, stream)
+    at, size, _keep = _scratch(workspace, voxzip_append_workspace_size(desc, layer_count, T, max_rows), k_cache.device, stream)
     _check("voxzip_append", lib().voxzip_append(
         ctypes.byref(desc._c), rotary and ctypes.byref(rotary._c), int(layer_begin), int(layer_count), T,
         qr and ctypes.byref(qr), ctypes.byref(kr), ctypes.byref(vr), _ptr(positions), _ptr(new_pos), seq_off.data_ptr(),
@@ -903,7 +928,7 @@ def voxzip_append_paged(desc: CacheDesc, pc, layer_begin: int, layer_count: int,
     T, qr, kr, vr, positions = _append_args(desc, layer_count, k, v, new_pos, seq_off, rotary, positions, q, q_out, True)
     _check_dense_state(desc, pc["score"], pc["pos"], pc["len"])
     ps = _paged_struct(desc, pc)
-    at, size, _keep = _scratch(workspace, voxzip_append_workspace_size(desc, layer_count), pc["k_pool"].device, stream)
+    at, size, _keep = _scratch(workspace, voxzip_append_workspace_size(desc, layer_count, T, max_rows), pc["k_pool"].device, stream)
     _check("voxzip_append_paged", lib().voxzip_append_paged(
         ctypes.byref(desc._c), ctypes.byref(ps), rotary and ctypes.byref(rotary._c), int(layer_begin), int(layer_count), T,
         qr and ctypes.byref(qr), ctypes.byref(kr), ctypes.byref(vr), _ptr(positions), _ptr(new_pos), seq_off.data_ptr(),
@@ -924,7 +949,7 @@ def _attention_args(desc: CacheDesc, layer_count: int, q, seq_off, out, max_rows
         raise ValueError(f"q: {L} layers, expected {layer_count}")
     _need(seq_off, "seq_off", torch.int32, (desc.batch + 1,))
     _need(out, "out", desc.dtype, (L, T, desc.q_heads, desc.head_dim))
-    need = voxzip_prompt_attention_workspace_size(desc, L, T, max_rows, max_len) if T else 0
+    need = voxzip_prompt_attention_workspace_size(desc, L, T, max_rows, max_len) if T and workspace is None else 0
     return T, qr, _scratch(workspace, need, out.device, stream)
 
 

@@ -85,8 +85,8 @@ CacheRows paged_rows(const voxzip_paged_cache &pc) {
 
 // Launches whose grid extents would not fit.
 bool counts_fit(const voxzip_cache_desc &d, int32_t layer_count, int32_t tokens) {
-    return (int64_t)layer_count * d.batch * d.kv_heads <= INT32_MAX && (int64_t)layer_count * d.kv_heads <= 65535 &&
-           (int64_t)layer_count * tokens <= INT32_MAX && (int64_t)tokens + d.batch <= INT32_MAX;
+    return (int64_t)layer_count * d.batch * d.kv_heads <= INT32_MAX && (int64_t)layer_count * tokens <= INT32_MAX &&
+           (int64_t)tokens + d.batch <= INT32_MAX;
 }
 
 voxzip_status from_cuda(cudaError_t e) { return e == cudaSuccess ? VOXZIP_OK : VOXZIP_ECUDA; }
@@ -107,8 +107,8 @@ voxzip_status append(const voxzip_cache_desc &d, const CacheRows &cache, const v
     if (!rows_ok(d, k, d.kv_heads, tokens, layer_count) || !rows_ok(d, v, d.kv_heads, tokens, layer_count))
         return VOXZIP_EINVAL;
     if (q && (!rows_ok(d, q, d.q_heads, tokens, layer_count) || !aligned(q_out, 16))) return VOXZIP_EINVAL;
-    if (!workspace || !aligned(workspace, 256) || workspace_bytes < voxzip::append_workspace_bytes(d, layer_count))
-        return VOXZIP_EINVAL;
+    const size_t need = voxzip::append_workspace_bytes(d, layer_count, tokens, max_rows);
+    if (need > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < need)) return VOXZIP_EINVAL;
     RotaryTable table = {};
     if (rotary && (!positions || !table_of(rotary, d, &table))) return VOXZIP_EINVAL;
     if (!counts_fit(d, layer_count, tokens)) return VOXZIP_EUNSUPPORTED;
@@ -132,7 +132,9 @@ voxzip_status attention(const voxzip_cache_desc &d, const CacheRows &cache, int3
     if (!counts_fit(d, layer_count, tokens)) return VOXZIP_EUNSUPPORTED;
     // a copy of a bf16 tile names its row by 32 bits
     if (d.dtype == VOXZIP_BF16 && cache.pool_rows > INT32_MAX) return VOXZIP_EUNSUPPORTED;
-    const size_t need = voxzip::prompt_plan(d, layer_count, tokens, max_rows, max_len).workspace;
+    const voxzip::PromptPlan plan = voxzip::prompt_plan(d, layer_count, tokens, max_rows, max_len);
+    if (plan.ctas > INT32_MAX) return VOXZIP_EUNSUPPORTED;
+    const size_t need = plan.workspace;
     if (need > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < need)) return VOXZIP_EINVAL;
     int32_t *status = nullptr;
     voxzip_status st = voxzip_status_word_address(&status);
@@ -164,10 +166,11 @@ voxzip_status voxzip_rotary(const voxzip_cache_desc *desc, const voxzip_rotary_d
                                            reinterpret_cast<cudaStream_t>(stream)));
 }
 
-size_t voxzip_append_workspace_size(const voxzip_cache_desc *desc, int32_t layer_count) {
+size_t voxzip_append_workspace_size(const voxzip_cache_desc *desc, int32_t layer_count, int32_t tokens,
+                                    int32_t max_rows) {
     Range range("voxzip_append_workspace_size");
-    if (!desc_ok(desc) || layer_count < 1 || layer_count > desc->layers) return 0;
-    return voxzip::append_workspace_bytes(*desc, layer_count);
+    if (!desc_ok(desc) || layer_count < 1 || layer_count > desc->layers || tokens < 1) return 0;
+    return voxzip::append_workspace_bytes(*desc, layer_count, tokens, max_rows);
 }
 
 voxzip_status voxzip_append(const voxzip_cache_desc *desc, const voxzip_rotary_desc *rotary, int32_t layer_begin,

@@ -39,7 +39,7 @@ cudaError_t launch_rotary(const voxzip_cache_desc &d, const RotaryTable &table, 
                           RowsView q, RowsView k, const int32_t *positions, void *q_out, void *k_out,
                           cudaStream_t stream);
 
-size_t append_workspace_bytes(const voxzip_cache_desc &d, int32_t layer_count);
+size_t append_workspace_bytes(const voxzip_cache_desc &d, int32_t layer_count, int32_t tokens, int32_t max_rows);
 cudaError_t launch_append(const voxzip_cache_desc &d, const RotaryTable *table, int32_t layer_begin,
                           int32_t layer_count, RowsView q, RowsView k, RowsView v, const int32_t *positions,
                           const int32_t *new_pos, const int32_t *seq_off, int32_t tokens, int32_t max_rows,
@@ -66,24 +66,37 @@ struct PromptAttn {
     int64_t kv_rows;  // rows of the K and V tensors (checked builds)
 };
 
+// A CTA's tile, split, kv-head and layer. CTAs start in order: the tiles that see the most keys first, of all heads, so
+// that the last ones to start are short.
+struct CtaAt {
+    int32_t x, split, h, l;
+};
+__device__ __forceinline__ CtaAt cta_at(const PromptAttn &p) {
+    const uint32_t units = p.Hkv * p.layer_count, i = blockIdx.x;
+    const uint32_t u = i % units, rest = i / units;
+    return CtaAt{(int32_t)(rest / p.splits), (int32_t)(rest % p.splits), (int32_t)(u % p.Hkv), (int32_t)(u / p.Hkv)};
+}
+
 // A CTA's place: tile `x` of those of all sequences, in packed order, the last tile of a sequence first (it sees the
 // most keys, and CTAs start in order).
 struct TileAt {
     int32_t b, t0, rows, before;  // sequence, first packed token, tokens of this tile, its first token's index in the sequence
-    int32_t m;                    // the sequence's tokens
+    int32_t m, n;                 // the sequence's tokens, the unit's length
 };
 
-// One warp, all lanes. False where x lies behind the last tile or the offsets are malformed up to it.
-__device__ __forceinline__ bool find_tile(const int32_t *seq_off, int32_t B, int32_t T, int32_t per, int32_t x,
-                                          int32_t *status, TileAt &at) {
+// One warp, all lanes. False where x lies behind the last tile or the offsets are malformed up to it. The lengths of the
+// units that it may turn out to be are loaded beside the offsets, not after them.
+__device__ __forceinline__ bool find_tile(const PromptAttn &p, const CtaAt &cta, TileAt &at) {
     const int lane = threadIdx.x & 31;
+    const int32_t B = p.B, T = p.T, per = p.tile_tokens, x = cta.x;
     int32_t first = 0;
     for (int32_t base = 0; base < B; base += 32) {
         const int32_t b = base + lane;
-        const int32_t o0 = b < B ? seq_off[b] : 0, o1 = b < B ? seq_off[b + 1] : 0;
+        const int32_t o0 = b < B ? p.seq_off[b] : 0, o1 = b < B ? p.seq_off[b + 1] : 0;
+        const int32_t len = b < B ? p.len[((int64_t)b * p.L + p.layer_begin + cta.l) * p.Hkv + cta.h] : 0;
         const bool bad = b < B && (o0 < 0 || o1 < o0 || o1 > T);
         if (__ballot_sync(0xffffffffu, bad)) {
-            if (lane == 0) raise_status(status, VOXZIP_DEV_BAD_SPANS);
+            if (lane == 0) raise_status(p.status, VOXZIP_DEV_BAD_SPANS);
             return false;
         }
         const int32_t n = (o1 - o0) / per + ((o1 - o0) % per != 0);
@@ -99,6 +112,7 @@ __device__ __forceinline__ bool find_tile(const int32_t *seq_off, int32_t B, int
             const int32_t idx = __shfl_sync(0xffffffffu, n - 1 - (x - (first + sum - n)), src);
             const int32_t s0 = __shfl_sync(0xffffffffu, o0, src), s1 = __shfl_sync(0xffffffffu, o1, src);
             at.b = base + src;
+            at.n = __shfl_sync(0xffffffffu, len, src);
             at.m = s1 - s0;
             at.before = idx * per;
             at.t0 = s0 + at.before;
@@ -110,13 +124,16 @@ __device__ __forceinline__ bool find_tile(const int32_t *seq_off, int32_t B, int
     return false;
 }
 
-// CTAs of a launch: every sequence has ceil(m / per) tiles, so all of them at most T / per + B.
-inline int64_t tile_bound(int64_t tokens, int64_t B, int per) { return tokens / per + (B < tokens ? B : tokens); }
+// Tiles of a launch at most: every sequence has ceil(m / per) of them.
+inline int64_t tile_bound(int64_t tokens, int64_t B, int per) {
+    return (tokens + (B < tokens ? B : tokens) * (per - 1)) / per;
+}
 
 cudaError_t launch_prompt_mma(const PromptAttn &p, int D, cudaStream_t stream);
 
 struct PromptPlan {
     int32_t splits, tile_tokens;
+    int64_t ctas;
     size_t workspace;
 };
 PromptPlan prompt_plan(const voxzip_cache_desc &d, int32_t layer_count, int32_t tokens, int32_t max_rows,

@@ -34,35 +34,62 @@ __device__ __forceinline__ int64_t cache_row(const PromptAttn &p, int64_t cu, in
     return r >= 0 && r < p.cache.pool_rows ? r : -1;
 }
 
-// Stores row `at` ([layer][token][head]) of the result, or of this CTA's split.
-template <typename T, int N>
-__device__ __forceinline__ void store_row(const PromptAttn &p, int64_t at, int d, const float (&o)[N], float inv,
-                                          bool split, int s, int D) {
-    if (split) {
-        float *to = p.part_o + ((int64_t)s * p.layer_count * p.T * p.Hq + at) * D + d;
-#pragma unroll
-        for (int i = 0; i < N; ++i) to[i] = o[i];
-    } else {
-        T *to = static_cast<T *>(p.out) + at * D + d;
-#pragma unroll
-        for (int i = 0; i < N; ++i) to[i] = Elem<T>::from_f(o[i] * inv);
-    }
+// 16 bytes to shared memory in the background; zeros where `from` is null.
+__device__ __forceinline__ void copy16(float *to, const float *from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ptx::smem_u32(to)), "l"(from), "r"(from ? 16 : 0)
+                 : "memory");
+}
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kPending> __device__ __forceinline__ void copies_wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(kPending) : "memory");
 }
 
-// 256 threads as 16 x 16: thread (ty, tx) has the logits of rows ty + 16 i and keys tx + 16 j, and of the output the
-// same rows' channels 4 tx (and 64 + 4 tx). Fused multiply-adds bound it: per four channels 128 of them meet twelve
-// 16-byte reads of shared memory.
+// A pair of products and sums: d += a b.
+struct Pair {
+    float x, y;
+};
+__device__ __forceinline__ void fma_pair(Pair &d, float a0, float a1, float b0, float b1) {
+    asm("{\n\t.reg .b64 a, b, c;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%0, %1};\n\t"
+        "fma.rn.f32x2 c, a, b, c;\n\tmov.b64 {%0, %1}, c;\n\t}"
+        : "+f"(d.x), "+f"(d.y)
+        : "f"(a0), "f"(a1), "f"(b0), "f"(b1));
+}
+
+// Tile rows of K or V: keys [key0, key0 + 64), zeros from `most` on.
+template <int D>
+__device__ __forceinline__ void copy_keys(const PromptAttn &p, const void *data, int64_t cu, int32_t key0, int32_t most,
+                                          float *to, int stride) {
+    for (int i = threadIdx.x; i < kKeys * (D / 4); i += 256) {
+        const int r = i / (D / 4), d = i % (D / 4) * 4;
+        const float *from = nullptr;
+        if (key0 + r < most) {
+            const int64_t row = cache_row(p, cu, key0 + r);
+            if (row < 0) {
+                if (d == 0) raise_status(p.status, VOXZIP_DEV_CAPACITY);
+            } else if (VOXZIP_IN_RANGE(p.status, row < p.kv_rows)) {
+                from = static_cast<const float *>(data) + row * D + d;
+            }
+        }
+        copy16(to + r * stride + d, from);
+    }
+    copies_end();
+}
+
+// fp32 rows. 256 threads as 16 x 16: thread (ty, tx) has the logits of rows ty + 16 i and keys tx + 16 j, and of the
+// output the same rows' channels 4 tx (and 64 + 4 tx). Fused multiply-adds bound it, two to an instruction: per four
+// channels 64 of these meet twelve 16-byte reads of shared memory. K's and V's next tiles come while the other's is used.
 template <int D>
 __global__ void __launch_bounds__(256) prompt_rows_kernel(const PromptAttn p) {
     extern __shared__ __align__(16) uint8_t raw[];
-    using T = float;
     Smem<D> &sm = *reinterpret_cast<Smem<D> *>(raw);
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
-    const int h = blockIdx.y % p.Hkv, l = blockIdx.y / p.Hkv, s = blockIdx.z;
+    const CtaAt cta = cta_at(p);
+    const int h = cta.h, l = cta.l, s = cta.split;
     ptx::grid_dependency_wait();
+    ptx::launch_dependents();  // the join may take its place on the SMs
     if (tid < 32) {
         TileAt at;
-        const bool ok = find_tile(p.seq_off, p.B, p.T, p.tile_tokens, blockIdx.x, p.status, at);
+        const bool ok = find_tile(p, cta, at);
         if (tid == 0) {
             sm.ok = ok;
             if (ok) sm.at = at;
@@ -72,7 +99,7 @@ __global__ void __launch_bounds__(256) prompt_rows_kernel(const PromptAttn p) {
     if (!sm.ok) return;
     const TileAt at = sm.at;
     const int64_t cu = ((int64_t)at.b * p.L + p.layer_begin + l) * p.Hkv + h;
-    const int32_t n = p.len[cu];
+    const int32_t n = at.n;
     if (n < 0 || n > p.C) {
         if (tid == 0) raise_status(p.status, VOXZIP_DEV_CAPACITY);
         return;
@@ -84,45 +111,34 @@ __global__ void __launch_bounds__(256) prompt_rows_kernel(const PromptAttn p) {
     const int32_t tiles = (most + kKeys - 1) / kKeys, per = (tiles + p.splits - 1) / p.splits;
     const int32_t j0 = min(tiles, s * per), j1 = min(tiles, j0 + per);
 
-    for (int i = tid; i < kRows * (D / 4); i += 256) {
-        const int r = i / (D / 4), d = i % (D / 4) * 4;
-        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (r < rows)
-            x = load4(static_cast<const T *>(p.q.data) + l * p.q.layer_stride +
-                      (int64_t)(at.t0 + r / p.G) * p.q.token_stride + (int64_t)(h * p.G + r % p.G) * D + d);
-        *reinterpret_cast<float4 *>(&sm.q[r * Smem<D>::kQ + d]) = x;
+    if (j0 < j1) {
+        for (int i = tid; i < kRows * (D / 4); i += 256) {
+            const int r = i / (D / 4), d = i % (D / 4) * 4;
+            copy16(&sm.q[r * Smem<D>::kQ + d],
+                   r < rows ? static_cast<const float *>(p.q.data) + l * p.q.layer_stride +
+                                  (int64_t)(at.t0 + r / p.G) * p.q.token_stride + (int64_t)(h * p.G + r % p.G) * D + d
+                            : nullptr);
+        }
+        copy_keys<D>(p, p.cache.k, cu, j0 * kKeys, most, sm.k, Smem<D>::kK);
+        copy_keys<D>(p, p.cache.v, cu, j0 * kKeys, most, sm.v, D);
     }
     int32_t lim[8];  // keys that each of this thread's rows sees
-    float mx[8], sum[8], o[8][D / 16];
+    float mx[8], sum[8];
+    Pair o[8][D / 32];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         lim[i] = first + (ty + 16 * i) / p.G;
         mx[i] = -INFINITY;
         sum[i] = 0.f;
 #pragma unroll
-        for (int d = 0; d < D / 16; ++d) o[i][d] = 0.f;
+        for (int d = 0; d < D / 32; ++d) o[i][d] = Pair{0.f, 0.f};
     }
     for (int32_t j = j0; j < j1; ++j) {
         const int32_t key0 = j * kKeys;
+        copies_wait<1>();  // K (and Q); V may be on its way
         __syncthreads();
-        for (int i = tid; i < kKeys * (D / 4); i += 256) {
-            const int r = i / (D / 4), d = i % (D / 4) * 4;
-            float4 k = make_float4(0.f, 0.f, 0.f, 0.f), v = k;
-            if (key0 + r < most) {
-                const int64_t row = cache_row(p, cu, key0 + r);
-                if (row < 0) {
-                    if (d == 0) raise_status(p.status, VOXZIP_DEV_CAPACITY);
-                } else if (VOXZIP_IN_RANGE(p.status, row < p.kv_rows)) {
-                    k = load4(static_cast<const T *>(p.cache.k) + row * D + d);
-                    v = load4(static_cast<const T *>(p.cache.v) + row * D + d);
-                }
-            }
-            *reinterpret_cast<float4 *>(&sm.k[r * Smem<D>::kK + d]) = k;
-            *reinterpret_cast<float4 *>(&sm.v[r * D + d]) = v;
-        }
-        __syncthreads();
-        float x[8][4] = {};
-#pragma unroll 4
+        Pair acc[8][4] = {};
+#pragma unroll 2
         for (int d = 0; d < D; d += 4) {
             float4 q[8], k[4];
 #pragma unroll
@@ -133,19 +149,18 @@ __global__ void __launch_bounds__(256) prompt_rows_kernel(const PromptAttn p) {
             for (int i = 0; i < 8; ++i)
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    x[i][c] = fmaf(q[i].x, k[c].x, x[i][c]);
-                    x[i][c] = fmaf(q[i].y, k[c].y, x[i][c]);
-                    x[i][c] = fmaf(q[i].z, k[c].z, x[i][c]);
-                    x[i][c] = fmaf(q[i].w, k[c].w, x[i][c]);
+                    fma_pair(acc[i][c], q[i].x, q[i].y, k[c].x, k[c].y);
+                    fma_pair(acc[i][c], q[i].z, q[i].w, k[c].z, k[c].w);
                 }
         }
         const bool masked = key0 + kKeys > first;  // some row does not see all of this tile
+        float x[8][4];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             float top = -INFINITY;
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-                x[i][c] *= p.scale_log2;
+                x[i][c] = (acc[i][c].x + acc[i][c].y) * p.scale_log2;
                 if (masked && key0 + tx + 16 * c >= lim[i]) x[i][c] = -INFINITY;
                 top = fmaxf(top, x[i][c]);
             }
@@ -162,7 +177,7 @@ __global__ void __launch_bounds__(256) prompt_rows_kernel(const PromptAttn p) {
                 sum[i] += x[i][c];
             }
 #pragma unroll
-            for (int d = 0; d < D / 16; ++d) o[i][d] *= keep;
+            for (int d = 0; d < D / 32; ++d) o[i][d].x *= keep, o[i][d].y *= keep;
         }
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
@@ -170,25 +185,27 @@ __global__ void __launch_bounds__(256) prompt_rows_kernel(const PromptAttn p) {
             to[0] = make_float4(x[0][c], x[1][c], x[2][c], x[3][c]);
             to[1] = make_float4(x[4][c], x[5][c], x[6][c], x[7][c]);
         }
+        copies_wait<0>();  // V
         __syncthreads();
+        if (j + 1 < j1) copy_keys<D>(p, p.cache.k, cu, key0 + kKeys, most, sm.k, Smem<D>::kK);
         auto accumulate = [&](auto guard) {
 #pragma unroll 4
             for (int key = 0; key < kKeys; ++key) {
                 const float4 *pr = reinterpret_cast<const float4 *>(&sm.p[key * Smem<D>::kP + ty * 8]);
                 const float4 pa = pr[0], pb = pr[1];
                 const float w[8] = {pa.x, pa.y, pa.z, pa.w, pb.x, pb.y, pb.z, pb.w};
-                float v[D / 16];
+                float4 v[D / 64];
 #pragma unroll
-                for (int c = 0; c < D / 64; ++c) {
-                    const float4 t = *reinterpret_cast<const float4 *>(&sm.v[key * D + 64 * c + 4 * tx]);
-                    v[4 * c] = t.x, v[4 * c + 1] = t.y, v[4 * c + 2] = t.z, v[4 * c + 3] = t.w;
-                }
+                for (int c = 0; c < D / 64; ++c) v[c] = *reinterpret_cast<const float4 *>(&sm.v[key * D + 64 * c + 4 * tx]);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const bool unseen = decltype(guard)::value && key0 + key >= lim[i];
 #pragma unroll
-                    for (int d = 0; d < D / 16; ++d)  // 0 times an infinity behind the mask is not 0
-                        o[i][d] = fmaf(w[i], unseen ? 0.f : v[d], o[i][d]);
+                    for (int c = 0; c < D / 64; ++c) {  // 0 times an infinity behind the mask is not 0
+                        const float4 u = unseen ? make_float4(0.f, 0.f, 0.f, 0.f) : v[c];
+                        fma_pair(o[i][2 * c], w[i], w[i], u.x, u.y);
+                        fma_pair(o[i][2 * c + 1], w[i], w[i], u.z, u.w);
+                    }
                 }
             }
         };
@@ -196,6 +213,8 @@ __global__ void __launch_bounds__(256) prompt_rows_kernel(const PromptAttn p) {
             accumulate(std::true_type{});
         else
             accumulate(std::false_type{});
+        __syncthreads();
+        if (j + 1 < j1) copy_keys<D>(p, p.cache.v, cu, key0 + kKeys, most, sm.v, D);
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -204,62 +223,75 @@ __global__ void __launch_bounds__(256) prompt_rows_kernel(const PromptAttn p) {
         const int r = ty + 16 * i;
         if (r >= rows) continue;
         const int64_t row = ((int64_t)l * p.T + at.t0 + r / p.G) * p.Hq + h * p.G + r % p.G;
-        const float inv = lim[i] <= 0 ? 0.f : 1.f / sum[i];  // a row that sees nothing is 0
-        if (p.splits > 1 && tx == 0)
-            p.part_ml[(int64_t)s * p.layer_count * p.T * p.Hq + row] = make_float2(mx[i], sum[i]);
+        const int64_t all = (int64_t)p.layer_count * p.T * p.Hq;
+        const bool split = p.splits > 1;
+        const float scale = split ? 1.f : lim[i] <= 0 ? 0.f : 1.f / sum[i];  // a row that sees nothing is 0
+        if (split && tx == 0) p.part_ml[s * all + row] = make_float2(mx[i], sum[i]);
+        if (split && j0 == j1) continue;  // the join does not read it
+        float *to = split ? p.part_o + (s * all + row) * D : static_cast<float *>(p.out) + row * D;
 #pragma unroll
-        for (int c = 0; c < D / 64; ++c) {
-            const float part[4] = {o[i][4 * c], o[i][4 * c + 1], o[i][4 * c + 2], o[i][4 * c + 3]};
-            store_row<T>(p, row, 64 * c + 4 * tx, part, inv, p.splits > 1, s, D);
-        }
+        for (int c = 0; c < D / 64; ++c)
+            *reinterpret_cast<float4 *>(&to[64 * c + 4 * tx]) =
+                make_float4(o[i][2 * c].x * scale, o[i][2 * c].y * scale, o[i][2 * c + 1].x * scale, o[i][2 * c + 1].y * scale);
     }
 }
 
 // Joins the splits: out = sum_s o_s 2^(m_s - m) / sum_s l_s 2^(m_s - m), m the greatest m_s. A warp per row.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) prompt_join_kernel(const PromptAttn p) {
-    ptx::grid_dependency_wait();
     const int lane = threadIdx.x & 31;
     const int64_t rows = (int64_t)p.layer_count * p.T * p.Hq;
     const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
     if (row >= rows) return;
-    // rows of no sequence, or of one whose unit was skipped, were not written
+    // Rows of no sequence, or of one whose unit was skipped, were not written. (What this reads is older than the launch
+    // before, which let this one start only after it had waited itself.)
     const int32_t t = (int32_t)(row / p.Hq % p.T);
     const int l = (int)(row / p.Hq / p.T), h = (int)(row % p.Hq) / p.G;
-    int32_t b = -1;
+    int32_t n = -1, seen = 0;
     for (int32_t base = 0; base < p.B; base += 32) {
         const int32_t c = base + lane;
         const int32_t o0 = c < p.B ? p.seq_off[c] : 0, o1 = c < p.B ? p.seq_off[c + 1] : 0;
+        const int32_t len = c < p.B ? p.len[((int64_t)c * p.L + p.layer_begin + l) * p.Hkv + h] : 0;
         if (__any_sync(0xffffffffu, c < p.B && (o0 < 0 || o1 < o0 || o1 > p.T))) return;
         const unsigned mine = __ballot_sync(0xffffffffu, c < p.B && o0 <= t && t < o1);
         if (mine) {
-            b = base + __ffs(mine) - 1;
+            n = __shfl_sync(0xffffffffu, len, __ffs(mine) - 1);
+            seen = n - __shfl_sync(0xffffffffu, o1, __ffs(mine) - 1) + t + 1;  // keys
             break;
         }
     }
-    if (b < 0) return;
-    const int32_t n = p.len[((int64_t)b * p.L + p.layer_begin + l) * p.Hkv + h];
     if (n < 0 || n > p.C) return;
-    const bool none = n - p.seq_off[b + 1] + t + 1 <= 0;
+    ptx::grid_dependency_wait();
+    // a lane's split's statistics; of all of them the greatest maximum
     float m = -INFINITY;
     for (int s = lane; s < p.splits; s += 32) m = fmaxf(m, p.part_ml[s * rows + row].x);
 #pragma unroll
     for (int w = 16; w > 0; w >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, w));
     if (m == -INFINITY) m = 0.f;
     float sum = 0.f, o[D / 32] = {};
-    for (int s = 0; s < p.splits; ++s) {
-        const float2 ml = p.part_ml[s * rows + row];
-        if (ml.x == -INFINITY && ml.y == 0.f) continue;  // it has no key of this row
-        const float w = exp2f(ml.x - m);
-        sum = fmaf(ml.y, w, sum);
-        const float *from = p.part_o + (s * rows + row) * D + lane * (D / 32);
+    for (int s0 = 0; s0 < p.splits; s0 += 4) {
+        float2 ml[4];
+        float part[4][D / 32];
 #pragma unroll
-        for (int d = 0; d < D / 32; ++d) o[d] = fmaf(from[d], w, o[d]);
+        for (int u = 0; u < 4; ++u) {
+            ml[u] = s0 + u < p.splits ? p.part_ml[(s0 + u) * rows + row] : make_float2(-INFINITY, 0.f);
+            const bool has = !(ml[u].x == -INFINITY && ml[u].y == 0.f);  // a key of this row
+            const float *from = p.part_o + ((s0 + u) * rows + row) * D + lane * (D / 32);
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d) part[u][d] = has ? from[d] : 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const float w = exp2f(ml[u].x - m);
+            sum = fmaf(ml[u].y, w, sum);
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d) o[d] = fmaf(part[u][d], w, o[d]);
+        }
     }
-    const float inv = none ? 0.f : 1.f / sum;
+    const float inv = 1.f / sum;
     T *to = static_cast<T *>(p.out) + row * D + lane * (D / 32);
 #pragma unroll
-    for (int d = 0; d < D / 32; ++d) to[d] = Elem<T>::from_f(none ? 0.f : o[d] * inv);
+    for (int d = 0; d < D / 32; ++d) to[d] = Elem<T>::from_f(seen <= 0 ? 0.f : o[d] * inv);
 }
 
 cudaLaunchConfig_t config(dim3 grid, int threads, size_t smem, cudaStream_t stream, cudaLaunchAttribute *attr) {
@@ -289,7 +321,7 @@ template <int D> cudaError_t launch_rows(const PromptAttn &p, cudaStream_t strea
     });
     if (e != cudaSuccess) return e;
     cudaLaunchAttribute attr[1];
-    cudaLaunchConfig_t cfg = config(dim3(p.tiles, p.Hkv * p.layer_count, p.splits), 256, sizeof(Smem<D>), stream, attr);
+    cudaLaunchConfig_t cfg = config(dim3(p.tiles * p.Hkv * p.layer_count * p.splits), 256, sizeof(Smem<D>), stream, attr);
     e = cudaLaunchKernelEx(&cfg, prompt_rows_kernel<D>, p);
     return e != cudaSuccess || p.splits == 1 ? e : launch_join<float, D>(p, stream);
 }
@@ -298,17 +330,20 @@ template <int D> cudaError_t launch_rows(const PromptAttn &p, cudaStream_t strea
 
 PromptPlan prompt_plan(const voxzip_cache_desc &d, int32_t layer_count, int32_t tokens, int32_t max_rows,
                        int32_t max_len) {
-    // Rows and keys of a CTA's tiles; a split wants a few tiles of keys to itself.
+    // Rows and keys of a CTA's tiles. Keys are shared out where there are fewer CTAs than the GPU takes at once. fp32
+    // (a key tile is 9 us of a CTA's work): up to three for each SM, as the last rows of a prompt see twice the keys of
+    // the average one (631 tokens, 32/4 heads: 164 us unsplit); bf16 (1.5 us): one, with two key tiles or more.
     const int G = d.q_heads / d.kv_heads;
     const bool mma = d.dtype == VOXZIP_BF16;
-    const int keys = mma ? 128 : kKeys, least = mma ? 2 : 4;
+    const int keys = mma ? 128 : kKeys, least = mma ? 2 : 1, per_sm = mma ? 1 : 3;
     PromptPlan plan;
     plan.tile_tokens = mma ? 2 * (128 / G) : kRows / G;
-    if (max_rows <= 0 || max_rows > tokens) max_rows = tokens;
     if (max_len <= 0 || max_len > d.capacity) max_len = d.capacity;
     const int64_t ctas = tile_bound(tokens, d.batch, plan.tile_tokens) * d.kv_heads * layer_count;
     const int64_t key_tiles = (max_len + keys - 1) / keys;
-    plan.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(kSms / std::max<int64_t>(1, ctas), key_tiles / least));
+    plan.splits = (int32_t)std::max<int64_t>(
+        1, std::min<int64_t>(per_sm * kSms / std::max<int64_t>(1, ctas), key_tiles / least));
+    plan.ctas = ctas * plan.splits;
     const size_t rows = (size_t)layer_count * tokens * d.q_heads;
     plan.workspace = plan.splits == 1 ? 0 : plan.splits * rows * (d.head_dim * sizeof(float) + sizeof(float2));
     plan.workspace = (plan.workspace + 255) / 256 * 256;

@@ -126,7 +126,8 @@ prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
     uint8_t *tiles = raw + front;
     uint8_t *q_smem = tiles, *ring = tiles + 2 * C::kTileBytes;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;  // uniform for the compiler too
-    const int h = blockIdx.y % p.Hkv, l = blockIdx.y / p.Hkv, split = blockIdx.z;
+    const CtaAt cta = cta_at(p);
+    const int h = cta.h, l = cta.l, split = cta.split;
 
     if (threadIdx.x == 0) {
         ptx::mbar_init(&sh.q_full, 1);
@@ -147,9 +148,10 @@ prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         ptx::prefetch_tmap(&map_v);
     }
     ptx::grid_dependency_wait();
+    ptx::launch_dependents();  // the join may take its place on the SMs
     if (warp == 0) {
         TileAt at;
-        const bool found = find_tile(p.seq_off, p.B, p.T, p.tile_tokens, blockIdx.x, p.status, at);
+        const bool found = find_tile(p, cta, at);
         if (lane == 0) {
             sh.ok = found;
             if (found) sh.at = at;
@@ -165,7 +167,7 @@ prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
     const int tile_tokens = kTile / p.G;
     if (ok) {
         w.cu = ((int64_t)at.b * p.L + p.layer_begin + l) * p.Hkv + h;
-        const int32_t n = p.len[w.cu];
+        const int32_t n = at.n;
         if (n < 0 || n > p.C) {
             if (threadIdx.x == 0) raise_status(p.status, VOXZIP_DEV_CAPACITY);
             ok = false;
@@ -527,7 +529,7 @@ template <int D, bool kPaged> cudaError_t launch(const PromptAttn &p, cudaStream
         !make_cache_map(&mv, p.cache.v, p.cache.pool_rows, D, rows))
         return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(p.tiles, p.Hkv * p.layer_count, p.splits);
+    cfg.gridDim = dim3(p.tiles * p.Hkv * p.layer_count * p.splits);
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = smem_bytes<D>();
     cfg.stream = stream;

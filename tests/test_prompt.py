@@ -52,7 +52,7 @@ def _append(N, L, desc=None, **o):
     rows = {n: o.get(n, _rows(N)) for n in "qkv"}
     ref = lambda x: None if x is None else ctypes.byref(x)  # noqa: E731
     g = o.get
-    return L.voxzip_append(ref(d), ref(g("rotary", _rot(N))), g("begin", 0), g("count", 1), g("tokens", 5),
+    return L.voxzip_append(ref(d), ref(g("rotary", _rot(N))), g("begin", 0), g("count", 1), g("tokens", 500),
                            ref(rows["q"]), ref(rows["k"]), ref(rows["v"]), g("positions", P), g("new_pos", P),
                            g("off", P), 0, g("kc", P), g("vc", P), g("score", P), g("pos", P), g("len", P),
                            g("q_out", P), g("ws", P), g("bytes", 1 << 20), None)
@@ -72,12 +72,13 @@ def test_append_is_validated(N):
         assert _append(N, L, **o) == 1, o
     for kw in (dict(head_dim=96), dict(q_heads=7), dict(batch=0), dict(dtype=2), dict(capacity=0)):
         assert _append(N, L, desc=_desc(N, **kw)) == 1, kw
-        assert L.voxzip_append_workspace_size(ctypes.byref(_desc(N, **kw)), 1) == 0
+        assert L.voxzip_append_workspace_size(ctypes.byref(_desc(N, **kw)), 1, 500, 0) == 0
     assert _append(N, L, tokens=0, k=None, v=None) == 0  # no rows: nothing to do
-    assert L.voxzip_append_workspace_size(ctypes.byref(_desc(N)), 4) == 0
-    assert L.voxzip_append_workspace_size(ctypes.byref(_desc(N)), 3) == 256
-    # more layers and heads than a grid has rows of
-    assert _append(N, L, desc=_desc(N, layers=40000), count=40000, **{n: _rows(N, layer=8) for n in "qkv"}) == 2
+    size = lambda *a: L.voxzip_append_workspace_size(ctypes.byref(_desc(N)), *a)  # noqa: E731
+    assert size(4, 500, 0) == 0 and size(3, 500, 0) == 256 == size(3, 500, 499)
+    assert size(3, 500, 6) == 0 == size(3, 5, 0)  # short sequences need none
+    # more tokens of layers than a grid has blocks for
+    assert _append(N, L, desc=_desc(N, layers=2 ** 23), count=2 ** 23, bytes=1 << 40, **{n: _rows(N, layer=8) for n in "qkv"}) == 2
 
 
 def test_rotary_is_validated(N):
@@ -121,7 +122,7 @@ def test_paged_forms_are_validated(N):
 
 
 def test_the_plan_fits_its_workspace(V):
-    """Launches that fill the GPU need none; others a part of the keys each, four tiles of 64 keys or more."""
+    """Launches that fill the GPU need none; others a part of the keys each, a tile of them or more."""
     for dtype in (torch.bfloat16, torch.float32):
         d = V.CacheDesc(4, 2, 32, 4, 128, 46080, dtype)
         size = V.voxzip_prompt_attention_workspace_size
@@ -129,8 +130,8 @@ def test_the_plan_fits_its_workspace(V):
         small = size(d, 1, 1, 1, 46080)
         assert small > 0 and small % 256 == 0
         per_split = 32 * (128 * 4 + 8)
-        assert 2 <= small // per_split <= 46080 // 256
-        assert size(d, 1, 1, 1, 200) == 0  # too few keys to share out
+        assert 2 <= small // per_split <= 46080 // 64
+        assert size(d, 1, 1, 1, 64) == 0  # too few keys to share out
         assert size(d, 1, 1, 1, 0) == small == size(d, 1, 1, 0, 0) == size(d, 1, 1, 7, 10 ** 9)
 
 
