@@ -7,8 +7,8 @@
 //   O_t += P_t V_j           128 x D, fp32, tensor memory
 // m is a row's reference, not its running maximum: it moves (and O_t with it) only when the maximum has grown by more
 // than 2^8 over it, so weights stay at most 1 and nearly every tile leaves O_t to the tensor cores alone.
-// Warps 0-7 and 8-15: a tile's weights, half a row of them per thread (a thread per row took 1500 cycles of a tile's turn,
-// which the other tile's 1000 cycles of products cannot hide). Warps 16 and 19: a tile's matrix instructions (one warp for
+// Warps 0-7 and 8-15: a tile's weights, a quarter of two rows per thread (a thread per row took 1500 cycles, which the
+// other tile's 1000 cycles of products cannot hide; halves of rows had to tell each other their maxima, 300). Warps 16 and 19: a tile's matrix instructions (one warp for
 // both would wait for one tile's weights while the other's lie ready). Warp 17: tile copies into a ring of K and V tiles.
 // Warp 18: what the mask hides of V.
 #include <algorithm>
@@ -40,8 +40,7 @@ template <int D> struct Cfg {
 
 template <int D> struct Shared {
     uint64_t q_full, full[Cfg<D>::kStages], empty[Cfg<D>::kStages], s_full[2], p_full[2], o_full[2], sent[4], clean[4], drained[2];
-    float half[2][2][kTile];  // what the two threads of a row tell each other
-    int gone[2][2][4];        // whether a wait of a weights' warp has given up
+    float sum[2][kTile], top[2][kTile];  // of the rows, when they are done
     TileAt at;
     uint32_t tmem;
     int ok, dead, dirty;
@@ -138,7 +137,6 @@ prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         ptx::mbar_init(&sh.drained[0], 1), ptx::mbar_init(&sh.drained[1], 1);
         ptx::fence_mbar_init();
         sh.dead = 0;
-        for (int i = 0; i < 16; ++i) (&sh.gone[0][0][0])[i] = 0;
         sh.dirty = 0;
     }
     if (warp == kMatrixWarp) tc::alloc(&sh.tmem, C::kColumns);
@@ -355,94 +353,105 @@ prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
             if (lane == 0) ptx::mbar_arrive(&sh.clean[j - max(w.j0, masked0)]);
         }
     } else {
-        // ------------------------------------------------------------ weights, half a row per thread
-        const int t = warp >> 3, hf = warp >> 2 & 1, r = threadIdx.x & (kTile - 1);
-        const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // this warp's 32 lanes
-        const uint32_t s_at = tmem + lanes + t * kTile + hf * 64, p_at = tmem + lanes + t * kTile + hf * 32;
-        constexpr int kCols = D / 2;  // this thread's of the output
-        const uint32_t o_at = tmem + lanes + C::kColO + t * D + hf * kCols;
-        const int pair = 1 + t * 4 + (warp & 3);  // the barrier of the two warps that have the same rows
-        const int32_t token = t * tile_tokens + r / p.G;
-        const int32_t lim = w.first + token;  // keys that the row sees
+        // ------------------------------------------------------------ weights, a quarter of two rows per thread
+        const int t = warp >> 3, hf = warp >> 2 & 1;
+        const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // the 32 lanes that this warp can reach
+        const uint32_t s_at = tmem + (lanes | (uint32_t)hf << 20) + t * kTile;  // 16 of them are its own
+        const uint32_t o_rows = tmem + (lanes | (uint32_t)hf << 20) + C::kColO + t * D;
+        const int own = (warp & 3) * 32 + hf * 16 + lane / 4;  // its first row; the second is 8 on
+        const int pair = 1 + t * 4 + (warp & 3);  // the barrier of the two warps that share the 32 lanes
         const int32_t t_end = t ? w.end1 : w.end0;
-        float m = -INFINITY, sum = 0.f;
+        int32_t lims[2];  // keys that the two rows see
+        float m[2] = {-INFINITY, -INFINITY};
+        float2 sums[2] = {};
+#pragma unroll
+        for (int e = 0; e < 2; ++e) lims[e] = w.first + t * tile_tokens + (own + 8 * e) / p.G;
         bool live = true;
         for (int32_t j = w.j0; j < t_end; ++j) {
-            live = wait_warp(sh, &sh.s_full[t], (j - w.j0) & 1);
+            if (!(live = wait_warp(sh, &sh.s_full[t], (j - w.j0) & 1))) break;
             tc::fence_after();
             float x[2][32];
-#pragma unroll
-            for (int c = 0; c < 2; ++c) tc::ld32(s_at + 32 * c, x[c]);
+            tc::ld_rows(s_at, x[0]);
+            tc::ld_rows(s_at + 64, x[1]);
             tc::wait_ld();
             if (j >= masked0) {
-                const int32_t seen = lim - j * kTile - hf * 64;
 #pragma unroll
                 for (int c = 0; c < 2; ++c)
 #pragma unroll
                     for (int i = 0; i < 32; ++i)
-                        if (32 * c + i >= seen) x[c][i] = -INFINITY;
+                        if (64 * c + i / 4 * 8 + (lane & 3) * 2 + (i & 1) >= lims[i >> 1 & 1] - j * kTile) x[c][i] = -INFINITY;
             }
-            float tops[4];
+            float top[2];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                tops[c] = fmaxf(x[c >> 1][16 * (c & 1)], x[c >> 1][16 * (c & 1) + 1]);
+            for (int e = 0; e < 2; ++e) {
+                float a = fmaxf(x[0][2 * e], x[0][2 * e + 1]), b = fmaxf(x[1][2 * e], x[1][2 * e + 1]);
 #pragma unroll
-                for (int i = 2; i < 16; i += 2)
-                    tops[c] = max3(tops[c], x[c >> 1][16 * (c & 1) + i], x[c >> 1][16 * (c & 1) + i + 1]);
+                for (int i = 4; i < 32; i += 4) {
+                    a = max3(a, x[0][i + 2 * e], x[0][i + 2 * e + 1]);
+                    b = max3(b, x[1][i + 2 * e], x[1][i + 2 * e + 1]);
+                }
+                top[e] = fmaxf(a, b);
             }
-            float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * p.scale_log2;
-            sh.half[t][hf][r] = top;
-            if (!live) sh.gone[t][hf][warp & 3] = 1;
-            pair_barrier(pair);
-            top = fmaxf(top, sh.half[t][hf ^ 1][r]);
-            // A warp whose wait gave up comes as far as this, so that the two leave together.
-            live = live && !*reinterpret_cast<volatile int *>(&sh.gone[t][hf ^ 1][warp & 3]);
-            if (!live) break;
-            const bool grown = top > m + kSlack;
-            if (__any_sync(0xffffffffu, grown)) {  // in both warps, or in neither
-                const float keep = grown ? ex2(m - top) : 1.f;  // a row does not depend on its neighbours
-                if (grown) m = top;
-                sum *= keep;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], 1));
+                top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], 2)) * p.scale_log2;
+            }
+            const bool grown[2] = {top[0] > m[0] + kSlack, top[1] > m[1] + kSlack};
+            if (__any_sync(0xffffffffu, grown[0] || grown[1])) {
+                float keep[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    keep[e] = grown[e] ? ex2(m[e] - top[e]) : 1.f;  // a row does not depend on its neighbours
+                    if (grown[e]) m[e] = top[e];
+                    sums[e].x *= keep[e], sums[e].y *= keep[e];
+                }
                 if (j > w.j0) {  // the products of the tiles before are done: the logits' commit came after theirs
-                    float o[16];
+                    float o[8];
 #pragma unroll 1
-                    for (int c = 0; c < kCols; c += 16) {
-                        tc::ld16(o_at + c, o);
+                    for (int c = 0; c < D; c += 16) {
+                        tc::ld_rows16(o_rows + c, o);
                         tc::wait_ld();
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) o[i] *= keep;
-                        tc::st16(o_at + c, reinterpret_cast<uint32_t(&)[16]>(o));
+                        for (int i = 0; i < 8; ++i) o[i] *= keep[i >> 1 & 1];
+                        tc::st_rows16(o_rows + c, o);
                     }
                 }
             }
-            const float ref = m == -INFINITY ? 0.f : -m - kSlack;
-            float2 s2[2] = {};
+            const float ref[2] = {m[0] == -INFINITY ? 0.f : -m[0] - kSlack, m[1] == -INFINITY ? 0.f : -m[1] - kSlack};
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
                 uint32_t u[16];
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const float2 e = fma2(x[c][2 * i], x[c][2 * i + 1], p.scale_log2, ref);
+                    const float2 e = fma2(x[c][2 * i], x[c][2 * i + 1], p.scale_log2, ref[i & 1]);
                     const float a = ex2(e.x), b = ex2(e.y);
-                    add2(s2[i & 1], a, b);
+                    add2(sums[i & 1], a, b);
                     u[i] = ptx::pack_bf16(a, b);
                 }
-                tc::st16(p_at + 16 * c, u);
+                tc::st_rows(s_at + 32 * c, u);
             }
             tc::wait_st();
             tc::fence_before();
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive(&sh.p_full[t]);
-            sum += (s2[0].x + s2[0].y) + (s2[1].x + s2[1].y);
         }
-        // ------------------------------------------------------------ results
+        // ------------------------------------------------------------ results, half a row per thread
+        constexpr int kCols = D / 2;
+        const uint32_t o_at = tmem + lanes + C::kColO + t * D + hf * kCols;
+        const int r = threadIdx.x & (kTile - 1);
+        const int32_t token = t * tile_tokens + r / p.G, lim = w.first + token;
         const bool any = t_end > w.j0;
-        if (any && live) {
-            live = wait_warp(sh, &sh.o_full[t], 0);
-            sh.half[t][hf][r] = sum;
-            pair_barrier(pair);
-            sum += sh.half[t][hf ^ 1][r];
+        if (live && any) live = wait_warp(sh, &sh.o_full[t], 0);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            float sum = sums[e].x + sums[e].y;
+            sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+            sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+            if ((lane & 3) == 0) sh.sum[t][own + 8 * e] = sum, sh.top[t][own + 8 * e] = m[e];
         }
+        pair_barrier(pair);  // both warps come, whatever their waits said
+        const float sum = sh.sum[t][r], m_row = sh.top[t][r];
         tc::fence_after();
         const bool mine = live && token < at.rows && r < tile_tokens * p.G;
         const int64_t row = ((int64_t)l * p.T + at.t0 + token) * p.Hq + h * p.G + r % p.G;
@@ -451,7 +460,7 @@ prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         const bool dirty = *reinterpret_cast<volatile int *>(&sh.dirty);
         const int64_t all = (int64_t)p.layer_count * p.T * p.Hq;
         if (mine && p.splits > 1 && hf == 0)
-            p.part_ml[split * all + row] = make_float2(!any || m == -INFINITY ? -INFINITY : m + kSlack, any ? sum : 0.f);
+            p.part_ml[split * all + row] = make_float2(!any || m_row == -INFINITY ? -INFINITY : m_row + kSlack, any ? sum : 0.f);
         if (live && any) {
 #pragma unroll
             for (int c = 0; c < kCols / 32; ++c) {

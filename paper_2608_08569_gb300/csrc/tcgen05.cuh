@@ -39,22 +39,43 @@ __device__ __forceinline__ void ld32(uint32_t addr, float (&r)[32]) {
           "=r"(u[25]), "=r"(u[26]), "=r"(u[27]), "=r"(u[28]), "=r"(u[29]), "=r"(u[30]), "=r"(u[31])
         : "r"(addr));
 }
-__device__ __forceinline__ void ld16(uint32_t addr, float (&r)[16]) {
+// Half of a warp's lanes (16 rows; the address names the first), 64 columns, four threads to a row: thread i has, of each
+// block b of 8 columns, columns 2 (i % 4) and the next of row i / 4 in r[4 b] and r[4 b + 1], and of row i / 4 + 8 in the
+// other two.
+__device__ __forceinline__ void ld_rows(uint32_t addr, float (&r)[32]) {
     uint32_t *u = reinterpret_cast<uint32_t *>(r);
     asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        "tcgen05.ld.sync.aligned.16x256b.x8.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
         : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]),
-          "=r"(u[9]), "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15])
+          "=r"(u[9]), "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15]), "=r"(u[16]),
+          "=r"(u[17]), "=r"(u[18]), "=r"(u[19]), "=r"(u[20]), "=r"(u[21]), "=r"(u[22]), "=r"(u[23]), "=r"(u[24]),
+          "=r"(u[25]), "=r"(u[26]), "=r"(u[27]), "=r"(u[28]), "=r"(u[29]), "=r"(u[30]), "=r"(u[31])
         : "r"(addr));
 }
-__device__ __forceinline__ void st16(uint32_t addr, const uint32_t (&u)[16]) {
+// The same rows and threads, 32 columns of one word each: of each block b of 4, column i % 4 of row i / 4 from u[2 b], of
+// row i / 4 + 8 from u[2 b + 1]. Pairs of the logits that ld_rows gave lie where their columns' halves are.
+__device__ __forceinline__ void st_rows(uint32_t addr, const uint32_t (&u)[16]) {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+        "tcgen05.st.sync.aligned.16x128b.x8.b32 [%0], "
         "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(addr),
         "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]), "r"(u[8]), "r"(u[9]),
         "r"(u[10]), "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]), "r"(u[15])
         : "memory");
+}
+// 16 columns in ld_rows' layout, both ways (an output's).
+__device__ __forceinline__ void ld_rows16(uint32_t addr, float (&r)[8]) {
+    uint32_t *u = reinterpret_cast<uint32_t *>(r);
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7])
+                 : "r"(addr));
+}
+__device__ __forceinline__ void st_rows16(uint32_t addr, const float (&r)[8]) {
+    const uint32_t *u = reinterpret_cast<const uint32_t *>(r);
+    asm volatile("tcgen05.st.sync.aligned.16x256b.x2.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(addr), "r"(u[0]),
+                 "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7])
+                 : "memory");
 }
 
 // ---------------------------------------------------------------- descriptors
