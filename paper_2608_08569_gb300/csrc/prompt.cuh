@@ -66,13 +66,13 @@ struct PromptAttn {
     int64_t kv_rows;  // rows of the K and V tensors (checked builds)
 };
 
-// A CTA's tile, split, kv-head and layer. CTAs start in order: the tiles that see the most keys first, of all heads, so
-// that the last ones to start are short.
+// The i-th piece of a launch's work: its tile, split, kv-head and layer. The tiles that see the most keys come first, of
+// all heads, so that the last ones to start are short.
 struct CtaAt {
     int32_t x, split, h, l;
 };
-__device__ __forceinline__ CtaAt cta_at(const PromptAttn &p) {
-    const uint32_t units = p.Hkv * p.layer_count, i = blockIdx.x;
+__device__ __forceinline__ CtaAt cta_at(const PromptAttn &p, int64_t piece) {
+    const uint32_t units = p.Hkv * p.layer_count, i = (uint32_t)piece;
     const uint32_t u = i % units, rest = i / units;
     return CtaAt{(int32_t)(rest / p.splits), (int32_t)(rest % p.splits), (int32_t)(u % p.Hkv), (int32_t)(u / p.Hkv)};
 }

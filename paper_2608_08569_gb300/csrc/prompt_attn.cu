@@ -83,7 +83,7 @@ __global__ void __launch_bounds__(256) prompt_rows_kernel(const PromptAttn p) {
     extern __shared__ __align__(16) uint8_t raw[];
     Smem<D> &sm = *reinterpret_cast<Smem<D> *>(raw);
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
-    const CtaAt cta = cta_at(p);
+    const CtaAt cta = cta_at(p, blockIdx.x);
     const int h = cta.h, l = cta.l, s = cta.split;
     ptx::grid_dependency_wait();
     ptx::launch_dependents();  // the join may take its place on the SMs

@@ -7,6 +7,9 @@
 //   O_t += P_t V_j           128 x D, fp32, tensor memory
 // m is a row's reference, not its running maximum: it moves (and O_t with it) only when the maximum has grown by more
 // than 2^8 over it, so weights stay at most 1 and nearly every tile leaves O_t to the tensor cores alone.
+// A CTA that is done takes the place of one that has not started: the copies and logits of its next tile begin while the
+// results of the last are on their way out (10-min prompt 380 us against 397, 32 ragged ones 5.0 ms against 5.3; a fixed
+// share for each CTA 401 us).
 // Warps 0-7 and 8-15: a tile's weights, a quarter of two rows per thread (a thread per row took 1500 cycles, which the
 // other tile's 1000 cycles of products cannot hide; halves of rows had to tell each other their maxima, 300). Warps 16 and 19: a tile's matrix instructions (one warp for
 // both would wait for one tile's weights while the other's lie ready). Warp 17: tile copies into a ring of K and V tiles.
@@ -38,17 +41,34 @@ template <int D> struct Cfg {
     static constexpr uint32_t kColumns = 512;
 };
 
+// A tile of the launch: 256 rows and the keys of its split.
+struct Item {
+    int32_t valid;           // 0: there is none left
+    int32_t h, l, split, t0, rows;  // kv-head, layer; first packed token, tokens
+    int32_t first;           // keys that its first token sees (may be < 1)
+    int32_t most;            // keys that its last one sees
+    int32_t j0, end0, end1;  // key tiles [j0, end0) and [j0, end1) of the two row tiles
+    int32_t dirty;           // the mask warp has taken elements out of V
+    int64_t cu;              // cache unit
+
+    __device__ __forceinline__ int32_t end() const { return max(end0, end1); }
+    // From this key tile on some row does not see all keys.
+    __device__ __forceinline__ int32_t masked0() const { return max(j0, max(0, first) / kTile); }
+};
+
 template <int D> struct Shared {
-    uint64_t q_full, full[Cfg<D>::kStages], empty[Cfg<D>::kStages], s_full[2], p_full[2], o_full[2], sent[4], clean[4], drained[2];
+    uint64_t item_full[2], item_empty[2], q_full, q_empty, full[Cfg<D>::kStages], empty[Cfg<D>::kStages], s_full[2], p_full[2],
+        o_full[2], o_empty[2], sent[2][4], clean[2][4], pair[8], drained[2], next_full;
+    alignas(16) uint4 next;  // the hardware's answer: a CTA that need not start
+    Item item[2];
     float sum[2][kTile], top[2][kTile];  // of the rows, when they are done
-    TileAt at;
     uint32_t tmem;
-    int ok, dead, dirty;
+    int dead;
 };
 
 // The tiles start on a multiple of 1024 behind Shared; a CTA's memory does too, but for what the compiler puts first.
 template <int D> constexpr size_t smem_bytes() { return 3072 + Cfg<D>::kBytes; }
-static_assert(sizeof(Shared<128>) <= 2560 && smem_bytes<128>() <= 232448, "what an SM has");
+static_assert(sizeof(Shared<128>) <= 3072 && sizeof(Shared<64>) <= 3072 && smem_bytes<128>() <= 232448, "what an SM has");
 
 // A bounded wait; once one has given up in a CTA, all do.
 template <int D> __device__ __forceinline__ bool wait(Shared<D> &sh, uint64_t *bar, uint32_t parity) {
@@ -64,9 +84,6 @@ template <int D> __device__ __forceinline__ bool wait(Shared<D> &sh, uint64_t *b
 template <int D> __device__ __forceinline__ bool wait_warp(Shared<D> &sh, uint64_t *bar, uint32_t parity) {
     return __all_sync(0xffffffffu, wait(sh, bar, parity));
 }
-
-// A barrier of two warps; both come, whatever their waits said.
-__device__ __forceinline__ void pair_barrier(int id) { asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory"); }
 
 __device__ __forceinline__ float ex2(float x) {
     float y;
@@ -102,13 +119,29 @@ __device__ __forceinline__ void tma_load_4d(void *dst, const CUtensorMap *map, i
         : "memory");
 }
 
-// What a CTA works on.
-struct Work {
-    int32_t first;       // keys that its first token sees (may be < 1)
-    int32_t most;        // keys that its last one sees
-    int32_t j0, end0, end1;  // key tiles [j0, end0) and [j0, end1) of the two row tiles
-    int64_t cu;          // cache unit
-};
+// Asks for a CTA of this launch that has not started, which then will not; the answer comes by `bar`.
+__device__ __forceinline__ void ask_next(uint4 *answer, uint64_t *bar) {
+    ptx::mbar_arrive_expect_tx(bar, 16);
+    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(
+                     ptx::smem_u32(answer)),
+                 "r"(ptx::smem_u32(bar))
+                 : "memory");
+}
+// Whether there was one, and its blockIdx.x.
+__device__ __forceinline__ bool canceled(const uint4 *answer, int64_t *x) {
+    uint32_t ok, cta;
+    asm volatile(
+        "{\n\t.reg .b128 a;\n\t.reg .pred p;\n\t.reg .b64 lo, hi;\n\t"
+        "ld.shared.v2.b64 {lo, hi}, [%2];\n\tmov.b128 a, {lo, hi};\n\t"
+        "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, a;\n\tselp.u32 %0, 1, 0, p;\n\tmov.u32 %1, 0;\n\t"
+        "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, a;\n\t}"
+        : "=r"(ok), "=r"(cta)
+        : "r"(ptx::smem_u32(answer))
+        : "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // read before the next answer is written
+    *x = cta;
+    return ok != 0;
+}
 
 template <int D, bool kPaged>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -125,19 +158,19 @@ prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
     uint8_t *tiles = raw + front;
     uint8_t *q_smem = tiles, *ring = tiles + 2 * C::kTileBytes;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;  // uniform for the compiler too
-    const CtaAt cta = cta_at(p);
-    const int h = cta.h, l = cta.l, split = cta.split;
-
     if (threadIdx.x == 0) {
-        ptx::mbar_init(&sh.q_full, 1);
+        for (int i = 0; i < 2; ++i) {
+            ptx::mbar_init(&sh.item_full[i], 1), ptx::mbar_init(&sh.item_empty[i], kMatrixWarp + 3);
+            ptx::mbar_init(&sh.s_full[i], 1), ptx::mbar_init(&sh.p_full[i], 8);
+            ptx::mbar_init(&sh.o_full[i], 1), ptx::mbar_init(&sh.o_empty[i], 8);
+            for (int e = 0; e < 4; ++e) ptx::mbar_init(&sh.sent[i][e], 1), ptx::mbar_init(&sh.clean[i][e], 1);
+            ptx::mbar_init(&sh.drained[i], 1);
+        }
+        ptx::mbar_init(&sh.q_full, 1), ptx::mbar_init(&sh.q_empty, 2), ptx::mbar_init(&sh.next_full, 1);
         for (int i = 0; i < C::kStages; ++i) ptx::mbar_init(&sh.full[i], 1), ptx::mbar_init(&sh.empty[i], 2);
-        for (int t = 0; t < 2; ++t)
-            ptx::mbar_init(&sh.s_full[t], 1), ptx::mbar_init(&sh.p_full[t], 8), ptx::mbar_init(&sh.o_full[t], 1);
-        for (int i = 0; i < 4; ++i) ptx::mbar_init(&sh.sent[i], 1), ptx::mbar_init(&sh.clean[i], 1);
-        ptx::mbar_init(&sh.drained[0], 1), ptx::mbar_init(&sh.drained[1], 1);
+        for (int i = 0; i < 8; ++i) ptx::mbar_init(&sh.pair[i], 2);
         ptx::fence_mbar_init();
         sh.dead = 0;
-        sh.dirty = 0;
     }
     if (warp == kMatrixWarp) tc::alloc(&sh.tmem, C::kColumns);
     if (warp == kCopyWarp && lane == 0) {
@@ -145,212 +178,272 @@ prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         ptx::prefetch_tmap(&map_k);
         ptx::prefetch_tmap(&map_v);
     }
-    ptx::grid_dependency_wait();
-    ptx::launch_dependents();  // the join may take its place on the SMs
-    if (warp == 0) {
-        TileAt at;
-        const bool found = find_tile(p, cta, at);
-        if (lane == 0) {
-            sh.ok = found;
-            if (found) sh.at = at;
-        }
-    }
     tc::fence_before();
     __syncthreads();
     tc::fence_after();
+    ptx::grid_dependency_wait();
+    ptx::launch_dependents();  // the join may take its place on the SMs
     const uint32_t tmem = __shfl_sync(0xffffffffu, sh.tmem, 0);
-    bool ok = sh.ok;
-    const TileAt at = sh.at;
-    Work w = {};
     const int tile_tokens = kTile / p.G;
-    if (ok) {
-        w.cu = ((int64_t)at.b * p.L + p.layer_begin + l) * p.Hkv + h;
-        const int32_t n = at.n;
-        if (n < 0 || n > p.C) {
-            if (threadIdx.x == 0) raise_status(p.status, VOXZIP_DEV_CAPACITY);
-            ok = false;
-        } else {
-            w.first = n - at.m + at.before + 1;
-            w.most = max(0, w.first + at.rows - 1);
-            // the keys of this split, of those that the CTA's last token sees; row tile 0 ends with its own last token's
-            const int32_t total = (w.most + kTile - 1) / kTile, per = (total + p.splits - 1) / p.splits;
-            w.j0 = min(total, split * per);
-            const int32_t j1 = min(total, w.j0 + per);
-            const int32_t most0 = max(0, w.first + min(tile_tokens, at.rows) - 1);
-            w.end0 = max(w.j0, min(j1, (most0 + kTile - 1) / kTile));
-            w.end1 = at.rows > tile_tokens ? j1 : w.j0;
-        }
-    }
-    const int32_t end = max(w.end0, w.end1);
-    const int32_t masked0 = max(0, w.first) / kTile;  // from this key tile on some row does not see all keys
+    bool live = true;
 
-    if (!ok) {
-        // nothing to do
-    } else if (warp == kCopyWarp) {
-        // ------------------------------------------------------------ copies
-        bool live = true;
-        int issued = 0;
-        if (lane == 0 && end > w.j0) {
-            const uint32_t bytes = p.G * tile_tokens * 128 * C::kHalves;
-            const int both = at.rows > tile_tokens ? 2 : 1;
-            ptx::mbar_arrive_expect_tx(&sh.q_full, bytes * both);
-            for (int t = 0; t < both; ++t)
-                for (int c = 0; c < C::kHalves; ++c)
-                    tma_load_4d(q_smem + t * C::kTileBytes + c * C::kHalfBytes, &map_q, 64 * c, h * p.G,
-                                at.t0 + t * tile_tokens, l, &sh.q_full);
-        }
-        int32_t pages = 0, pages_at = INT32_MIN;  // this lane's of 32 consecutive page indices
-        for (int32_t j = w.j0; j < end && live; ++j) {
-            int32_t row[2];
-            if constexpr (kPaged) {
-                constexpr int kPages = kTile / kPageTokens;
-                const int32_t first_page = j * kPages;
-                if (first_page >= pages_at + 32 || pages_at == INT32_MIN) {
-                    pages_at = first_page;
-                    const int32_t at_page = first_page + lane;
-                    pages = -1;
-                    if (at_page * kPageTokens < w.most) {
-                        pages = p.cache.pv.table[w.cu * p.cache.pv.max_pages + at_page];
-                        if (pages < 0 || (int64_t)pages * kPageTokens >= p.cache.pool_rows) {
-                            raise_status(p.status, VOXZIP_DEV_CAPACITY);
-                            pages = -1;
+    if (warp == kCopyWarp) {
+        // ------------------------------------------------------------ items and copies
+        const int64_t items = (int64_t)p.tiles * p.splits * p.Hkv * p.layer_count;
+        int issued = 0, queries = 0, given = 0;
+        // Its own, then those of CTAs that have not started: the hardware gives them out in order.
+        int64_t i = blockIdx.x;
+        uint32_t asked = 0;
+        bool more = true;
+        for (bool first = true; live; first = false) {
+            if (!first) {
+                if (!(live = wait_warp(sh, &sh.next_full, (asked - 1) & 1))) break;
+                more = canceled(&sh.next, &i);
+                __syncwarp();
+            }
+            if (more) {
+                if (lane == 0) ask_next(&sh.next, &sh.next_full);
+                ++asked;
+            }
+            Item w = {};
+            if (more) {
+                if (i >= items) continue;
+                const CtaAt cta = cta_at(p, i);
+                TileAt at;
+                if (!find_tile(p, cta, at)) continue;
+                if (at.n < 0 || at.n > p.C) {
+                    if (lane == 0) raise_status(p.status, VOXZIP_DEV_CAPACITY);
+                    continue;
+                }
+                w.valid = 1;
+                w.h = cta.h, w.l = cta.l, w.split = cta.split, w.t0 = at.t0, w.rows = at.rows;
+                w.cu = ((int64_t)at.b * p.L + p.layer_begin + cta.l) * p.Hkv + cta.h;
+                w.first = at.n - at.m + at.before + 1;
+                w.most = max(0, w.first + at.rows - 1);
+                // the keys of this split, of those that the last token sees; row tile 0 ends with its own last token's
+                const int32_t total = (w.most + kTile - 1) / kTile, per = (total + p.splits - 1) / p.splits;
+                w.j0 = min(total, cta.split * per);
+                const int32_t j1 = min(total, w.j0 + per);
+                const int32_t most0 = max(0, w.first + min(tile_tokens, at.rows) - 1);
+                w.end0 = max(w.j0, min(j1, (most0 + kTile - 1) / kTile));
+                w.end1 = at.rows > tile_tokens ? j1 : w.j0;
+            }
+            const int place = given & 1;
+            if (given >= 2 && !(live = wait_warp(sh, &sh.item_empty[place], (given >> 1 & 1) ^ 1))) break;
+            if (lane == 0) {
+                sh.item[place] = w;
+                ptx::mbar_arrive(&sh.item_full[place]);
+            }
+            __syncwarp();
+            ++given;
+            if (!w.valid) break;
+            const int32_t end = w.end(), masked0 = w.masked0();
+            if (end > w.j0) {
+                if (queries > 0 && !(live = wait_warp(sh, &sh.q_empty, (queries - 1) & 1))) break;
+                ++queries;
+                if (lane == 0) {
+                    const uint32_t bytes = p.G * tile_tokens * 128 * C::kHalves;
+                    const int both = w.rows > tile_tokens ? 2 : 1;
+                    ptx::mbar_arrive_expect_tx(&sh.q_full, bytes * both);
+                    for (int t = 0; t < both; ++t)
+                        for (int c = 0; c < C::kHalves; ++c)
+                            tma_load_4d(q_smem + t * C::kTileBytes + c * C::kHalfBytes, &map_q, 64 * c, w.h * p.G,
+                                        w.t0 + t * tile_tokens, w.l, &sh.q_full);
+                }
+            }
+            int32_t pages = 0, pages_at = INT32_MIN;  // this lane's of 32 consecutive page indices
+            for (int32_t j = w.j0; j < end && live; ++j) {
+                int32_t row[2];
+                if constexpr (kPaged) {
+                    constexpr int kPages = kTile / kPageTokens;
+                    const int32_t first_page = j * kPages;
+                    if (pages_at == INT32_MIN || first_page >= pages_at + 32) {
+                        pages_at = first_page;
+                        const int32_t at_page = first_page + lane;
+                        pages = -1;
+                        if (at_page * kPageTokens < w.most) {
+                            pages = p.cache.pv.table[w.cu * p.cache.pv.max_pages + at_page];
+                            if (pages < 0 || (int64_t)pages * kPageTokens >= p.cache.pool_rows) {
+                                raise_status(p.status, VOXZIP_DEV_CAPACITY);
+                                pages = -1;
+                            }
                         }
                     }
-                }
 #pragma unroll
-                for (int i = 0; i < kPages; ++i) {
-                    const int32_t page = __shfl_sync(0xffffffffu, pages, first_page - pages_at + i);
-                    row[i] = page < 0 ? (int32_t)p.cache.pool_rows : page * kPageTokens;  // outside: zeros
-                }
-            } else {
-                row[0] = (int32_t)(w.cu * p.C + (int64_t)j * kTile);
-                row[1] = row[0] + kTile / 2;
-                (void)VOXZIP_IN_RANGE(p.status, row[0] >= 0 && row[0] < p.kv_rows);
-            }
-            if (lane == 0) {
-                for (int kv = 0; kv < 2 && live; ++kv) {
-                    const int slot = issued % C::kStages;
-                    live = issued < C::kStages || wait(sh, &sh.empty[slot], (issued / C::kStages & 1) ^ 1);
-                    if (!live) break;
-                    const CUtensorMap *map = kv ? &map_v : &map_k;
-                    uint8_t *to = ring + slot * C::kTileBytes;
-                    ptx::mbar_arrive_expect_tx(&sh.full[slot], C::kTileBytes);
-                    for (int c = 0; c < C::kHalves; ++c) {
-                        ptx::tma_load_2d(to + c * C::kHalfBytes, map, 64 * c, row[0], &sh.full[slot]);
-                        if (kPaged)
-                            ptx::tma_load_2d(to + c * C::kHalfBytes + C::kHalfBytes / 2, map, 64 * c, row[1], &sh.full[slot]);
+                    for (int i = 0; i < kPages; ++i) {
+                        const int32_t page = __shfl_sync(0xffffffffu, pages, first_page - pages_at + i);
+                        row[i] = page < 0 ? (int32_t)p.cache.pool_rows : page * kPageTokens;  // outside: zeros
                     }
-                    ++issued;
-                    if (kv && j >= masked0) ptx::mbar_arrive(&sh.sent[j - max(w.j0, masked0)]);
+                } else {
+                    row[0] = (int32_t)(w.cu * p.C + (int64_t)j * kTile);
+                    row[1] = row[0] + kTile / 2;
+                    (void)VOXZIP_IN_RANGE(p.status, row[0] >= 0 && row[0] < p.kv_rows);
                 }
+                if (lane == 0) {
+                    for (int kv = 0; kv < 2 && live; ++kv) {
+                        const int slot = issued % C::kStages;
+                        live = issued < C::kStages || wait(sh, &sh.empty[slot], (issued / C::kStages & 1) ^ 1);
+                        if (!live) break;
+                        const CUtensorMap *map = kv ? &map_v : &map_k;
+                        uint8_t *to = ring + slot * C::kTileBytes;
+                        ptx::mbar_arrive_expect_tx(&sh.full[slot], C::kTileBytes);
+                        for (int c = 0; c < C::kHalves; ++c) {
+                            ptx::tma_load_2d(to + c * C::kHalfBytes, map, 64 * c, row[0], &sh.full[slot]);
+                            if (kPaged)
+                                ptx::tma_load_2d(to + c * C::kHalfBytes + C::kHalfBytes / 2, map, 64 * c, row[1],
+                                                 &sh.full[slot]);
+                        }
+                        ++issued;
+                        if (kv && j >= masked0) ptx::mbar_arrive(&sh.sent[place][j - masked0]);
+                    }
+                }
+                live = __shfl_sync(0xffffffffu, live, 0);
             }
-            live = __shfl_sync(0xffffffffu, live, 0);
         }
-        if (lane == 0 && !live)  // a wait gave up: no copy is left in flight behind this CTA
+        if (lane == 0 && !live) {  // a wait gave up: no copy is left in flight behind this CTA
             for (int i = max(0, issued - C::kStages); i < issued; ++i)
                 ptx::mbar_wait_bounded(&sh.full[i % C::kStages], i / C::kStages & 1, kPolls);
+            if (queries > 0) ptx::mbar_wait_bounded(&sh.q_full, (queries - 1) & 1, kPolls);
+            if (asked > 0) ptx::mbar_wait_bounded(&sh.next_full, (asked - 1) & 1, kPolls);
+        }
     } else if (warp == kMatrixWarp || warp == kMatrixWarp1) {
-        // ------------------------------------------------------------ matrix instructions, a thread per row tile
+        // ------------------------------------------------------------ matrix instructions, a warp per row tile
+        constexpr uint32_t kInstS = tc::instruction(kTile, false), kInstO = tc::instruction(D, true);
         const int t = warp == kMatrixWarp1;
-        const int32_t t_end = t ? w.end1 : w.end0;
-        if (end > w.j0) {
-            constexpr uint32_t kInstS = tc::instruction(kTile, false), kInstO = tc::instruction(D, true);
-            const uint32_t q_at = ptx::smem_u32(q_smem) + t * C::kTileBytes, ring_at = ptx::smem_u32(ring);
-            const uint32_t s_at = tmem + t * kTile, o_at = tmem + C::kColO + t * D;
-            int slot = 0, phase = 0;  // of the ring's next tile
-            auto logits = [&](int k_slot) {
-                const uint32_t k_at = ring_at + k_slot * C::kTileBytes;
+        const uint32_t q_at = ptx::smem_u32(q_smem) + t * C::kTileBytes, ring_at = ptx::smem_u32(ring);
+        const uint32_t s_at = tmem + t * kTile, o_at = tmem + C::kColO + t * D;
+        int slot = 0, phase = 0;  // of the ring's next tile
+        uint32_t weights_phase = 0, results = 0, queries_phase = 0, clean_phase[2] = {0, 0};
+        auto advance = [&] {
+            if (++slot == C::kStages) slot = 0, phase ^= 1;
+        };
+        auto logits = [&](int k_slot) {
+            const uint32_t k_at = ring_at + k_slot * C::kTileBytes;
 #pragma unroll
-                for (int k = 0; k < D / 16; ++k) {
-                    const uint32_t off = k / 4 * C::kHalfBytes + k % 4 * 32;
-                    tc::mma(s_at, tc::operand(q_at + off, 0), tc::operand(k_at + off, 0), kInstS, k > 0);
-                }
-                tc::commit(&sh.s_full[t]);
-            };
-            // Gives a tile of the ring back. One that this warp has no use for goes back only when it has come: before
-            // that, the barrier's phase is that of its last use.
-            auto release = [&](int at_slot, bool used) {
-                if (used)
-                    tc::commit(&sh.empty[at_slot]);
-                else if (lane == 0)
-                    ptx::mbar_arrive(&sh.empty[at_slot]);
-            };
-            bool live = wait_warp(sh, &sh.q_full, 0) && wait_warp(sh, &sh.full[0], 0);
-            if (live) {
-                tc::fence_after();
-                if (w.j0 < t_end) logits(0);
-                release(0, w.j0 < t_end);
-                slot = 1;
+            for (int k = 0; k < D / 16; ++k) {
+                const uint32_t off = k / 4 * C::kHalfBytes + k % 4 * 32;
+                tc::mma(s_at, tc::operand(q_at + off, 0), tc::operand(k_at + off, 0), kInstS, k > 0);
             }
-            for (int32_t j = w.j0; j < end && live; ++j) {
+            tc::commit(&sh.s_full[t]);
+        };
+        // Gives memory back. What this warp has no use for goes back only when it has come: before that, the barrier's
+        // phase is that of its last use.
+        auto release = [&](uint64_t *bar, bool used) {
+            if (used)
+                tc::commit(bar);
+            else if (lane == 0)
+                ptx::mbar_arrive(bar);
+        };
+        for (int n = 0; live; ++n) {
+            const int place = n & 1;
+            if (!(live = wait_warp(sh, &sh.item_full[place], n >> 1 & 1))) break;
+            const Item &w = sh.item[place];
+            const int32_t valid = w.valid, j0 = w.j0, t_end = t ? w.end1 : w.end0, end = w.end(), masked0 = w.masked0();
+            if (!valid) break;
+            if (end == j0) {
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(&sh.item_empty[place]);
+                continue;
+            }
+            live = wait_warp(sh, &sh.q_full, queries_phase) && wait_warp(sh, &sh.full[slot], phase);
+            if (!live) break;
+            queries_phase ^= 1;
+            tc::fence_after();
+            if (j0 < t_end) logits(slot);
+            release(&sh.empty[slot], j0 < t_end);
+            if (j0 + 1 >= t_end) release(&sh.q_empty, j0 < t_end);
+            advance();
+            for (int32_t j = j0; j < end; ++j) {
                 // V of this key tile and K of the next, before the weights: their copies are long done
                 const int v_slot = slot;
                 live = wait_warp(sh, &sh.full[slot], phase);
-                if (++slot == C::kStages) slot = 0, phase ^= 1;
+                advance();
                 const int k_slot = slot;
                 if (live && j + 1 < end) {
                     live = wait_warp(sh, &sh.full[slot], phase);
-                    if (++slot == C::kStages) slot = 0, phase ^= 1;
+                    advance();
                 }
-                if (live && j >= masked0) live = wait_warp(sh, &sh.clean[j - max(w.j0, masked0)], 0);
+                if (live && j >= masked0)
+                    live = wait_warp(sh, &sh.clean[place][j - masked0], clean_phase[place] >> (j - masked0) & 1);
                 if (live && j < t_end) {
-                    if (!(live = wait_warp(sh, &sh.p_full[t], (j - w.j0) & 1))) break;
+                    live = wait_warp(sh, &sh.p_full[t], weights_phase);
+                    weights_phase ^= 1;
+                    if (live && j == j0 && results > 0) live = wait_warp(sh, &sh.o_empty[t], (results - 1) & 1);
+                    if (!live) break;
                     tc::fence_after();
                     const uint32_t v_at = ring_at + v_slot * C::kTileBytes;
 #pragma unroll
                     for (int k = 0; k < kTile / 16; ++k)
                         tc::mma_ta(o_at, s_at + k * 8, tc::operand(v_at + k * 16 * 128, C::kHalfBytes), kInstO,
-                                   j > w.j0 || k > 0);
+                                   j > j0 || k > 0);
                     if (j + 1 < t_end) logits(k_slot);
                     if (j + 1 == t_end) tc::commit(&sh.o_full[t]);
                 }
                 if (!live) break;
-                release(v_slot, j < t_end);
-                if (j + 1 < end) release(k_slot, j + 1 < t_end);
+                release(&sh.empty[v_slot], j < t_end);
+                if (j + 1 < end) release(&sh.empty[k_slot], j + 1 < t_end);
+                if (j + 2 == t_end) tc::commit(&sh.q_empty);
             }
-            if (!live) {  // a wait gave up: what was issued ends before the tensor memory goes
-                tc::commit(&sh.drained[t]);
-                ptx::mbar_wait_bounded(&sh.drained[t], 0, kPolls);
-                raise_status(p.status, VOXZIP_DEV_TIMEOUT);
-            }
+            if (j0 < t_end) ++results;
+            clean_phase[place] ^= (1u << max(0, end - masked0)) - 1;
+            if (live && lane == 0) ptx::mbar_arrive(&sh.item_empty[place]);
+        }
+        if (!live) {  // a wait gave up: what was issued ends before the tensor memory goes
+            tc::commit(&sh.drained[t]);
+            ptx::mbar_wait_bounded(&sh.drained[t], 0, kPolls);
+            raise_status(p.status, VOXZIP_DEV_TIMEOUT);
         }
     } else if (warp == kMaskWarp) {
         // ------------------------------------------------------------ V behind the mask
         // A weight of 0 times an infinity or a NaN would be NaN in rows that do not see the key. Rows that nobody sees
         // become 0. In rows that some see such elements do, and join the result at the end.
-        for (int32_t j = max(w.j0, masked0); j < end; ++j) {
-            const int i = 2 * (j - w.j0) + 1, slot = i % C::kStages;
-            // only once its copy is asked for is a phase of the slot's barrier this tile's
-            if (!wait_warp(sh, &sh.sent[j - max(w.j0, masked0)], 0)) break;
-            if (!wait_warp(sh, &sh.full[slot], i / C::kStages & 1)) break;
-            uint8_t *tile = ring + slot * C::kTileBytes;
-            const int32_t key0 = j * kTile;
-            const int r0 = max(0, w.first - key0), r1 = min(kTile, max(0, w.most - key0));
-            bool found = false;
-            for (int i = r0 * 8 + lane; i < kTile * 8; i += 32) {
+        int tiles_before = 0;  // of the ring
+        uint32_t sent_phase[2] = {0, 0};
+        for (int n = 0; live; ++n) {
+            const int place = n & 1;
+            if (!(live = wait_warp(sh, &sh.item_full[place], n >> 1 & 1))) break;
+            Item &w = sh.item[place];
+            if (!w.valid) break;
+            const int32_t j0 = w.j0, end = w.end(), masked0 = w.masked0();
+            for (int32_t j = masked0; j < end && live; ++j) {
+                const int i = tiles_before + 2 * (j - j0) + 1, slot = i % C::kStages;
+                // only once its copy is asked for is a phase of the slot's barrier this tile's
+                live = wait_warp(sh, &sh.sent[place][j - masked0], sent_phase[place] >> (j - masked0) & 1) &&
+                       wait_warp(sh, &sh.full[slot], i / C::kStages & 1);
+                if (!live) break;
+                uint8_t *tile = ring + slot * C::kTileBytes;
+                const int32_t key0 = j * kTile;
+                const int r0 = max(0, w.first - key0), r1 = min(kTile, max(0, w.most - key0));
+                bool found = false;
+                for (int i = r0 * 8 + lane; i < kTile * 8; i += 32) {
 #pragma unroll
-                for (int c = 0; c < C::kHalves; ++c) {
-                    uint4 *at16 = reinterpret_cast<uint4 *>(tile + c * C::kHalfBytes) + i;
-                    if (i >= r1 * 8) {
-                        *at16 = make_uint4(0, 0, 0, 0);
-                        continue;
-                    }
-                    uint4 u = *at16;
-                    uint32_t *x = &u.x;
-                    bool bad = false;
+                    for (int c = 0; c < C::kHalves; ++c) {
+                        uint4 *at16 = reinterpret_cast<uint4 *>(tile + c * C::kHalfBytes) + i;
+                        if (i >= r1 * 8) {
+                            *at16 = make_uint4(0, 0, 0, 0);
+                            continue;
+                        }
+                        uint4 u = *at16;
+                        uint32_t *x = &u.x;
+                        bool bad = false;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        if ((x[e] & 0x7f80u) == 0x7f80u) x[e] &= 0xffff0000u, bad = true;
-                        if ((x[e] & 0x7f800000u) == 0x7f800000u) x[e] &= 0x0000ffffu, bad = true;
+                        for (int e = 0; e < 4; ++e) {
+                            if ((x[e] & 0x7f80u) == 0x7f80u) x[e] &= 0xffff0000u, bad = true;
+                            if ((x[e] & 0x7f800000u) == 0x7f800000u) x[e] &= 0x0000ffffu, bad = true;
+                        }
+                        if (bad) *at16 = u;
+                        found |= bad;
                     }
-                    if (bad) *at16 = u;
-                    found |= bad;
                 }
+                if (__any_sync(0xffffffffu, found) && lane == 0) *reinterpret_cast<volatile int32_t *>(&w.dirty) = 1;
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(&sh.clean[place][j - masked0]);
             }
-            if (__any_sync(0xffffffffu, found) && lane == 0) *reinterpret_cast<volatile int *>(&sh.dirty) = 1;
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            tiles_before += 2 * (end - j0);
+            sent_phase[place] ^= (1u << max(0, end - masked0)) - 1;
             __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(&sh.clean[j - max(w.j0, masked0)]);
+            if (lane == 0) ptx::mbar_arrive(&sh.item_empty[place]);
         }
     } else {
         // ------------------------------------------------------------ weights, a quarter of two rows per thread
@@ -359,147 +452,171 @@ prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         const uint32_t s_at = tmem + (lanes | (uint32_t)hf << 20) + t * kTile;  // 16 of them are its own
         const uint32_t o_rows = tmem + (lanes | (uint32_t)hf << 20) + C::kColO + t * D;
         const int own = (warp & 3) * 32 + hf * 16 + lane / 4;  // its first row; the second is 8 on
-        const int pair = 1 + t * 4 + (warp & 3);  // the barrier of the two warps that share the 32 lanes
-        const int32_t t_end = t ? w.end1 : w.end0;
-        int32_t lims[2];  // keys that the two rows see
-        float m[2] = {-INFINITY, -INFINITY};
-        float2 sums[2] = {};
+        uint64_t *pair = &sh.pair[t * 4 + (warp & 3)];  // of the two warps that share the 32 lanes
+        uint32_t logits_phase = 0, results_phase = 0;
+        for (int n = 0; live; ++n) {
+            const int place = n & 1;
+            if (!(live = wait_warp(sh, &sh.item_full[place], n >> 1 & 1))) break;
+            const Item &w = sh.item[place];
+            if (!w.valid) break;
+            const int32_t t_end = t ? w.end1 : w.end0, j0 = w.j0, masked0 = w.masked0();
+            float m[2] = {-INFINITY, -INFINITY};
+            float2 sums[2] = {};
+            for (int32_t j = j0; j < t_end; ++j) {
+                if (!(live = wait_warp(sh, &sh.s_full[t], logits_phase))) break;
+                logits_phase ^= 1;
+                tc::fence_after();
+                float x[2][32];
+                tc::ld_rows(s_at, x[0]);
+                tc::ld_rows(s_at + 64, x[1]);
+                tc::wait_ld();
+                if (j >= masked0) {
+                    int row0 = own;
+                    asm volatile("" : "+r"(row0));  // (what follows is not kept in registers from tile to tile)
+                    int32_t lims[2];                // keys that the two rows see
 #pragma unroll
-        for (int e = 0; e < 2; ++e) lims[e] = w.first + t * tile_tokens + (own + 8 * e) / p.G;
-        bool live = true;
-        for (int32_t j = w.j0; j < t_end; ++j) {
-            if (!(live = wait_warp(sh, &sh.s_full[t], (j - w.j0) & 1))) break;
-            tc::fence_after();
-            float x[2][32];
-            tc::ld_rows(s_at, x[0]);
-            tc::ld_rows(s_at + 64, x[1]);
-            tc::wait_ld();
-            if (j >= masked0) {
+                    for (int e = 0; e < 2; ++e) lims[e] = w.first + t * tile_tokens + (row0 + 8 * e) / p.G;
 #pragma unroll
-                for (int c = 0; c < 2; ++c)
+                    for (int c = 0; c < 2; ++c)
 #pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        if (64 * c + i / 4 * 8 + (lane & 3) * 2 + (i & 1) >= lims[i >> 1 & 1] - j * kTile) x[c][i] = -INFINITY;
-            }
-            float top[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                float a = fmaxf(x[0][2 * e], x[0][2 * e + 1]), b = fmaxf(x[1][2 * e], x[1][2 * e + 1]);
-#pragma unroll
-                for (int i = 4; i < 32; i += 4) {
-                    a = max3(a, x[0][i + 2 * e], x[0][i + 2 * e + 1]);
-                    b = max3(b, x[1][i + 2 * e], x[1][i + 2 * e + 1]);
+                        for (int i = 0; i < 32; ++i)
+                            if (64 * c + i / 4 * 8 + (lane & 3) * 2 + (i & 1) >= lims[i >> 1 & 1] - j * kTile) x[c][i] = -INFINITY;
                 }
-                top[e] = fmaxf(a, b);
-            }
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], 1));
-                top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], 2)) * p.scale_log2;
-            }
-            const bool grown[2] = {top[0] > m[0] + kSlack, top[1] > m[1] + kSlack};
-            if (__any_sync(0xffffffffu, grown[0] || grown[1])) {
-                float keep[2];
+                float top[2];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    keep[e] = grown[e] ? ex2(m[e] - top[e]) : 1.f;  // a row does not depend on its neighbours
-                    if (grown[e]) m[e] = top[e];
-                    sums[e].x *= keep[e], sums[e].y *= keep[e];
-                }
-                if (j > w.j0) {  // the products of the tiles before are done: the logits' commit came after theirs
-                    float o[8];
-#pragma unroll 1
-                    for (int c = 0; c < D; c += 16) {
-                        tc::ld_rows16(o_rows + c, o);
-                        tc::wait_ld();
+                    float a = fmaxf(x[0][2 * e], x[0][2 * e + 1]), b = fmaxf(x[1][2 * e], x[1][2 * e + 1]);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) o[i] *= keep[i >> 1 & 1];
-                        tc::st_rows16(o_rows + c, o);
+                    for (int i = 4; i < 32; i += 4) {
+                        a = max3(a, x[0][i + 2 * e], x[0][i + 2 * e + 1]);
+                        b = max3(b, x[1][i + 2 * e], x[1][i + 2 * e + 1]);
                     }
+                    top[e] = fmaxf(a, b);
                 }
-            }
-            const float ref[2] = {m[0] == -INFINITY ? 0.f : -m[0] - kSlack, m[1] == -INFINITY ? 0.f : -m[1] - kSlack};
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                uint32_t u[16];
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float2 e = fma2(x[c][2 * i], x[c][2 * i + 1], p.scale_log2, ref[i & 1]);
-                    const float a = ex2(e.x), b = ex2(e.y);
-                    add2(sums[i & 1], a, b);
-                    u[i] = ptx::pack_bf16(a, b);
+                for (int e = 0; e < 2; ++e) {
+                    top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], 1));
+                    top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], 2)) * p.scale_log2;
                 }
-                tc::st_rows(s_at + 32 * c, u);
-            }
-            tc::wait_st();
-            tc::fence_before();
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(&sh.p_full[t]);
-        }
-        // ------------------------------------------------------------ results, half a row per thread
-        constexpr int kCols = D / 2;
-        const uint32_t o_at = tmem + lanes + C::kColO + t * D + hf * kCols;
-        const int r = threadIdx.x & (kTile - 1);
-        const int32_t token = t * tile_tokens + r / p.G, lim = w.first + token;
-        const bool any = t_end > w.j0;
-        if (live && any) live = wait_warp(sh, &sh.o_full[t], 0);
+                const bool grown[2] = {top[0] > m[0] + kSlack, top[1] > m[1] + kSlack};
+                if (__any_sync(0xffffffffu, grown[0] || grown[1])) {
+                    float keep[2];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            float sum = sums[e].x + sums[e].y;
-            sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-            sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-            if ((lane & 3) == 0) sh.sum[t][own + 8 * e] = sum, sh.top[t][own + 8 * e] = m[e];
-        }
-        pair_barrier(pair);  // both warps come, whatever their waits said
-        const float sum = sh.sum[t][r], m_row = sh.top[t][r];
-        tc::fence_after();
-        const bool mine = live && token < at.rows && r < tile_tokens * p.G;
-        const int64_t row = ((int64_t)l * p.T + at.t0 + token) * p.Hq + h * p.G + r % p.G;
-        const bool none = !any || lim <= 0;
-        const float inv = none ? 0.f : 1.f / sum;
-        const bool dirty = *reinterpret_cast<volatile int *>(&sh.dirty);
-        const int64_t all = (int64_t)p.layer_count * p.T * p.Hq;
-        if (mine && p.splits > 1 && hf == 0)
-            p.part_ml[split * all + row] = make_float2(!any || m_row == -INFINITY ? -INFINITY : m_row + kSlack, any ? sum : 0.f);
-        if (live && any) {
+                    for (int e = 0; e < 2; ++e) {
+                        keep[e] = grown[e] ? ex2(m[e] - top[e]) : 1.f;  // a row does not depend on its neighbours
+                        if (grown[e]) m[e] = top[e];
+                        sums[e].x *= keep[e], sums[e].y *= keep[e];
+                    }
+                    if (j > j0) {  // the products of the tiles before are done: the logits' commit came after theirs
+                        float o[8];
+#pragma unroll 1
+                        for (int c = 0; c < D; c += 16) {
+                            tc::ld_rows16(o_rows + c, o);
+                            tc::wait_ld();
 #pragma unroll
-            for (int c = 0; c < kCols / 32; ++c) {
-                float o[32];
-                tc::ld32(o_at + 32 * c, o);
-                tc::wait_ld();
-                if (!mine) continue;
-                const int col = hf * kCols + 32 * c;
-                if (p.splits == 1)
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) o[i] = none ? 0.f : o[i] * inv;
-                if (dirty) {  // the elements of V that the mask warp took out, for the rows that see them
-                    const int32_t k0 = max(max(0, w.first), w.j0 * kTile), k1 = min(lim, t_end * kTile);
-                    for (int32_t key = k0; key < k1; ++key) {
-                        const int64_t at_row = kPaged ? paged_row(p.cache.pv, w.cu, key) : w.cu * p.C + key;
-                        if (at_row < 0 || at_row >= p.kv_rows) continue;
-                        const __nv_bfloat16 *v = static_cast<const __nv_bfloat16 *>(p.cache.v) + at_row * D + col;
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            const float e = __bfloat162float(v[i]);
-                            if (!isfinite(e)) o[i] += e;
+                            for (int i = 0; i < 8; ++i) o[i] *= keep[i >> 1 & 1];
+                            tc::st_rows16(o_rows + c, o);
                         }
                     }
                 }
-                if (p.splits > 1) {
-                    float4 *to = reinterpret_cast<float4 *>(p.part_o + (split * all + row) * D + col);
+                const float ref[2] = {m[0] == -INFINITY ? 0.f : -m[0] - kSlack, m[1] == -INFINITY ? 0.f : -m[1] - kSlack};
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) to[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
-                } else {
-                    uint4 *to = reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) + row * D + col);
+                for (int c = 0; c < 2; ++c) {
+                    uint32_t u[16];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        to[i] = make_uint4(ptx::pack_bf16(o[8 * i], o[8 * i + 1]), ptx::pack_bf16(o[8 * i + 2], o[8 * i + 3]),
-                                           ptx::pack_bf16(o[8 * i + 4], o[8 * i + 5]), ptx::pack_bf16(o[8 * i + 6], o[8 * i + 7]));
+                    for (int i = 0; i < 16; ++i) {
+                        const float2 e = fma2(x[c][2 * i], x[c][2 * i + 1], p.scale_log2, ref[i & 1]);
+                        const float a = ex2(e.x), b = ex2(e.y);
+                        add2(sums[i & 1], a, b);
+                        u[i] = ptx::pack_bf16(a, b);
+                    }
+                    tc::st_rows(s_at + 32 * c, u);
                 }
+                tc::wait_st();
+                tc::fence_before();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(&sh.p_full[t]);
             }
-        } else if (mine && p.splits == 1) {
-            uint4 *to = reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) + row * D + hf * kCols);
-            for (int i = 0; i < kCols / 8; ++i) to[i] = make_uint4(0, 0, 0, 0);
+            // ------------------------------------------------------------ results, half a row per thread
+            constexpr int kCols = D / 2;
+            const uint32_t o_at = tmem + lanes + C::kColO + t * D + hf * kCols;
+            int r = threadIdx.x & (kTile - 1);
+            asm volatile("" : "+r"(r));  // (nor is this)
+            const int32_t token = t * tile_tokens + r / p.G, lim = w.first + token;
+            const bool any = t_end > j0;
+            float sum = 0.f, m_row = -INFINITY;
+            if (live && any) {
+                live = wait_warp(sh, &sh.o_full[t], results_phase);
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float part = sums[e].x + sums[e].y;
+                    part += __shfl_xor_sync(0xffffffffu, part, 1);
+                    part += __shfl_xor_sync(0xffffffffu, part, 2);
+                    if ((lane & 3) == 0) sh.sum[t][own + 8 * e] = part, sh.top[t][own + 8 * e] = m[e];
+                }
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(pair);
+                live = wait_warp(sh, pair, results_phase) && live;
+                results_phase ^= 1;
+                sum = sh.sum[t][r], m_row = sh.top[t][r];
+            }
+            if (!live) break;
+            tc::fence_after();
+            const bool mine = token < w.rows && r < tile_tokens * p.G;
+            const int64_t row = ((int64_t)w.l * p.T + w.t0 + token) * p.Hq + w.h * p.G + r % p.G;
+            const bool none = !any || lim <= 0;
+            const float inv = none ? 0.f : 1.f / sum;
+            const bool dirty = *reinterpret_cast<volatile int32_t *>(&sh.item[place].dirty);
+            const int64_t all = (int64_t)p.layer_count * p.T * p.Hq;
+            if (mine && p.splits > 1 && hf == 0)
+                p.part_ml[w.split * all + row] = make_float2(!any || m_row == -INFINITY ? -INFINITY : m_row + kSlack, any ? sum : 0.f);
+            if (any) {
+#pragma unroll
+                for (int c = 0; c < kCols / 32; ++c) {
+                    float o[32];
+                    tc::ld32(o_at + 32 * c, o);
+                    tc::wait_ld();
+                    if (c == kCols / 32 - 1) {  // the last of it is in registers: the next item's products may come
+                        tc::fence_before();
+                        __syncwarp();
+                        if (lane == 0) ptx::mbar_arrive(&sh.o_empty[t]);
+                    }
+                    if (!mine) continue;
+                    const int col = hf * kCols + 32 * c;
+                    if (p.splits == 1)
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) o[i] = none ? 0.f : o[i] * inv;
+                    if (dirty) {  // the elements of V that the mask warp took out, for the rows that see them
+                        const int32_t k0 = max(max(0, w.first), w.j0 * kTile), k1 = min(lim, t_end * kTile);
+                        for (int32_t key = k0; key < k1; ++key) {
+                            const int64_t at_row = kPaged ? paged_row(p.cache.pv, w.cu, key) : w.cu * p.C + key;
+                            if (at_row < 0 || at_row >= p.kv_rows) continue;
+                            const __nv_bfloat16 *v = static_cast<const __nv_bfloat16 *>(p.cache.v) + at_row * D + col;
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) {
+                                const float e = __bfloat162float(v[i]);
+                                if (!isfinite(e)) o[i] += e;
+                            }
+                        }
+                    }
+                    if (p.splits > 1) {
+                        float4 *to = reinterpret_cast<float4 *>(p.part_o + (w.split * all + row) * D + col);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) to[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                    } else {
+                        uint4 *to = reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) + row * D + col);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            to[i] = make_uint4(ptx::pack_bf16(o[8 * i], o[8 * i + 1]), ptx::pack_bf16(o[8 * i + 2], o[8 * i + 3]),
+                                               ptx::pack_bf16(o[8 * i + 4], o[8 * i + 5]), ptx::pack_bf16(o[8 * i + 6], o[8 * i + 7]));
+                    }
+                }
+            } else if (mine && p.splits == 1) {
+                uint4 *to = reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) + row * D + hf * kCols);
+                for (int i = 0; i < kCols / 8; ++i) to[i] = make_uint4(0, 0, 0, 0);
+            }
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(&sh.item_empty[place]);
         }
     }
     tc::fence_before();
