@@ -7,6 +7,9 @@ upper bound on the cache length (read back once after stage 1) so that every dec
 sized without a device-to-host sync; the decode loop of a request can therefore be captured once
 in a CUDA graph and replayed (``capture_loop``).
 
+A later turn of the conversation joins a session by ``extend``: its rows are rotated, appended behind the rows that
+the cache has kept, and attend over all of them.
+
 With ``kv_bits=4`` the session's cache holds its rows in 4 bits per channel: stage 1 runs into a staging cache of
 plain rows, which is packed right after it, and decode steps and evictions work on the packed rows. The staging
 rows are needed during ``prefill`` alone: it makes them and gives them back to torch's allocator. Rows that the caller
@@ -126,6 +129,38 @@ class Session:
                     launch(self.staging)
                 finally:
                     turn.done = at.record_event()
+
+    # a later turn -------------------------------------------------------------------------------
+    def extend(self, q, k, v, new_pos, seq_off, out, *, max_rows: int, rotary=None, positions=None, q_out=None,
+               sm_scale: float = 0.0, layer_begin=0, layer_count=None, stream=None):
+        """A turn's prompt for a layer range (all layers by default): packed rows q, k and v [layers][tokens][heads][D] of
+        every sequence (see voxzip_append) join its units, k and q rotated on the way, and the queries' causal attention
+        over all rows goes to `out`. `max_rows` bounds the tokens of one sequence. With a rotation and no `q_out` the
+        rotated queries live for the call."""
+        if self.kv_bits != 16:
+            raise ValueError("extend needs a cache whose rows are in the descriptor's dtype (kv_bits=16)")
+        if max_rows < 0:
+            raise ValueError("max_rows must bound the tokens of a sequence")
+        c = self.cache
+        lc = self.desc.layers if layer_count is None else layer_count
+        longest = min(self.n_max + int(max_rows), self.desc.capacity)
+        if rotary is not None and q_out is None:
+            with torch.cuda.stream(_torch_stream(stream)):  # the launches' own, as it is what they use it on
+                q_out = torch.empty(q.shape, dtype=q.dtype, device=self.device)
+        turn = dict(rotary=rotary, positions=positions, max_rows=max_rows, stream=stream)
+        if q_out is not None:
+            turn.update(q=q, q_out=q_out)
+        attend = dict(sm_scale=sm_scale, max_rows=max_rows, max_len=longest, stream=stream)
+        queries = q if q_out is None else q_out
+        if self.paged:
+            N.voxzip_append_paged(self.desc, c, layer_begin, lc, k, v, new_pos, seq_off, **turn)
+            N.voxzip_prompt_attention_paged(self.desc, c, layer_begin, lc, queries, seq_off, out, **attend)
+        else:
+            N.voxzip_append(self.desc, layer_begin, lc, k, v, new_pos, seq_off, c["k"], c["v"], c["score"], c["pos"],
+                            c["len"], **turn)
+            N.voxzip_prompt_attention(self.desc, layer_begin, lc, queries, seq_off, c["k"], c["v"], c["len"], out, **attend)
+        if layer_begin + lc == self.desc.layers:
+            self.n_max = longest
 
     # stage 2 -------------------------------------------------------------------------------------
     def decode(self, q, k_new, v_new, new_pos, out, *, layer_begin=0, layer_count=None, stream=None):

@@ -523,6 +523,119 @@ def test_binding_refuses(V):
         V.voxzip_prompt_attention(desc, 1, 1, q, off, c["k"], c["v"], c["len"], out)
 
 
+# ----------------------------------------------------------------------------- all of it, as it is used
+
+@pytest.mark.parametrize("dtype,paged", [(BF16, False), (BF16, True), (F32, False)])
+def test_a_conversation(V, dtype, paged):
+    """A prompt made into a slab, stage 1, decode steps on rotated rows, an eviction, a second turn, and steps after it:
+    every attention against the plain one on the rows that the cache holds."""
+    B, L, Hq, H, D, ms = 2, 2, 4, 2, 64, [90, 70]
+    stride, cap = max(ms), 256
+    rnd = gen(8)
+    r = V.RotaryDesc.make(64, sections=(12, 10, 10), in_turns=True)
+    slab = V.CacheDesc(B, L, Hq, H, D, stride, dtype)
+    pre = dict(k=torch.full((B, L, H, stride, D), math.nan, dtype=dtype, device="cuda"), v=torch.zeros(B, L, H, stride, D, dtype=dtype, device="cuda"),
+               len=torch.zeros(B, L, H, dtype=I32, device="cuda"))
+
+    def rows(m):
+        qkv = rnd(L, sum(m), (Hq + 2 * H) * D).to(dtype)
+        return [x.unflatten(-1, (-1, D)) for x in qkv.split([Hq * D, H * D, H * D], -1)]
+
+    # the prompt, layer by layer, as a model runs
+    q, k, v = rows(ms)
+    off, T = offsets(ms), sum(ms)
+    pos = torch.cat([torch.arange(m) for m in ms]).to(I32).cuda().expand(3, T).contiguous()
+    qo, out = torch.empty(L, T, Hq, D, dtype=dtype, device="cuda"), torch.empty(L, T, Hq, D, dtype=dtype, device="cuda")
+    for l in range(L):
+        V.voxzip_append(slab, l, 1, k[l:l + 1], v[l:l + 1], None, off, pre["k"], pre["v"], None, None, pre["len"], rotary=r,
+                        positions=pos, q=q[l:l + 1], q_out=qo[l:l + 1], max_rows=stride)
+        V.voxzip_prompt_attention(slab, l, 1, qo[l:l + 1], off, pre["k"], pre["v"], pre["len"], out[l:l + 1], max_rows=stride)
+    want_k, size = R.rotate(k, pos, r)
+    for b, m in enumerate(ms):
+        t = slice(int(off[b]), int(off[b + 1]))
+        for l in range(L):
+            for h in range(H):
+                close(pre["k"][b, l, h, :m], want_k[l, t, h], R.rotate_bound(want_k, size, dtype)[l, t, h])
+                want, mag, big = R.attention(qo[l, t, 2 * h:2 * h + 2], pre["k"][b, l, h, :m], pre["v"][b, l, h, :m], 1, 0.125)
+                close(out[l, t, 2 * h:2 * h + 2], want, R.attention_bound(want, mag, big, m, D, dtype))
+
+    # stage 1: spans of four tokens to one row, from the tenth token on
+    desc = V.CacheDesc(B, L, Hq, H, D, cap, dtype)
+    from paper_2608_08569_gb300.session import Session
+    s = Session(desc, [60, 50], 0.98, pages=64 if paged else None)
+    starts = [torch.arange(10, m - 3, 4, dtype=I32) for m in ms]
+    n = [len(x) for x in starts]
+    i32 = lambda x: torch.as_tensor(x, dtype=I32).cuda()  # noqa: E731
+    begin, length = [10, 10], [4 * x for x in n]
+    s.prefill(pre["k"].nan_to_num(), pre["v"], i32(ms), i32(begin), i32(length), i32([0, n[0], n[0] + n[1]]), torch.cat(starts).cuda(),
+              torch.cat(starts).cuda() + 4, i32([1] * sum(n)))
+    kept = [m - 3 * x for m, x in zip(ms, n)]
+    assert s.cache["len"][:, 0, 0].tolist() == kept
+
+    def step(at):
+        q, k, v = (x.view(L, B, -1, D) for x in rows([1, 1]))
+        p = i32(at).expand(3, B).contiguous()
+        qr, kr = torch.empty_like(q).contiguous(), torch.empty(L, B, H, D, dtype=dtype, device="cuda")
+        V.voxzip_rotary(desc, r, p, q=q, k=k, q_out=qr, k_out=kr)
+        out = torch.empty_like(qr)
+        s.decode(qr, kr, v.contiguous(), p[0].contiguous(), out)
+        for b in range(B):
+            for l in range(L):
+                for h in range(H):
+                    m = int(s.cache["len"][b, l, h])
+                    kk, vv = unit_rows(s.cache, b, l, h, m)
+                    assert torch.equal(kk[-1], kr[l, b, h])
+                    want, mag, big = R.attention(qr[l, b, 2 * h:2 * h + 2][None], kk, vv, m, 0.125)
+                    # (the step adds its parts up in another order: twice the bound)
+                    close(out[l, b, 2 * h:2 * h + 2][None], want, 2 * R.attention_bound(want, mag, big, m, D, dtype))
+
+    at = list(ms)
+    for _ in range(3):
+        step(at)
+        at = [x + 1 for x in at]
+    before = s.cache["len"][:, 0, 0].tolist()
+    s.evict()
+    assert s.cache["len"][:, 0, 0].tolist() == [min(x, y) for x, y in zip(before, (60, 50))]
+
+    # the second turn, and its answer
+    turn = [33, 5]
+    n0 = s.cache["len"][:, 0, 0].tolist()
+    q, k, v = rows(turn)
+    T = sum(turn)
+    pos = torch.cat([torch.arange(m) + a for m, a in zip(turn, at)]).to(I32).cuda()
+    out, qo = torch.empty(L, T, Hq, D, dtype=dtype, device="cuda"), torch.empty(L, T, Hq, D, dtype=dtype, device="cuda")
+    for l in range(L):
+        s.extend(q[l:l + 1], k[l:l + 1], v[l:l + 1], pos, offsets(turn), out[l:l + 1], max_rows=33, rotary=r,
+                 positions=pos.expand(3, T).contiguous(), q_out=qo[l:l + 1], layer_begin=l, layer_count=1)
+    assert s.n_max >= max(x + m for x, m in zip(n0, turn)) and (s.cache["len"][:, 1, 1].tolist() == [x + m for x, m in zip(n0, turn)])
+    off = offsets(turn)
+    for b, m in enumerate(turn):
+        t = slice(int(off[b]), int(off[b + 1]))
+        for l in range(L):
+            for h in range(H):
+                kk, vv = unit_rows(s.cache, b, l, h, n0[b] + m)
+                assert torch.equal(vv[n0[b]:], v[l, t, h])
+                want, mag, big = R.attention(qo[l, t, 2 * h:2 * h + 2], kk, vv, n0[b] + 1, 0.125)
+                close(out[l, t, 2 * h:2 * h + 2], want, R.attention_bound(want, mag, big, n0[b] + m, D, dtype))
+    assert (s.cache["score"][0, :, :, n0[0]:n0[0] + 33] == 0).all()
+    step([a + m for a, m in zip(at, turn)])
+    if paged:
+        check_pages(desc, s.cache)
+    # without a place for the rotated queries, and without a rotation
+    again = torch.empty_like(out)
+    s.extend(q, k, v, pos, offsets(turn), again, max_rows=33, rotary=r, positions=pos.expand(3, T).contiguous())
+    s.extend(q, k, v, pos, offsets(turn), again, max_rows=33)
+    assert s.cache["len"][:, 0, 0].tolist() == [x + 3 * m + 1 for x, m in zip(n0, turn)]
+
+
+def test_a_packed_session_refuses_a_turn(V):
+    from paper_2608_08569_gb300.session import Session
+    s = Session(V.CacheDesc(1, 1, 2, 1, 64, 64, BF16), [32], 0.9, kv_bits=4)
+    x = torch.zeros(1, 3, 2, 64, dtype=BF16, device="cuda")
+    with pytest.raises(ValueError, match="kv_bits"):
+        s.extend(x, x[:, :, :1], x[:, :, :1], torch.zeros(3, dtype=I32, device="cuda"), offsets([3]), x.clone(), max_rows=3)
+
+
 @pytest.mark.skipif(os.environ.get("VOXZIP_CHECKED", "0") not in ("", "0"), reason="this is the checked run")
 def test_checked_build(V):
     """The range-checked build gives the same results and no bit of VOXZIP_DEV_BOUNDS."""
