@@ -470,7 +470,7 @@ voxzip_status voxzip_evict_q4(const voxzip_cache_desc *desc, const voxzip_q4_cac
  * The rows of several sequences are packed: sequence b's tokens are rows [seq_off[b], seq_off[b + 1]) of q, k and v,
  * with 0 <= seq_off[b] <= seq_off[b + 1] <= tokens (sequences may be empty; rows of no sequence are left alone, in the
  * outputs too). Offsets that break this set VOXZIP_DEV_BAD_SPANS; nothing is appended then, and no sequence from the
- * first bad one on attends.
+ * first bad one on attends (which of those before it do is not said).
  */
 typedef struct {
     const void *data;     /* [layer][token][head][D]: heads D apart; 16-byte aligned */
@@ -563,8 +563,8 @@ size_t voxzip_prompt_attention_workspace_size(const voxzip_cache_desc *desc, int
  *              (the capacity). Hints for the launch: others change which CTAs share the keys, not what is computed
  *   workspace  device scratch of voxzip_prompt_attention_workspace_size() bytes for the same arguments, 256-byte
  *              aligned; NULL where that is 0
- * Requires D in {64, 128}, G <= 16. Device errors: VOXZIP_DEV_CAPACITY (a length outside [0, C]; the unit's rows of
- * out are not written), BAD_SPANS.
+ * Requires D in {64, 128}, G <= 16, and for bf16 at most 2^31 - 1 rows of K. Device errors: VOXZIP_DEV_CAPACITY (a length
+ * outside [0, C]; the unit's rows of out are not written), BAD_SPANS, TIMEOUT (a bounded wait gave up).
  */
 voxzip_status voxzip_prompt_attention(const voxzip_cache_desc *desc, int32_t layer_begin, int32_t layer_count,
                                       int32_t tokens, const voxzip_rows *q, const int32_t *seq_off,

@@ -828,6 +828,12 @@ def _rows(t, name: str, desc: CacheDesc, heads: int, like=None):
     return _Rows(t.data_ptr(), st, sl)
 
 
+def _on_current_device(t, name: str) -> None:
+    """The launches go to the current device: its streams, its plans, its tensor maps."""
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+
+
 def _positions(positions, rotary: RotaryDesc, tokens: int) -> None:
     axes = rotary.num_axes
     if positions is not None and isinstance(positions, torch.Tensor) and positions.dim() == 1 and axes == 1:
@@ -868,6 +874,7 @@ def voxzip_rotary(desc: CacheDesc, rotary: RotaryDesc, positions, *, q=None, k=N
     if k is not None:
         _need(k_out, "k_out", desc.dtype, (L, T, desc.kv_heads, desc.head_dim))
     _positions(positions, rotary, T)
+    _on_current_device(positions, "positions")
     if L == 0:
         return
     _check("voxzip_rotary", lib().voxzip_rotary(
@@ -886,6 +893,7 @@ def _append_args(desc: CacheDesc, layer_count: int, k, v, new_pos, seq_off, rota
         raise ValueError(f"k: {L} layers, expected {layer_count}")
     vr = _rows(v, "v", desc, desc.kv_heads, (L, T))
     _need(seq_off, "seq_off", torch.int32, (desc.batch + 1,))
+    _on_current_device(seq_off, "seq_off")
     if pos_kept or new_pos is not None:
         _need(new_pos, "new_pos", torch.int32, (T,))
     qr = None
@@ -948,6 +956,7 @@ def _attention_args(desc: CacheDesc, layer_count: int, q, seq_off, out, max_rows
     if L != layer_count:
         raise ValueError(f"q: {L} layers, expected {layer_count}")
     _need(seq_off, "seq_off", torch.int32, (desc.batch + 1,))
+    _on_current_device(seq_off, "seq_off")
     _need(out, "out", desc.dtype, (L, T, desc.q_heads, desc.head_dim))
     need = voxzip_prompt_attention_workspace_size(desc, L, T, max_rows, max_len) if T and workspace is None else 0
     return T, qr, _scratch(workspace, need, out.device, stream)

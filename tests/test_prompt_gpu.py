@@ -523,6 +523,89 @@ def test_binding_refuses(V):
         V.voxzip_prompt_attention(desc, 1, 1, q, off, c["k"], c["v"], c["len"], out)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_several_layers_in_one_call(V, dtype):
+    """Layers whose units differ in length (budgets per layer), queries at a stride of layers of their own."""
+    ms, desc = [40, 3], V.CacheDesc(2, 4, 6, 2, 64, 200, dtype)
+    c = fill(V, desc, [160, 90])
+    c["len"][:, 2] -= 17
+    c["len"][1, 3, 1] += 5
+    c["k"].nan_to_num_(0.0)
+    c["v"].nan_to_num_(0.0)
+    for first, count in ((0, 4), (1, 3), (3, 1)):
+        q = gen(2)(count, 2, 45, 6, 64).to(dtype)[:, 1]
+        out = torch.empty(count, 45, 6, 64, dtype=dtype, device="cuda")
+        V.voxzip_prompt_attention(desc, first, count, q, offsets(ms), c["k"], c["v"], c["len"], out)
+        for b, t in enumerate((slice(0, 40), slice(40, 43))):
+            for l in range(count):
+                for h in range(2):
+                    n = int(c["len"][b, first + l, h])
+                    k, v = unit_rows(c, b, first + l, h, n)
+                    want, mag, size = R.attention(q[l, t, 3 * h:3 * h + 3], k, v, n - ms[b] + 1, 0.125)
+                    close(out[l, t, 3 * h:3 * h + 3], want, R.attention_bound(want, mag, size, n, 64, dtype), (b, l, h))
+
+
+@pytest.mark.parametrize("dtype,paged", [(BF16, False), (BF16, True), (F32, False)])
+def test_many_sequences(V, dtype, paged):
+    """More sequences than a warp has lanes, most of a token or none."""
+    ms = [i % 4 for i in range(75)] + [140]
+    ns = [m + 3 * i % 60 for i, m in enumerate(ms)]
+    desc = V.CacheDesc(len(ms), 1, 4, 2, 64, 256, dtype)
+    check_attention(V, desc, fill(V, desc, ns, paged=paged), ms, ns, gap=1)
+
+
+def test_a_wrong_hint_of_the_rows_appends_the_same(V):
+    desc, r = V.CacheDesc(2, 1, 4, 2, 64, 400, BF16), V.RotaryDesc.make(64)
+    qkv, pos, off = gen(1)(1, 310, 8, 64).to(BF16), torch.arange(310, dtype=I32, device="cuda"), offsets([300, 10])
+    got = []
+    for hint in (0, 1, 300, 10 ** 6):
+        c, qo = fill(V, desc, [7, 90]), torch.empty(1, 310, 4, 64, dtype=BF16, device="cuda")
+        append(V, desc, c, 0, 1, qkv[:, :, 4:6], qkv[:, :, 6:], pos, off, rotary=r, positions=pos, q=qkv[:, :, :4], q_out=qo, max_rows=hint)
+        got.append({**c, "q": qo})
+    for g in got[1:]:
+        for x in g:
+            assert torch.equal(torch.nan_to_num(g[x].float()), torch.nan_to_num(got[0][x].float())), x
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_a_cache_beyond_32_bit_offsets(V, dtype):
+    """More than 2^32 bytes, and elements beyond 2^31, in front of the unit."""
+    D, C = 128, 3_000_000
+    desc = V.CacheDesc(1, 3, 4, 2, D, C, dtype)
+    k, v = (torch.empty(1, 3, 2, C, D, dtype=dtype, device="cuda") for _ in range(2))
+    assert k.numel() > 2 ** 31
+    ln = torch.zeros(1, 3, 2, dtype=I32, device="cuda")
+    n = C - 25
+    for first in (n - 300, 0):  # the rows in front of the turn: the last ones of the unit, and the first ones
+        rows = torch.arange(first, first + 300, device="cuda")
+        rnd = gen(first % 97)
+        kk, vv = rnd(2, 320, D).to(dtype), rnd(2, 320, D).to(dtype)
+        k[0, 2, :, rows], v[0, 2, :, rows] = kk[:, :300], vv[:, :300]
+        ln[0, 2] = first + 300
+        V.voxzip_append(desc, 2, 1, kk[None, :, 300:].transpose(1, 2).contiguous(), vv[None, :, 300:].transpose(1, 2).contiguous(), None,
+                        offsets([20]), k, v, None, None, ln)
+        assert (ln[0, 2] == first + 320).all() and torch.equal(k[0, 2, :, first + 300:first + 320], kk[:, 300:])
+        if first == 0:
+            q, out = rnd(1, 20, 4, D).to(dtype), torch.empty(1, 20, 4, D, dtype=dtype, device="cuda")
+            V.voxzip_prompt_attention(desc, 2, 1, q, offsets([20]), k, v, ln, out, max_len=320)
+            for h in range(2):
+                want, mag, size = R.attention(q[0, :, 2 * h:2 * h + 2], kk[h], vv[h], 301, D ** -0.5)
+                close(out[0, :, 2 * h:2 * h + 2], want, R.attention_bound(want, mag, size, 320, D, dtype))
+
+
+def test_another_device_is_refused(V, monkeypatch):
+    desc = V.CacheDesc(1, 1, 4, 2, 64, 64, BF16)
+    c, q = fill(V, desc, [10]), torch.zeros(1, 4, 4, 64, dtype=BF16, device="cuda")
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    with pytest.raises(ValueError, match="current device"):
+        V.voxzip_prompt_attention(desc, 0, 1, q, offsets([4]), c["k"], c["v"], c["len"], q.clone())
+    with pytest.raises(ValueError, match="current device"):
+        V.voxzip_append(desc, 0, 1, q[:, :, :2], q[:, :, :2], torch.zeros(4, dtype=I32, device="cuda"), offsets([4]), c["k"], c["v"], c["score"],
+                        c["pos"], c["len"])
+    with pytest.raises(ValueError, match="current device"):
+        V.voxzip_rotary(desc, V.RotaryDesc.make(64), torch.zeros(4, dtype=I32, device="cuda"), q=q, q_out=q)
+
+
 # ----------------------------------------------------------------------------- all of it, as it is used
 
 @pytest.mark.parametrize("dtype,paged", [(BF16, False), (BF16, True), (F32, False)])
