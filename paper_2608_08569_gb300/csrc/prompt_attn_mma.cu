@@ -69,8 +69,9 @@ template <int D> struct Shared {
 };
 
 // The tiles start on a multiple of 1024 behind Shared; a CTA's memory does too, but for what the compiler puts first.
-template <int D> constexpr size_t smem_bytes() { return 3072 + Cfg<D>::kBytes; }
-static_assert(sizeof(Shared<128>) <= 3072 && sizeof(Shared<64>) <= 3072 && smem_bytes<128>() <= 232448, "what an SM has");
+constexpr size_t kFront = 3 * 1024;
+template <int D> constexpr size_t smem_bytes() { return kFront + Cfg<D>::kBytes; }
+static_assert(sizeof(Shared<128>) <= kFront && sizeof(Shared<64>) <= kFront && smem_bytes<128>() <= 232448, "what an SM has");
 
 // A bounded wait; once one has given up in a CTA, all do.
 template <int D> __device__ __forceinline__ bool wait(Shared<D> &sh, uint64_t *bar, uint32_t parity) {
