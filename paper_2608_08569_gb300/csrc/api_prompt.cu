@@ -97,7 +97,7 @@ CacheRows paged_rows(const voxzip_paged_cache &pc) {
 
 // Launches whose grid extents would not fit.
 bool counts_fit(const voxzip_cache_desc &d, int32_t layer_count, int32_t tokens) {
-    return (int64_t)layer_count * d.batch * d.kv_heads <= INT32_MAX && (int64_t)layer_count * tokens <= INT32_MAX &&
+    return (int64_t)layer_count * d.batch * d.kv_heads <= INT32_MAX / 8 && (int64_t)layer_count * tokens <= INT32_MAX &&
            (int64_t)tokens + d.batch <= INT32_MAX;
 }
 

@@ -77,7 +77,7 @@ static_assert(sizeof(Shared<128>) <= kFront && sizeof(Shared<64>) <= kFront && s
 template <int D> __device__ __forceinline__ bool wait(Shared<D> &sh, uint64_t *bar, uint32_t parity) {
     for (uint32_t i = 0; i < kPolls; ++i) {
         if (ptx::mbar_try_wait(bar, parity)) return true;
-        if (*reinterpret_cast<volatile int *>(&sh.dead)) return false;
+        if ((i & 63) == 63 && *reinterpret_cast<volatile int *>(&sh.dead)) return false;
     }
     *reinterpret_cast<volatile int *>(&sh.dead) = 1;
     return false;
@@ -418,25 +418,28 @@ prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 const int32_t key0 = j * kTile;
                 const int r0 = max(0, w.first - key0), r1 = min(kTile, max(0, w.most - key0));
                 bool found = false;
-                for (int i = r0 * 8 + lane; i < kTile * 8; i += 32) {
 #pragma unroll
-                    for (int c = 0; c < C::kHalves; ++c) {
-                        uint4 *at16 = reinterpret_cast<uint4 *>(tile + c * C::kHalfBytes) + i;
-                        if (i >= r1 * 8) {
-                            *at16 = make_uint4(0, 0, 0, 0);
-                            continue;
-                        }
-                        uint4 u = *at16;
-                        uint32_t *x = &u.x;
-                        bool bad = false;
+                for (int c = 0; c < C::kHalves; ++c) {
+                    uint4 *half = reinterpret_cast<uint4 *>(tile + c * C::kHalfBytes);
+                    for (int i0 = r0 * 8 + lane; i0 < r1 * 8; i0 += 2 * 32) {  // two at a time on their way
+                        uint4 u[2];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            if ((x[e] & 0x7f80u) == 0x7f80u) x[e] &= 0xffff0000u, bad = true;
-                            if ((x[e] & 0x7f800000u) == 0x7f800000u) x[e] &= 0x0000ffffu, bad = true;
+                        for (int e = 0; e < 2; ++e)
+                            u[e] = i0 + 32 * e < r1 * 8 ? half[i0 + 32 * e] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            uint32_t *x = &u[e].x;
+                            bool bad = false;
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                if ((x[k] & 0x7f80u) == 0x7f80u) x[k] &= 0xffff0000u, bad = true;
+                                if ((x[k] & 0x7f800000u) == 0x7f800000u) x[k] &= 0x0000ffffu, bad = true;
+                            }
+                            if (bad) half[i0 + 32 * e] = u[e];
+                            found |= bad;
                         }
-                        if (bad) *at16 = u;
-                        found |= bad;
                     }
+                    for (int i = r1 * 8 + lane; i < kTile * 8; i += 32) half[i] = make_uint4(0, 0, 0, 0);
                 }
                 if (__any_sync(0xffffffffu, found) && lane == 0) *reinterpret_cast<volatile int32_t *>(&w.dirty) = 1;
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");

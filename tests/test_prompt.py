@@ -76,7 +76,7 @@ def test_append_is_validated(N):
     assert _append(N, L, tokens=0, k=None, v=None) == 0  # no rows: nothing to do
     size = lambda *a: L.voxzip_append_workspace_size(ctypes.byref(_desc(N)), *a)  # noqa: E731
     assert size(4, 500, 0) == 0 and size(3, 500, 0) == 256 == size(3, 500, 499)
-    assert size(3, 500, 6) == 0 == size(3, 5, 0)  # short sequences need none
+    assert size(3, 500, 60) == 0 == size(3, 5, 0)  # short sequences need none
     # more tokens of layers than a grid has blocks for
     assert _append(N, L, desc=_desc(N, layers=2 ** 23), count=2 ** 23, bytes=1 << 40, **{n: _rows(N, layer=8) for n in "qkv"}) == 2
 
