@@ -14,8 +14,9 @@
 // other tile's 1000 cycles of products cannot hide). Warps 16 and 19: a tile's matrix instructions (one warp for both
 // would wait for one tile's weights while the other's lie ready). Warp 17: items, and copies of their tiles into a ring of
 // K and V. Warp 18: what the mask hides of V.
-// 46 024 tokens, 32/4 heads, D = 128: 11.4 ms, 1 520 TFLOP/s, 0.78 of the measured burst rate, 0.88 of the sustained one:
-// the card is then at its power limit (1 390 W at 1 940 MHz, sw_power_cap), the tensor cores busy for 63% of the cycles.
+// 46 024 tokens, 32/4 heads, D = 128: 11.4 to 12.1 ms by box, up to 1 520 TFLOP/s, 0.78 of the measured burst rate and 0.88
+// of the sustained one: the card is then at its power limit (1 390 W at 1 940 MHz, sw_power_cap), the tensor cores busy
+// for 63% of the cycles.
 #include <algorithm>
 
 #include "evict_policy.cuh"  // once_per_device

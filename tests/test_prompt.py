@@ -164,3 +164,13 @@ def test_binding_rejects_what_the_kernels_cannot_address(V):
         N._rows([1], "k", d, 2)
     with pytest.raises(ValueError, match="needs q or k"):
         V.voxzip_rotary(d, V.RotaryDesc.make(64), torch.zeros(3, dtype=torch.int32))
+
+
+def test_every_wait_of_the_tensor_core_kernel_is_bounded():
+    """Barriers in shared memory are waited for by wait() and wait_warp() alone, which give up; there is no barrier of some
+    warps that another's give-up would leave waiting."""
+    import os
+    from paper_2608_08569_gb300 import build as B
+    s = open(os.path.join(B.CSRC, "prompt_attn_mma.cu")).read()
+    assert s.count("mbar_try_wait(") == 1 and "for (uint32_t i = 0; i < kPolls; ++i)" in s
+    assert "bar.sync" not in s and s.count("__syncthreads()") == 2
