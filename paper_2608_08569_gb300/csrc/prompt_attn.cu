@@ -339,11 +339,14 @@ PromptPlan prompt_plan(const voxzip_cache_desc &d, int32_t layer_count, int32_t 
     PromptPlan plan;
     plan.tile_tokens = mma ? 2 * (128 / G) : kRows / G;
     if (max_len <= 0 || max_len > d.capacity) max_len = d.capacity;
-    const int64_t ctas = tile_bound(tokens, d.batch, plan.tile_tokens) * d.kv_heads * layer_count;
+    const int64_t units = (int64_t)d.kv_heads * layer_count;
+    const int64_t bound = tile_bound(tokens, d.batch, plan.tile_tokens);
+    const int64_t hinted = max_rows > 0 && max_rows < tokens
+                               ? (int64_t)d.batch * ((max_rows + plan.tile_tokens - 1) / plan.tile_tokens) : bound;
     const int64_t key_tiles = (max_len + keys - 1) / keys;
     plan.splits = (int32_t)std::max<int64_t>(
-        1, std::min<int64_t>(per_sm * kSms / std::max<int64_t>(1, ctas), key_tiles / least));
-    plan.ctas = ctas * plan.splits;
+        1, std::min<int64_t>(per_sm * kSms / std::max<int64_t>(1, std::min(bound, hinted) * units), key_tiles / least));
+    plan.ctas = bound * units * plan.splits;
     const size_t rows = (size_t)layer_count * tokens * d.q_heads;
     plan.workspace = plan.splits == 1 ? 0 : plan.splits * rows * (d.head_dim * sizeof(float) + sizeof(float2));
     plan.workspace = (plan.workspace + 255) / 256 * 256;

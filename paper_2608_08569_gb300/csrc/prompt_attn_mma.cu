@@ -5,6 +5,7 @@
 //   S_t = Q_t K_j'           128 x 128, fp32, tensor memory
 //   P_t = 2^(c S_t - m - 8)  bf16, over S_t's columns; rounding it costs 2^-8 of each weight, as much as the output's
 //   O_t += P_t V_j           128 x D, fp32, tensor memory
+// (a tile's products run in the order in which its one warp issues them, so S_t's next logits may overwrite P_t).
 // m is a row's reference, not its running maximum: it moves (and O_t with it) only when the maximum has grown by more
 // than 2^8 over it, so weights stay at most 1 and nearly every tile leaves O_t to the tensor cores alone.
 // A CTA that is done takes the place of one that has not started: the copies and logits of its next tile begin while the
