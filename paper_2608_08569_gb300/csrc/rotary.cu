@@ -83,7 +83,7 @@ __device__ __forceinline__ int32_t sequence_of(const int32_t *off, int32_t B, in
         lo = next;
     }
     const int32_t b = lo - 1;
-    return b >= 0 && b < B && off[b] <= t && t < off[b + 1] ? b : -1;
+    return b >= 0 && b < B && off[b] >= 0 && off[b] <= t && t < off[b + 1] ? b : -1;
 }
 
 // A lane's part of its token's rows: two vectors, and the angles of their pairs. A warp has kLanes rows in hand at once.
@@ -326,8 +326,8 @@ __global__ void __launch_bounds__(32 * kUnitWarps) append_unit_kernel(const Plan
     ptx::grid_dependency_wait();
     const UnitIdx ui = unit_of(blockIdx.x / ctas, p.B, p.L, p.Hkv, p.layer_begin);
     const int32_t t0 = p.seq_off[ui.b], t1 = p.seq_off[ui.b + 1], first = rank * kUnitWarps + warp;
-    // (the first token's angles while the plan is made)
-    if (t0 >= 0 && t1 <= p.T && first < t1 - t0) token_angles(p, t0 + first, angles[warp]);
+    // (the first token's angles while the plan is made; the offsets may be anything, their difference too)
+    if (0 <= t0 && t0 <= t1 && t1 <= p.T && first < t1 - t0) token_angles(p, t0 + first, angles[warp]);
     if (rank == 0 && warp == 0) {
         const int32_t n = pp.len[ui.cache_unit];
         const bool ok = offsets_ok(p.seq_off, p.B, p.T);
