@@ -242,26 +242,25 @@ __global__ void __launch_bounds__(256) prompt_join_kernel(const PromptAttn p) {
     const int lane = threadIdx.x & 31;
     const int64_t rows = (int64_t)p.layer_count * p.T * p.Hq;
     const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-    if (row >= rows) return;
     // Rows of no sequence, or of one whose unit was skipped, were not written. (What this reads is older than the launch
     // before, which let this one start only after it had waited itself.)
-    const int32_t t = (int32_t)(row / p.Hq % p.T);
+    const int32_t t = (int32_t)(row / p.Hq % p.T), B = row < rows ? p.B : 0;
     const int l = (int)(row / p.Hq / p.T), h = (int)(row % p.Hq) / p.G;
     int32_t n = -1, seen = 0;
-    for (int32_t base = 0; base < p.B; base += 32) {
+    for (int32_t base = 0; base < B; base += 32) {
         const int32_t c = base + lane;
-        const int32_t o0 = c < p.B ? p.seq_off[c] : 0, o1 = c < p.B ? p.seq_off[c + 1] : 0;
-        const int32_t len = c < p.B ? p.len[((int64_t)c * p.L + p.layer_begin + l) * p.Hkv + h] : 0;
-        if (__any_sync(0xffffffffu, c < p.B && (o0 < 0 || o1 < o0 || o1 > p.T))) return;
-        const unsigned mine = __ballot_sync(0xffffffffu, c < p.B && o0 <= t && t < o1);
+        const int32_t o0 = c < B ? p.seq_off[c] : 0, o1 = c < B ? p.seq_off[c + 1] : 0;
+        const int32_t len = c < B ? p.len[((int64_t)c * p.L + p.layer_begin + l) * p.Hkv + h] : 0;
+        if (__any_sync(0xffffffffu, c < B && (o0 < 0 || o1 < o0 || o1 > p.T))) break;
+        const unsigned mine = __ballot_sync(0xffffffffu, c < B && o0 <= t && t < o1);
         if (mine) {
             n = __shfl_sync(0xffffffffu, len, __ffs(mine) - 1);
             seen = n - __shfl_sync(0xffffffffu, o1, __ffs(mine) - 1) + t + 1;  // keys
             break;
         }
     }
+    ptx::grid_dependency_wait();  // by every warp: this launch ends after the one before it
     if (n < 0 || n > p.C) return;
-    ptx::grid_dependency_wait();
     // a lane's split's statistics; of all of them the greatest maximum
     float m = -INFINITY;
     for (int s = lane; s < p.splits; s += 32) m = fmaxf(m, p.part_ml[s * rows + row].x);

@@ -157,6 +157,7 @@ prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
     Shared<D> &sh = *reinterpret_cast<Shared<D> *>(raw);
     const uint32_t front = (sizeof(Shared<D>) + ptx::smem_u32(raw) + 1023) / 1024 * 1024 - ptx::smem_u32(raw);
     if (front + C::kBytes > smem_bytes<D>()) {  // (never: the memory in front of raw is a multiple of 1024)
+        ptx::grid_dependency_wait();
         raise_status(p.status, VOXZIP_DEV_TIMEOUT);
         return;
     }
