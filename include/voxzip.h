@@ -546,7 +546,8 @@ voxzip_status voxzip_append_paged(const voxzip_cache_desc *desc, const voxzip_pa
                                   void *workspace, size_t workspace_bytes, voxzip_stream_t stream);
 
 /* Bytes of workspace voxzip_prompt_attention and its paged form need: 0 for a call whose rows fill the GPU (and if the
-   arguments are invalid); otherwise the parts of the keys that CTAs share out, before they are joined. */
+   arguments are invalid); otherwise the parts of the keys that CTAs share out, before they are joined: up to 21 MB (bf16) or
+   32 MB (fp32), whatever the hints say and however many rows belong to no sequence. */
 size_t voxzip_prompt_attention_workspace_size(const voxzip_cache_desc *desc, int32_t layer_count, int32_t tokens,
                                               int32_t max_rows, int32_t max_len);
 
@@ -560,7 +561,7 @@ size_t voxzip_prompt_attention_workspace_size(const voxzip_cache_desc *desc, int
  *   seq_off    [B + 1] device int32;  len [B][L][Hkv] device int32, read
  *   sm_scale   logit scale; <= 0 selects 1/sqrt(D)
  *   max_rows   host-side bound on the tokens of one sequence, or 0 (tokens);  max_len on the length of a unit, or 0
- *              (the capacity). Hints for the launch: others change which CTAs share the keys, not what is computed
+ *              (the capacity). Hints for the launch: wrong ones change which CTAs share the keys, not what is computed
  *   workspace  device scratch of voxzip_prompt_attention_workspace_size() bytes for the same arguments, 256-byte
  *              aligned; NULL where that is 0
  * Requires D in {64, 128}, G <= 16, and for bf16 at most 2^31 - 1 rows of K. Device errors: VOXZIP_DEV_CAPACITY (a length

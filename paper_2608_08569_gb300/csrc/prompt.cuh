@@ -54,27 +54,30 @@ struct PromptAttn {
     const int32_t *len;
     CacheRows cache;
     void *out;
-    float *part_o;   // [splits][layer_count * T * Hq][D], of splits > 1
-    float2 *part_ml; // [splits][layer_count * T * Hq]: running maximum (in units of log2) and sum
+    float *part_o;   // [splits][part_tiles][layer_count][Hkv][part_tokens * G][D], of splits > 1
+    float2 *part_ml; // the same rows: running maximum (in units of log2) and sum
     int32_t *status;
     float scale_log2;  // logit scale times log2(e)
     int32_t B, L, Hq, Hkv, G, C, T;
     int32_t layer_begin, layer_count;
     int32_t tile_tokens;  // tokens per CTA
-    int32_t tiles;        // bound on the CTAs of all sequences
-    int32_t splits;
+    int32_t tiles;        // bound on the tiles of all sequences
+    int32_t splits;       // pieces of the keys of the first part_tiles tiles, if they have up to part_tokens tokens
+    int32_t part_tiles, part_tokens;
     int64_t kv_rows;  // rows of the K and V tensors (checked builds)
 };
 
-// The i-th piece of a launch's work: its tile, split, kv-head and layer. The tiles that see the most keys come first, of
-// all heads, so that the last ones to start are short.
+// The i-th piece of a launch's work: its tile, split, kv-head and layer. Of one sequence the tiles that see the most keys
+// come first, of all heads, so that the last ones to start are short; sequences come in their order.
 struct CtaAt {
     int32_t x, split, h, l;
 };
 __device__ __forceinline__ CtaAt cta_at(const PromptAttn &p, int64_t piece) {
     const uint32_t units = p.Hkv * p.layer_count, i = (uint32_t)piece;
-    const uint32_t u = i % units, rest = i / units;
-    return CtaAt{(int32_t)(rest / p.splits), (int32_t)(rest % p.splits), (int32_t)(u % p.Hkv), (int32_t)(u / p.Hkv)};
+    const uint32_t u = i % units, rest = i / units, split = p.part_tiles * p.splits;
+    const bool whole = rest >= split;  // a tile behind those that the workspace has parts for
+    return CtaAt{(int32_t)(whole ? rest - split + p.part_tiles : rest / p.splits), (int32_t)(whole ? 0 : rest % p.splits),
+                 (int32_t)(u % p.Hkv), (int32_t)(u / p.Hkv)};
 }
 
 // A CTA's place: tile `x` of those of all sequences, in packed order, the last tile of a sequence first (it sees the
@@ -124,16 +127,31 @@ __device__ __forceinline__ bool find_tile(const PromptAttn &p, const CtaAt &cta,
     return false;
 }
 
+// Whether a tile's keys are shared out among CTAs. The workspace has parts for the tiles of a right hint of the rows; what a
+// wrong one did not foresee is done whole.
+__device__ __forceinline__ bool in_parts(const PromptAttn &p, int32_t x, const TileAt &at) {
+    return p.splits > 1 && x < p.part_tiles && at.rows <= p.part_tokens;
+}
+// Which of the [splits][part_tiles][layer_count][Hkv] a piece's part is; its rows are (token, head) pairs.
+__device__ __forceinline__ int32_t part_of(const PromptAttn &p, const CtaAt &cta) {
+    return ((cta.split * p.part_tiles + cta.x) * p.layer_count + cta.l) * p.Hkv + cta.h;
+}
+
 // Tiles of a launch at most: every sequence has ceil(m / per) of them.
 inline int64_t tile_bound(int64_t tokens, int64_t B, int per) {
     return (tokens + (B < tokens ? B : tokens) * (per - 1)) / per;
 }
 
+// Pieces of a launch, one to a CTA.
+inline int32_t pieces(const PromptAttn &p) {
+    return (p.tiles + p.part_tiles * (p.splits - 1)) * p.Hkv * p.layer_count;
+}
+
 cudaError_t launch_prompt_mma(const PromptAttn &p, int D, cudaStream_t stream);
 
 struct PromptPlan {
-    int32_t splits, tile_tokens;
-    int64_t ctas;
+    int32_t splits, tile_tokens, part_tiles, part_tokens;
+    int64_t tiles, ctas;
     size_t workspace;
 };
 PromptPlan prompt_plan(const voxzip_cache_desc &d, int32_t layer_count, int32_t tokens, int32_t max_rows,

@@ -104,11 +104,14 @@ __global__ void __launch_bounds__(256) prompt_rows_kernel(const PromptAttn p) {
         if (tid == 0) raise_status(p.status, VOXZIP_DEV_CAPACITY);
         return;
     }
+    const bool split = in_parts(p, cta.x, at);
+    if (!split && s > 0) return;
+    const int splits = split ? p.splits : 1;
     const int rows = at.rows * p.G;
     const int32_t first = n - at.m + at.before + 1;  // keys that the tile's first token sees (none if < 1)
     const int32_t most = max(0, first + at.rows - 1);
     // this split's keys
-    const int32_t tiles = (most + kKeys - 1) / kKeys, per = (tiles + p.splits - 1) / p.splits;
+    const int32_t tiles = (most + kKeys - 1) / kKeys, per = (tiles + splits - 1) / splits;
     const int32_t j0 = min(tiles, s * per), j1 = min(tiles, j0 + per);
 
     if (j0 < j1) {
@@ -223,12 +226,11 @@ __global__ void __launch_bounds__(256) prompt_rows_kernel(const PromptAttn p) {
         const int r = ty + 16 * i;
         if (r >= rows) continue;
         const int64_t row = ((int64_t)l * p.T + at.t0 + r / p.G) * p.Hq + h * p.G + r % p.G;
-        const int64_t all = (int64_t)p.layer_count * p.T * p.Hq;
-        const bool split = p.splits > 1;
+        const int32_t part = split ? part_of(p, cta) * (p.part_tokens * p.G) + r : 0;
         const float scale = split ? 1.f : lim[i] <= 0 ? 0.f : 1.f / sum[i];  // a row that sees nothing is 0
-        if (split && tx == 0) p.part_ml[s * all + row] = make_float2(mx[i], sum[i]);
+        if (split && tx == 0) p.part_ml[part] = make_float2(mx[i], sum[i]);
         if (split && j0 == j1) continue;  // the join does not read it
-        float *to = split ? p.part_o + (s * all + row) * D : static_cast<float *>(p.out) + row * D;
+        float *to = split ? p.part_o + (int64_t)part * D : static_cast<float *>(p.out) + row * D;
 #pragma unroll
         for (int c = 0; c < D / 64; ++c)
             *reinterpret_cast<float4 *>(&to[64 * c + 4 * tx]) =
@@ -236,34 +238,24 @@ __global__ void __launch_bounds__(256) prompt_rows_kernel(const PromptAttn p) {
     }
 }
 
-// Joins the splits: out = sum_s o_s 2^(m_s - m) / sum_s l_s 2^(m_s - m), m the greatest m_s. A warp per row.
+// Joins the splits: out = sum_s o_s 2^(m_s - m) / sum_s l_s 2^(m_s - m), m the greatest m_s. A warp per row of the parts.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) prompt_join_kernel(const PromptAttn p) {
     const int lane = threadIdx.x & 31;
-    const int64_t rows = (int64_t)p.layer_count * p.T * p.Hq;
-    const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-    // Rows of no sequence, or of one whose unit was skipped, were not written. (What this reads is older than the launch
-    // before, which let this one start only after it had waited itself.)
-    const int32_t t = (int32_t)(row / p.Hq % p.T), B = row < rows ? p.B : 0;
-    const int l = (int)(row / p.Hq / p.T), h = (int)(row % p.Hq) / p.G;
-    int32_t n = -1, seen = 0;
-    for (int32_t base = 0; base < B; base += 32) {
-        const int32_t c = base + lane;
-        const int32_t o0 = c < B ? p.seq_off[c] : 0, o1 = c < B ? p.seq_off[c + 1] : 0;
-        const int32_t len = c < B ? p.len[((int64_t)c * p.L + p.layer_begin + l) * p.Hkv + h] : 0;
-        if (__any_sync(0xffffffffu, c < B && (o0 < 0 || o1 < o0 || o1 > p.T))) break;
-        const unsigned mine = __ballot_sync(0xffffffffu, c < B && o0 <= t && t < o1);
-        if (mine) {
-            n = __shfl_sync(0xffffffffu, len, __ffs(mine) - 1);
-            seen = n - __shfl_sync(0xffffffffu, o1, __ffs(mine) - 1) + t + 1;  // keys
-            break;
-        }
-    }
+    const int32_t per = p.part_tokens * p.G, units = p.layer_count * p.Hkv, rows = p.part_tiles * units * per;
+    const int32_t at_row = blockIdx.x * 8 + (threadIdx.x >> 5), r = at_row % per, u = at_row / per % units;
+    const CtaAt cta{at_row / per / units, 0, u % p.Hkv, u / p.Hkv};
+    // (What this reads is older than the launch before, which let this one start only after it had waited itself.)
+    TileAt at;
+    const bool found = at_row < rows && find_tile(p, cta, at);
     ptx::grid_dependency_wait();  // by every warp: this launch ends after the one before it
-    if (n < 0 || n > p.C) return;
+    // rows of no tile, of a whole one, and of a unit that was skipped
+    if (!found || !in_parts(p, cta.x, at) || r >= at.rows * p.G || at.n < 0 || at.n > p.C) return;
+    const int32_t seen = at.n - at.m + at.before + r / p.G + 1;  // keys
+    const int64_t row = ((int64_t)cta.l * p.T + at.t0 + r / p.G) * p.Hq + cta.h * p.G + r % p.G;
     // a lane's split's statistics; of all of them the greatest maximum
     float m = -INFINITY;
-    for (int s = lane; s < p.splits; s += 32) m = fmaxf(m, p.part_ml[s * rows + row].x);
+    for (int s = lane; s < p.splits; s += 32) m = fmaxf(m, p.part_ml[s * rows + at_row].x);
 #pragma unroll
     for (int w = 16; w > 0; w >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, w));
     if (m == -INFINITY) m = 0.f;
@@ -273,9 +265,9 @@ __global__ void __launch_bounds__(256) prompt_join_kernel(const PromptAttn p) {
         float part[4][D / 32];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-            ml[u] = s0 + u < p.splits ? p.part_ml[(s0 + u) * rows + row] : make_float2(-INFINITY, 0.f);
+            ml[u] = s0 + u < p.splits ? p.part_ml[(s0 + u) * rows + at_row] : make_float2(-INFINITY, 0.f);
             const bool has = !(ml[u].x == -INFINITY && ml[u].y == 0.f);  // a key of this row
-            const float *from = p.part_o + ((s0 + u) * rows + row) * D + lane * (D / 32);
+            const float *from = p.part_o + (int64_t)((s0 + u) * rows + at_row) * D + lane * (D / 32);
 #pragma unroll
             for (int d = 0; d < D / 32; ++d) part[u][d] = has ? from[d] : 0.f;
         }
@@ -307,9 +299,9 @@ cudaLaunchConfig_t config(dim3 grid, int threads, size_t smem, cudaStream_t stre
 }
 
 template <typename T, int D> cudaError_t launch_join(const PromptAttn &p, cudaStream_t stream) {
-    const int64_t rows = (int64_t)p.layer_count * p.T * p.Hq;
+    const int rows = p.part_tiles * p.layer_count * p.Hkv * p.part_tokens * p.G;
     cudaLaunchAttribute attr[1];
-    cudaLaunchConfig_t cfg = config(dim3((unsigned)((rows + 7) / 8)), 256, 0, stream, attr);
+    cudaLaunchConfig_t cfg = config(dim3((rows + 7) / 8), 256, 0, stream, attr);
     return cudaLaunchKernelEx(&cfg, prompt_join_kernel<T, D>, p);
 }
 
@@ -320,7 +312,7 @@ template <int D> cudaError_t launch_rows(const PromptAttn &p, cudaStream_t strea
     });
     if (e != cudaSuccess) return e;
     cudaLaunchAttribute attr[1];
-    cudaLaunchConfig_t cfg = config(dim3(p.tiles * p.Hkv * p.layer_count * p.splits), 256, sizeof(Smem<D>), stream, attr);
+    cudaLaunchConfig_t cfg = config(dim3(pieces(p)), 256, sizeof(Smem<D>), stream, attr);
     e = cudaLaunchKernelEx(&cfg, prompt_rows_kernel<D>, p);
     return e != cudaSuccess || p.splits == 1 ? e : launch_join<float, D>(p, stream);
 }
@@ -339,16 +331,20 @@ PromptPlan prompt_plan(const voxzip_cache_desc &d, int32_t layer_count, int32_t 
     plan.tile_tokens = mma ? 2 * (128 / G) : kRows / G;
     if (max_len <= 0 || max_len > d.capacity) max_len = d.capacity;
     const int64_t units = (int64_t)d.kv_heads * layer_count;
-    const int64_t bound = tile_bound(tokens, d.batch, plan.tile_tokens);
-    const int64_t hinted = max_rows > 0 && max_rows < tokens
-                               ? (int64_t)d.batch * ((max_rows + plan.tile_tokens - 1) / plan.tile_tokens) : bound;
-    const int64_t key_tiles = (max_len + keys - 1) / keys;
+    const int64_t most = max_rows > 0 && max_rows < tokens ? max_rows : tokens;  // tokens of a sequence, by the hint
+    const int64_t hinted = d.batch * ((most + plan.tile_tokens - 1) / plan.tile_tokens);
+    const int64_t key_tiles = ((int64_t)max_len + keys - 1) / keys;
+    plan.tiles = tile_bound(tokens, d.batch, plan.tile_tokens);
+    const int64_t likely = std::min(plan.tiles, hinted);
     plan.splits = (int32_t)std::max<int64_t>(
-        1, std::min<int64_t>(per_sm * kSms / std::max<int64_t>(1, std::min(bound, hinted) * units), key_tiles / least));
-    plan.ctas = bound * units * plan.splits;
-    const size_t rows = (size_t)layer_count * tokens * d.q_heads;
-    plan.workspace = plan.splits == 1 ? 0 : plan.splits * rows * (d.head_dim * sizeof(float) + sizeof(float2));
-    plan.workspace = (plan.workspace + 255) / 256 * 256;
+        1, std::min<int64_t>(per_sm * kSms / std::max<int64_t>(1, likely * units), key_tiles / least));
+    // Parts are kept for the tiles that the hint allows, which are few where keys are shared out: they take up to
+    // per_sm * SMs * 256 rows (bf16 20 MB, fp32 30 MB), whatever the packed tensor holds besides and however wrong the hint.
+    plan.part_tiles = plan.splits == 1 ? 0 : (int32_t)likely;
+    plan.part_tokens = plan.splits == 1 ? 0 : (int32_t)std::min<int64_t>(plan.tile_tokens, most);
+    plan.ctas = (plan.tiles + (int64_t)plan.part_tiles * (plan.splits - 1)) * units;
+    const size_t rows = (size_t)plan.splits * plan.part_tiles * units * plan.part_tokens * G;
+    plan.workspace = (rows * (d.head_dim * sizeof(float) + sizeof(float2)) + 255) / 256 * 256;
     return plan;
 }
 
@@ -375,14 +371,16 @@ cudaError_t launch_prompt_attention(const voxzip_cache_desc &d, int32_t layer_be
     p.layer_begin = layer_begin;
     p.layer_count = layer_count;
     p.splits = plan.splits;
+    p.part_tiles = plan.part_tiles;
+    p.part_tokens = plan.part_tokens;
     p.kv_rows = cache.pool_rows;
     if (plan.splits > 1) {
-        const size_t rows = (size_t)layer_count * tokens * d.q_heads * plan.splits;
+        const size_t rows = (size_t)plan.splits * plan.part_tiles * layer_count * d.kv_heads * plan.part_tokens * p.G;
         p.part_o = static_cast<float *>(workspace);
         p.part_ml = reinterpret_cast<float2 *>(p.part_o + rows * d.head_dim);
     }
     p.tile_tokens = plan.tile_tokens;
-    p.tiles = (int32_t)tile_bound(tokens, d.batch, p.tile_tokens);
+    p.tiles = (int32_t)plan.tiles;
     if (d.dtype == VOXZIP_BF16) {
         const cudaError_t e = launch_prompt_mma(p, d.head_dim, stream);
         return e != cudaSuccess || p.splits == 1 ? e

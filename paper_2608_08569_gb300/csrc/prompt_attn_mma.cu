@@ -48,7 +48,8 @@ template <int D> struct Cfg {
 // A tile of the launch: 256 rows and the keys of its split.
 struct Item {
     int32_t valid;           // 0: there is none left
-    int32_t h, l, split, t0, rows;  // kv-head, layer; first packed token, tokens
+    int32_t h, l, t0, rows;  // kv-head, layer; first packed token, tokens
+    int32_t part;            // where its part goes, -1: all keys are its own
     int32_t first;           // keys that its first token sees (may be < 1)
     int32_t most;            // keys that its last one sees
     int32_t j0, end0, end1;  // key tiles [j0, end0) and [j0, end1) of the two row tiles
@@ -195,7 +196,7 @@ prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
 
     if (warp == kCopyWarp) {
         // ------------------------------------------------------------ items and copies
-        const int64_t items = (int64_t)p.tiles * p.splits * p.Hkv * p.layer_count;
+        const int64_t items = (int64_t)(p.tiles + p.part_tiles * (p.splits - 1)) * p.Hkv * p.layer_count;
         int issued = 0, queries = 0, given = 0;
         // Its own, then those of CTAs that have not started: the hardware gives them out in order.
         int64_t i = blockIdx.x;
@@ -221,13 +222,17 @@ prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     if (lane == 0) raise_status(p.status, VOXZIP_DEV_CAPACITY);
                     continue;
                 }
+                const bool split = in_parts(p, cta.x, at);
+                if (!split && cta.split > 0) continue;
+                const int splits = split ? p.splits : 1;
                 w.valid = 1;
-                w.h = cta.h, w.l = cta.l, w.split = cta.split, w.t0 = at.t0, w.rows = at.rows;
+                w.h = cta.h, w.l = cta.l, w.t0 = at.t0, w.rows = at.rows;
+                w.part = split ? part_of(p, cta) : -1;
                 w.cu = ((int64_t)at.b * p.L + p.layer_begin + cta.l) * p.Hkv + cta.h;
                 w.first = at.n - at.m + at.before + 1;
                 w.most = max(0, w.first + at.rows - 1);
                 // the keys of this split, of those that the last token sees; row tile 0 ends with its own last token's
-                const int32_t total = (w.most + kTile - 1) / kTile, per = (total + p.splits - 1) / p.splits;
+                const int32_t total = (w.most + kTile - 1) / kTile, per = (total + splits - 1) / splits;
                 w.j0 = min(total, cta.split * per);
                 const int32_t j1 = min(total, w.j0 + per);
                 const int32_t most0 = max(0, w.first + min(tile_tokens, at.rows) - 1);
@@ -576,9 +581,10 @@ prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
             const bool none = !any || lim <= 0;
             const float inv = none ? 0.f : 1.f / sum;
             const bool dirty = *reinterpret_cast<volatile int32_t *>(&sh.item[place].dirty);
-            const int64_t all = (int64_t)p.layer_count * p.T * p.Hq;
-            if (mine && p.splits > 1 && hf == 0)
-                p.part_ml[w.split * all + row] = make_float2(!any || m_row == -INFINITY ? -INFINITY : m_row + kSlack, any ? sum : 0.f);
+            const bool whole = w.part < 0;
+            const int32_t part = w.part * (p.part_tokens * p.G) + token * p.G + r % p.G;
+            if (mine && !whole && hf == 0)
+                p.part_ml[part] = make_float2(!any || m_row == -INFINITY ? -INFINITY : m_row + kSlack, any ? sum : 0.f);
             if (any) {
 #pragma unroll
                 for (int c = 0; c < kCols / 32; ++c) {
@@ -592,7 +598,7 @@ prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     }
                     if (!mine) continue;
                     const int col = hf * kCols + 32 * c;
-                    if (p.splits == 1)
+                    if (whole)
 #pragma unroll
                         for (int i = 0; i < 32; ++i) o[i] = none ? 0.f : o[i] * inv;
                     if (dirty) {  // the elements of V that the mask warp took out, for the rows that see them
@@ -608,8 +614,8 @@ prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                             }
                         }
                     }
-                    if (p.splits > 1) {
-                        float4 *to = reinterpret_cast<float4 *>(p.part_o + (w.split * all + row) * D + col);
+                    if (!whole) {
+                        float4 *to = reinterpret_cast<float4 *>(p.part_o + (int64_t)part * D + col);
 #pragma unroll
                         for (int i = 0; i < 8; ++i) to[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
                     } else {
@@ -620,7 +626,7 @@ prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                                                ptx::pack_bf16(o[8 * i + 4], o[8 * i + 5]), ptx::pack_bf16(o[8 * i + 6], o[8 * i + 7]));
                     }
                 }
-            } else if (mine && p.splits == 1) {
+            } else if (mine && whole) {
                 uint4 *to = reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) + row * D + hf * kCols);
                 for (int i = 0; i < kCols / 8; ++i) to[i] = make_uint4(0, 0, 0, 0);
             }
@@ -664,7 +670,7 @@ template <int D, bool kPaged> cudaError_t launch(const PromptAttn &p, cudaStream
         !make_cache_map(&mv, p.cache.v, p.cache.pool_rows, D, rows))
         return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(p.tiles * p.Hkv * p.layer_count * p.splits);
+    cfg.gridDim = dim3(pieces(p));
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = smem_bytes<D>();
     cfg.stream = stream;

@@ -18,3 +18,31 @@ def test_no_warp_leaves_before_the_launch_in_front():
             assert wait and not re.search(r"\breturn\b", before), (f, SOURCES[f].count("\n", 0, m.start()) + 1)
             found += 1
     assert found >= 6
+
+
+def _parts_limit(D, dtype):
+    """Pieces that are at work at once (bf16 one to an SM of 256 rows, fp32 three of 128), a row of fp32 sums and two
+    statistics each; on as many SMs as a device of this kind may have."""
+    rows = 256 if dtype is torch.bfloat16 else 3 * 128
+    return 160 * rows * (D * 4 + 8) + 256
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("D", [64, 128])
+def test_no_hint_makes_the_workspace_large(V, dtype, D):
+    """Padded rows with a right hint of the rows, and hints that are too low: a few tens of MB at most."""
+    limit = _parts_limit(D, dtype)
+    for Hq, H, L in ((32, 4, 1), (2, 1, 1), (5, 1, 1), (16, 16, 4), (32, 4, 48)):
+        for B in (1, 4, 77):
+            desc = V.CacheDesc(B, L, Hq, H, D, 46080, dtype)
+            for T in (1, 57, 228, 4096, 8012, 46024, 10 ** 6):
+                for max_rows in (0, 1, 2, 57, 300, 4000, T):
+                    for max_len in (0, 64, 2358):
+                        size = V.voxzip_prompt_attention_workspace_size(desc, L, T, max_rows, max_len)
+                        assert size <= limit, (Hq, H, L, B, T, max_rows, max_len, size)
+
+
+def test_the_workspace_does_not_grow_with_rows_of_no_sequence(V):
+    desc = V.CacheDesc(4, 1, 32, 4, 128, 2368, torch.bfloat16)
+    sizes = [V.voxzip_prompt_attention_workspace_size(desc, 1, T, 57, 2358) for T in (228, 4096, 46024)]
+    assert sizes[0] > 0 and sizes[0] == sizes[1] == sizes[2]

@@ -35,3 +35,44 @@ def test_offsets_whose_difference_does_not_fit(V, off, max_rows, paged):
         assert torch.equal(torch.nan_to_num(c[x].float()), torch.nan_to_num(t.float())), x
     P.attend(V, desc, c, 0, 1, q, off, torch.empty_like(q))
     assert V.voxzip_get_status() == V.DEV_BAD_SPANS
+
+
+def attend_rows(V, desc, c, ms, ns, T, **kw):
+    """Attention of packed rows of which the last ones belong to no sequence, against the plain form."""
+    D, G = desc.head_dim, desc.q_heads // desc.kv_heads
+    q = gen(sum(ms))(1, T, desc.q_heads, D).to(desc.dtype)
+    out = torch.full_like(q, 7.0)
+    P.attend(V, desc, c, 0, 1, q, offsets(ms), out, **kw)
+    assert (out[:, sum(ms):] == 7).all()
+    end = 0
+    for b, (m, n) in enumerate(zip(ms, ns)):
+        t = slice(end, end + m)
+        end += m
+        for h in range(desc.kv_heads):
+            k, v = P.unit_rows(c, b, 0, h, n)
+            heads = slice(h * G, (h + 1) * G)
+            want, mag, size = R.attention(q[0, t, heads], k, v, n - m + 1, 1 / math.sqrt(D))
+            close(out[0, t, heads], want, R.attention_bound(want, mag, size, n, D, desc.dtype), (b, h))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("paged", [False, True])
+def test_padded_rows_with_a_hint(V, dtype, paged):
+    """A buffer of fixed size, of which few rows are of sequences: their keys are shared out."""
+    ms, ns = [57, 0, 41, 57, 1], [1300, 40, 1000, 57, 900]
+    desc = V.CacheDesc(5, 1, 8, 2, 64, 1344, dtype)
+    kw = dict(max_rows=57, max_len=1300)
+    assert V.voxzip_prompt_attention_workspace_size(desc, 1, 4096, **kw) > 0
+    attend_rows(V, desc, fill(V, desc, ns, paged=paged), ms, ns, 4096, **kw)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("Hq,H,D", [(8, 2, 64), (5, 1, 128)])
+@pytest.mark.parametrize("ms", [[600, 40, 5], [5, 40, 600]])
+@pytest.mark.parametrize("hint", [1, 5, 10, 100])
+def test_a_hint_that_is_too_low(V, dtype, Hq, H, D, ms, hint):
+    """The workspace has parts for the tiles that the hint allows; tiles beyond them, and longer ones, are done whole."""
+    ns = [1500 if m == 600 else 1400 for m in ms]
+    desc = V.CacheDesc(3, 1, Hq, H, D, 1536, dtype)
+    assert V.voxzip_prompt_attention_workspace_size(desc, 1, 700, max_rows=hint) > 0
+    attend_rows(V, desc, fill(V, desc, ns), ms, ns, 700, max_rows=hint)
