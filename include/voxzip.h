@@ -321,7 +321,8 @@ voxzip_status voxzip_evict_ex(const voxzip_cache_desc *desc, int32_t layer_begin
  * decode loop runs without a host round trip and can be captured in a CUDA graph:
  *   - voxzip_paged_init gives unit u page u for slot 0 and stacks the rest as free;
  *   - voxzip_anchor_fuse_paged returns each unit's pages and takes the ones its stage-1 rows need;
- *   - voxzip_decode_step_paged takes a page when an append fills the unit's last one;
+ *   - voxzip_decode_step_paged takes a page when its row fills the unit's last one, voxzip_append_paged the ones that its
+ *     rows need;
  *   - voxzip_evict_paged returns the pages beyond the budget.
  * After every call a unit of length n holds the pages of slots [0, n] (the next append's slot
  * included) when the pool allowed it. A decode whose slot has no page, or a stage 1 the pool
@@ -535,9 +536,10 @@ voxzip_status voxzip_append(const voxzip_cache_desc *desc, const voxzip_rotary_d
                             int32_t *pos, int32_t *len, void *q_out, void *workspace, size_t workspace_bytes,
                             voxzip_stream_t stream);
 
-/* voxzip_append on a paged cache, in the descriptor's dtype: a unit takes the pages of its new rows and of the next
-   append's slot, or, with VOXZIP_DEV_CAPACITY, none and is skipped. A page index outside the pool sets
-   VOXZIP_DEV_CAPACITY too; its rows are not written. */
+/* voxzip_append on a paged cache, in the descriptor's dtype: a unit takes the pages of its new rows, or, with
+   VOXZIP_DEV_CAPACITY, none and is skipped. What the pool has left when all units have theirs goes to units whose next
+   append starts a page; one that gets none there is as long as the others, and its next decode step finds no page. A unit
+   without new rows takes none. A page index outside the pool sets VOXZIP_DEV_CAPACITY too; its rows are not written. */
 voxzip_status voxzip_append_paged(const voxzip_cache_desc *desc, const voxzip_paged_cache *paged,
                                   const voxzip_rotary_desc *rotary, int32_t layer_begin, int32_t layer_count,
                                   int32_t tokens, const voxzip_rows *q, const voxzip_rows *k, const voxzip_rows *v,

@@ -252,41 +252,34 @@ __device__ __forceinline__ int32_t take_pages(const PageView &pv, int32_t want) 
     return -1;
 }
 
+// What the page table holds, from the plan of an append to its last launch, where the unit's next slot wants a page. It is
+// taken when all units have those of their rows, so that no unit goes without for another one's next slot.
+constexpr int32_t kWantedPage = -2;
+
 // A warp: whether unit ui takes its sequence's m rows behind its n, and the pages that they need. 0, or the error.
 __device__ __forceinline__ uint32_t plan_unit(const PlanParams &p, int64_t cu, int32_t n, int32_t m) {
     const int lane = threadIdx.x & 31;
     if (n < 0 || n > p.C || m > p.C - n) return VOXZIP_DEV_CAPACITY;
-    if (!p.pv.table) return 0;
-    // pages of slots [n, n + m), and of n + m (the next append's), that the unit does not hold
+    if (!p.pv.table || m == 0) return 0;
+    // pages of slots [n, n + m) that the unit does not hold
     int32_t *table = p.pv.table + cu * p.pv.max_pages;
-    const int32_t p0 = n / kPageTokens, p1 = min(p.pv.max_pages, (n + m) / kPageTokens + 1);
-    const int32_t must = m > 0 ? (n + m - 1) / kPageTokens + 1 : p0;  // pages below it are needed now
-    int32_t missing = 0, needed = 0;
-    for (int32_t base = p0; base < p1; base += 32) {
-        const bool none = base + lane < p1 && table[base + lane] < 0;
-        missing += __popc(__ballot_sync(0xffffffffu, none));
-        needed += __popc(__ballot_sync(0xffffffffu, none && base + lane < must));
-    }
-    if (missing == 0) return 0;
-    int32_t at = -1, got = missing;
-    if (lane == 0) {
-        at = take_pages(p.pv, missing);
-        if (at < 0 && needed < missing) {
-            got = needed;
-            at = needed > 0 ? take_pages(p.pv, needed) : 0;
+    const int32_t p0 = n / kPageTokens, p1 = (n + m - 1) / kPageTokens + 1;
+    int32_t missing = 0;
+    for (int32_t base = p0; base < p1; base += 32)
+        missing += __popc(__ballot_sync(0xffffffffu, base + lane < p1 && table[base + lane] < 0));
+    if (missing > 0) {
+        int32_t at = lane == 0 ? take_pages(p.pv, missing) : 0;
+        at = __shfl_sync(0xffffffffu, at, 0);
+        if (at < 0) return VOXZIP_DEV_CAPACITY;
+        int32_t done = 0;  // the highest stack entry first, as take_page does
+        for (int32_t base = p0; base < p1; base += 32) {
+            const bool none = base + lane < p1 && table[base + lane] < 0;
+            const unsigned who = __ballot_sync(0xffffffffu, none);
+            if (none) table[base + lane] = p.pv.free_pages[at + missing - 1 - done - __popc(who & ((1u << lane) - 1u))];
+            done += __popc(who);
         }
     }
-    at = __shfl_sync(0xffffffffu, at, 0);
-    got = __shfl_sync(0xffffffffu, got, 0);
-    if (at < 0) return VOXZIP_DEV_CAPACITY;
-    int32_t done = 0;  // the highest stack entry first, as take_page does
-    for (int32_t base = p0; base < p1 && done < got; base += 32) {
-        const bool none = base + lane < p1 && table[base + lane] < 0;
-        const unsigned who = __ballot_sync(0xffffffffu, none);
-        const int32_t i = done + __popc(who & ((1u << lane) - 1u));
-        if (none && i < got) table[base + lane] = p.pv.free_pages[at + got - 1 - i];
-        done += __popc(who);
-    }
+    if (lane == 0 && (n + m) % kPageTokens == 0 && p1 < p.pv.max_pages && table[p1] < 0) table[p1] = kWantedPage;
     return 0;
 }
 
@@ -315,6 +308,19 @@ __global__ void __launch_bounds__(128) append_plan_kernel(const PlanParams p) {
     }
 }
 
+// A thread per unit, behind the rows: the pages of the next append's slots, as far as there are any.
+__global__ void __launch_bounds__(128) append_next_page_kernel(const PlanParams p) {
+    ptx::grid_dependency_wait();
+    ptx::launch_dependents();
+    const int32_t u = blockIdx.x * 128 + threadIdx.x;
+    if (u >= p.units) return;
+    const UnitIdx ui = unit_of(u, p.B, p.L, p.Hkv, p.layer_begin);
+    const int32_t n = p.len[ui.cache_unit];
+    if (n <= 0 || n % kPageTokens != 0 || n / kPageTokens >= p.pv.max_pages) return;
+    int32_t *entry = p.pv.table + ui.cache_unit * p.pv.max_pages + n / kPageTokens;
+    if (*entry == kWantedPage) *entry = take_page(p.pv);
+}
+
 // The same and the rows in one launch, for short sequences: a cluster per unit has its k and v rows and its query heads',
 // a token per warp. Its first CTA plans; the others read from its shared memory where the rows go.
 constexpr int kUnitWarps = 8, kUnitCtas = 8;
@@ -324,6 +330,7 @@ __global__ void __launch_bounds__(32 * kUnitWarps) append_unit_kernel(const Plan
     __shared__ int32_t plan[2];  // the unit's length before (-1: it is skipped), its rows
     const int warp = threadIdx.x >> 5, rank = blockIdx.x % ctas;
     ptx::grid_dependency_wait();
+    ptx::launch_dependents();
     const UnitIdx ui = unit_of(blockIdx.x / ctas, p.B, p.L, p.Hkv, p.layer_begin);
     const int32_t t0 = p.seq_off[ui.b], t1 = p.seq_off[ui.b + 1], first = rank * kUnitWarps + warp;
     // (the first token's angles while the plan is made; the offsets may be anything, their difference too)
@@ -474,6 +481,7 @@ cudaError_t launch_append(const voxzip_cache_desc &d, const RotaryTable *table, 
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
+    cudaError_t e;
     if (short_sequences(tokens, max_rows)) {
         const int bound = max_rows > 0 && max_rows < tokens ? max_rows : tokens;
         int ctas = 1;
@@ -487,16 +495,23 @@ cudaError_t launch_append(const voxzip_cache_desc &d, const RotaryTable *table, 
         cfg.attrs = both;
         cfg.numAttrs = 2;
         if (d.dtype == VOXZIP_BF16)
-            return d.head_dim == 128 ? cudaLaunchKernelEx(&cfg, append_unit_kernel<__nv_bfloat16, 128>, pp, p, ctas)
-                                     : cudaLaunchKernelEx(&cfg, append_unit_kernel<__nv_bfloat16, 64>, pp, p, ctas);
-        return d.head_dim == 128 ? cudaLaunchKernelEx(&cfg, append_unit_kernel<float, 128>, pp, p, ctas)
-                                 : cudaLaunchKernelEx(&cfg, append_unit_kernel<float, 64>, pp, p, ctas);
+            e = d.head_dim == 128 ? cudaLaunchKernelEx(&cfg, append_unit_kernel<__nv_bfloat16, 128>, pp, p, ctas)
+                                  : cudaLaunchKernelEx(&cfg, append_unit_kernel<__nv_bfloat16, 64>, pp, p, ctas);
+        else
+            e = d.head_dim == 128 ? cudaLaunchKernelEx(&cfg, append_unit_kernel<float, 128>, pp, p, ctas)
+                                  : cudaLaunchKernelEx(&cfg, append_unit_kernel<float, 64>, pp, p, ctas);
+    } else {
+        cfg.gridDim = dim3((pp.units + 3) / 4);
+        cfg.blockDim = dim3(128);
+        e = cudaLaunchKernelEx(&cfg, append_plan_kernel, pp);
+        if (e == cudaSuccess) e = launch_rows(d, p, true, stream);
     }
-    cfg.gridDim = dim3((pp.units + 3) / 4);
+    if (e != cudaSuccess || !cache.pv.table) return e;
+    cfg.gridDim = dim3((pp.units + 127) / 128);
     cfg.blockDim = dim3(128);
-    cudaError_t e = cudaLaunchKernelEx(&cfg, append_plan_kernel, pp);
-    if (e != cudaSuccess) return e;
-    return launch_rows(d, p, true, stream);
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, append_next_page_kernel, pp);
 }
 
 }  // namespace voxzip

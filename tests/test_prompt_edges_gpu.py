@@ -76,3 +76,43 @@ def test_a_hint_that_is_too_low(V, dtype, Hq, H, D, ms, hint):
     desc = V.CacheDesc(3, 1, Hq, H, D, 1536, dtype)
     assert V.voxzip_prompt_attention_workspace_size(desc, 1, 700, max_rows=hint) > 0
     attend_rows(V, desc, fill(V, desc, ns), ms, ns, 700, max_rows=hint)
+
+
+@pytest.mark.parametrize("max_rows", [60, 0])  # one launch, or a planning one
+@pytest.mark.parametrize("free", [1, 3, 9])
+@pytest.mark.parametrize("D,dtype", [(64, BF16), (128, F32)])
+def test_no_unit_takes_another_ones_page_for_its_next_slot(V, max_rows, free, D, dtype):
+    """Eight units fill their page and would like one for the next append's slot; the ninth needs one for its rows, and gets
+    it. What is left goes to the others; a unit without new rows takes none."""
+    ms, n0 = [54] * 8 + [60, 0], [10] * 9 + [64]
+    desc, k = V.CacheDesc(10, 1, 2, 1, D, 192, dtype), gen(1)(1, 492, 1, D).to(dtype)
+    c = fill(V, desc, n0, paged=True, pages=11 + free)
+    gone = int(c["page_table"][9, 0, 0, 1])
+    c["page_table"][9, 0, 0, 1] = -1  # (lost when the pool was empty)
+    assert int(c["free_count"]) == free
+    V.voxzip_append_paged(desc, c, 0, 1, k, k, torch.zeros(492, dtype=I32, device="cuda"), offsets(ms), max_rows=max_rows)
+    assert V.voxzip_get_status() == 0
+    assert c["len"].flatten().tolist() == [64] * 8 + [70, 64]
+    table = c["page_table"][:, 0, 0].cpu()
+    assert (table[:8, 1] >= 0).sum() == free - 1 and int(c["free_count"]) == 0
+    assert (table[:, 2] == -1).all() and (table[:8, 1] >= -1).all() and table[9, 1] == -1
+    held = table[table >= 0].tolist()
+    assert sorted(held + [gone]) == list(range(11 + free))
+    for b in range(9):
+        assert torch.equal(P.unit_rows(c, b, 0, 0, ms[b] + 10)[1][10:], k[0, sum(ms[:b]):sum(ms[:b + 1]), 0])
+
+
+@pytest.mark.parametrize("max_rows", [60, 0])
+def test_a_skipped_unit_takes_no_page(V, max_rows):
+    """Two units need more pages than there are: one gets them, the other none, nor one for its next slot."""
+    desc, k = V.CacheDesc(3, 1, 2, 1, 64, 192, BF16), gen(1)(1, 120, 1, 64).to(BF16)
+    c = fill(V, desc, [64, 64, 10], paged=True, pages=5)
+    lost = [int(c["page_table"][b, 0, 0, 1]) for b in (0, 1)]
+    c["page_table"][:2, 0, 0, 1] = -1
+    c["free_pages"][:1] = lost[0]
+    c["free_count"].fill_(1)
+    V.voxzip_append_paged(desc, c, 0, 1, k, k, torch.zeros(120, dtype=I32, device="cuda"), offsets([60, 60, 0]), max_rows=max_rows)
+    assert V.voxzip_get_status() == V.DEV_CAPACITY
+    got = c["len"].flatten().tolist()
+    assert sorted(got[:2]) == [64, 124] and int(c["free_count"]) == 0
+    assert sorted(c["page_table"][:2, 0, 0, 1].tolist()) == [-1, lost[0]] and (c["page_table"][:, 0, 0, 2] == -1).all()
