@@ -135,15 +135,17 @@ class Session:
                sm_scale: float = 0.0, layer_begin=0, layer_count=None, stream=None):
         """A turn's prompt for a layer range (all layers by default): packed rows q, k and v [layers][tokens][heads][D] of
         every sequence (see voxzip_append) join its units, k and q rotated on the way, and the queries' causal attention
-        over all rows goes to `out`. `max_rows` bounds the tokens of one sequence. With a rotation and no `q_out` the
-        rotated queries live for the call."""
+        over all rows goes to `out`. `max_rows` bounds the tokens of one sequence (0: the packed tokens do). With a rotation
+        and no `q_out` the rotated queries live for the call."""
         if self.kv_bits != 16:
             raise ValueError("extend needs a cache whose rows are in the descriptor's dtype (kv_bits=16)")
         if max_rows < 0:
             raise ValueError("max_rows must bound the tokens of a sequence")
         c = self.cache
         lc = self.desc.layers if layer_count is None else layer_count
-        longest = min(self.n_max + int(max_rows), self.desc.capacity)
+        tokens = k.shape[1]
+        max_rows = min(int(max_rows), tokens) if max_rows else tokens
+        longest = min(self.n_max + max_rows, self.desc.capacity)
         if rotary is not None and q_out is None:
             with torch.cuda.stream(_torch_stream(stream)):  # the launches' own, as it is what they use it on
                 q_out = torch.empty(q.shape, dtype=q.dtype, device=self.device)

@@ -116,3 +116,34 @@ def test_a_skipped_unit_takes_no_page(V, max_rows):
     got = c["len"].flatten().tolist()
     assert sorted(got[:2]) == [64, 124] and int(c["free_count"]) == 0
     assert sorted(c["page_table"][:2, 0, 0, 1].tolist()) == [-1, lost[0]] and (c["page_table"][:, 0, 0, 2] == -1).all()
+
+
+@pytest.mark.parametrize("paged", [False, True])
+@pytest.mark.parametrize("max_rows", [0, 10 ** 9])
+def test_a_turn_of_unknown_rows_and_the_steps_after_it(V, paged, max_rows):
+    """max_rows=0: the packed tokens bound a sequence's rows, so the next decode step knows how long a unit may be."""
+    from paper_2608_08569_gb300.session import Session
+    B, L, Hq, H, D = 2, 2, 4, 2, 64
+    desc, rnd = V.CacheDesc(B, L, Hq, H, D, 4096, BF16), gen(3)
+    s = Session(desc, [4096, 4096], 0.9, pages=800 if paged else None)
+    ms = [1500, 20]
+    for turn in range(2):
+        T = sum(ms)
+        qkv = rnd(L, T, Hq + 2 * H, D).to(BF16)
+        out = torch.empty(L, T, Hq, D, dtype=BF16, device="cuda")
+        s.extend(qkv[:, :, :Hq], qkv[:, :, Hq:Hq + H], qkv[:, :, Hq + H:], torch.arange(T, dtype=I32, device="cuda"), offsets(ms), out,
+                 max_rows=max_rows)
+        assert max(ms) * (turn + 1) + turn <= s.n_max <= T * (turn + 1) + turn  # (a step of one row lies between)
+        q, k, v = rnd(L, B, Hq, D).to(BF16), rnd(L, B, H, D).to(BF16), rnd(L, B, H, D).to(BF16)
+        got = torch.full_like(q, 7.0)
+        s.decode(q, k, v, torch.zeros(B, dtype=I32, device="cuda"), got)
+        assert V.voxzip_get_status() == 0
+        for b, m in enumerate(ms):
+            n = (turn + 1) * (m + 1)
+            assert (s.cache["len"][b] == n).all()
+            for l in range(L):
+                for h in range(H):
+                    kk, vv = P.unit_rows(s.cache, b, l, h, n)
+                    want, mag, size = R.attention(q[l, b, 2 * h:2 * h + 2][None], kk, vv, n, 0.125)
+                    # (the step adds its parts up in another order: twice the bound)
+                    close(got[l, b, 2 * h:2 * h + 2][None], want, 2 * R.attention_bound(want, mag, size, n, D, BF16))
