@@ -32,7 +32,12 @@ namespace {
 constexpr int kTile = 128;       // rows of a tile, keys of a tile
 constexpr int kMatrixWarp = 16, kCopyWarp = 17, kMaskWarp = 18, kMatrixWarp1 = 19;
 constexpr int kThreads = 20 * 32;
+// Polls of a wait: 4 s (3.8 us a poll; 8 ms in checked builds, shorter than the items of their tests).
+#ifdef VOXZIP_CHECKED
+constexpr uint32_t kPolls = 1u << 11;
+#else
 constexpr uint32_t kPolls = 1u << 20;
+#endif
 constexpr float kSlack = 8.f;    // growth of a row's maximum that its reference lets pass (log2)
 
 template <int D> struct Cfg {
@@ -67,7 +72,7 @@ template <int D> struct Shared {
     alignas(16) uint4 next;  // the hardware's answer: a CTA that need not start
     Item item[2];
     float sum[2][kTile], top[2][kTile];  // of the rows, when they are done
-    uint32_t tmem;
+    uint32_t tmem, steps;  // (of the copy warp)
     int dead;
 };
 
@@ -86,9 +91,27 @@ template <int D> __device__ __forceinline__ bool wait(Shared<D> &sh, uint64_t *b
     return false;
 }
 
+// The same for what takes as long as an item: it gives up when the copy warp has not come further for kPolls. (A tile's copy
+// waits for the products of the one whose place it takes, so while there are copies all warps advance, and an item has so
+// many tiles. Every other wait is for a few tiles.)
+template <int D> __device__ __forceinline__ bool wait_item(Shared<D> &sh, uint64_t *bar, uint32_t parity) {
+    uint32_t steps = 0;  // (before the first one)
+    for (uint32_t i = 0; i < kPolls / 64; ++i) {
+        if (ptx::mbar_wait_bounded(bar, parity, 64)) return true;
+        if (*reinterpret_cast<volatile int *>(&sh.dead)) return false;
+        const uint32_t now = *reinterpret_cast<volatile uint32_t *>(&sh.steps);
+        if (now != steps) steps = now, i = 0;
+    }
+    *reinterpret_cast<volatile int *>(&sh.dead) = 1;
+    return false;
+}
+
 // The same by all lanes of a warp, which stay together whatever each of them saw.
 template <int D> __device__ __forceinline__ bool wait_warp(Shared<D> &sh, uint64_t *bar, uint32_t parity) {
     return __all_sync(0xffffffffu, wait(sh, bar, parity));
+}
+template <int D> __device__ __forceinline__ bool wait_item_warp(Shared<D> &sh, uint64_t *bar, uint32_t parity) {
+    return __all_sync(0xffffffffu, wait_item(sh, bar, parity));
 }
 
 __device__ __forceinline__ float ex2(float x) {
@@ -178,6 +201,7 @@ prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         for (int i = 0; i < 8; ++i) ptx::mbar_init(&sh.pair[i], 2);
         ptx::fence_mbar_init();
         sh.dead = 0;
+        sh.steps = 0;
     }
     if (warp == kMatrixWarp) tc::alloc(&sh.tmem, C::kColumns);
     if (warp == kCopyWarp && lane == 0) {
@@ -200,9 +224,11 @@ prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         int issued = 0, queries = 0, given = 0;
         // Its own, then those of CTAs that have not started: the hardware gives them out in order.
         int64_t i = blockIdx.x;
-        uint32_t asked = 0;
+        uint32_t asked = 0, steps = 0;
         bool more = true;
+        auto step = [&] { *reinterpret_cast<volatile uint32_t *>(&sh.steps) = ++steps; };  // (lane 0)
         for (bool first = true; live; first = false) {
+            if (lane == 0) step();
             if (!first) {
                 if (!(live = wait_warp(sh, &sh.next_full, (asked - 1) & 1))) break;
                 more = canceled(&sh.next, &i);
@@ -305,6 +331,7 @@ prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                                                  &sh.full[slot]);
                         }
                         ++issued;
+                        step();
                         if (kv && j >= masked0) ptx::mbar_arrive(&sh.sent[place][j - masked0]);
                     }
                 }
@@ -347,7 +374,7 @@ prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         };
         for (int n = 0; live; ++n) {
             const int place = n & 1;
-            if (!(live = wait_warp(sh, &sh.item_full[place], n >> 1 & 1))) break;
+            if (!(live = wait_item_warp(sh, &sh.item_full[place], n >> 1 & 1))) break;
             const Item &w = sh.item[place];
             const int32_t valid = w.valid, j0 = w.j0, t_end = t ? w.end1 : w.end0, end = w.end(), masked0 = w.masked0();
             if (!valid) break;
@@ -412,14 +439,14 @@ prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         uint32_t sent_phase[2] = {0, 0};
         for (int n = 0; live; ++n) {
             const int place = n & 1;
-            if (!(live = wait_warp(sh, &sh.item_full[place], n >> 1 & 1))) break;
+            if (!(live = wait_item_warp(sh, &sh.item_full[place], n >> 1 & 1))) break;
             Item &w = sh.item[place];
             if (!w.valid) break;
             const int32_t j0 = w.j0, end = w.end(), masked0 = w.masked0();
             for (int32_t j = masked0; j < end && live; ++j) {
                 const int i = tiles_before + 2 * (j - j0) + 1, slot = i % C::kStages;
                 // only once its copy is asked for is a phase of the slot's barrier this tile's
-                live = wait_warp(sh, &sh.sent[place][j - masked0], sent_phase[place] >> (j - masked0) & 1) &&
+                live = wait_item_warp(sh, &sh.sent[place][j - masked0], sent_phase[place] >> (j - masked0) & 1) &&
                        wait_warp(sh, &sh.full[slot], i / C::kStages & 1);
                 if (!live) break;
                 uint8_t *tile = ring + slot * C::kTileBytes;
@@ -470,7 +497,7 @@ prompt_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         uint32_t logits_phase = 0, results_phase = 0;
         for (int n = 0; live; ++n) {
             const int place = n & 1;
-            if (!(live = wait_warp(sh, &sh.item_full[place], n >> 1 & 1))) break;
+            if (!(live = wait_item_warp(sh, &sh.item_full[place], n >> 1 & 1))) break;
             const Item &w = sh.item[place];
             if (!w.valid) break;
             const int32_t t_end = t ? w.end1 : w.end0, j0 = w.j0, masked0 = w.masked0();

@@ -147,3 +147,47 @@ def test_a_turn_of_unknown_rows_and_the_steps_after_it(V, paged, max_rows):
                     want, mag, size = R.attention(q[l, b, 2 * h:2 * h + 2][None], kk, vv, n, 0.125)
                     # (the step adds its parts up in another order: twice the bound)
                     close(got[l, b, 2 * h:2 * h + 2][None], want, 2 * R.attention_bound(want, mag, size, n, D, BF16))
+
+
+@pytest.mark.parametrize("paged", [False, True])
+def test_items_of_many_keys(V, paged):
+    """Whole tiles over 3 million rows (some 25 ms each): the mask warp waits for all keys in front of the masked ones, and
+    gives up only where nothing moves. (The checked build's waits are 8 ms.)"""
+    n, m, G, D = 3_000_000, 2432, 16, 64  # 152 tiles of 16 tokens: keys are not shared out
+    C = n + 64
+    desc, rnd = V.CacheDesc(1, 1, G, 1, D, C, BF16), gen(5)
+    c = dict(k=rnd(1, 1, 1, C, D).to(BF16), v=rnd(1, 1, 1, C, D).to(BF16))
+    at = slice(n - m, n)  # what a token sees of its own turn shows
+    c["v"][..., at, :] += 4.0
+    if paged:
+        pages = C // 64
+        table = torch.randperm(pages, generator=torch.Generator().manual_seed(1)).cuda()
+        pool = {x: torch.empty(pages, 64, D, dtype=BF16, device="cuda") for x in "kv"}
+        for x in "kv":
+            pool[x][table] = c[x].view(pages, 64, D)
+        z = torch.zeros(1, 1, 1, C, device="cuda")
+        pc = dict(k_pool=pool["k"], v_pool=pool["v"], page_table=table.to(I32).view(1, 1, 1, pages), free_pages=torch.zeros(pages, dtype=I32, device="cuda"),
+                  free_count=torch.zeros(1, dtype=I32, device="cuda"), score=z, pos=z.to(I32), pages=pages, max_pages=pages)
+    ln = torch.full((1, 1, 1), n, dtype=I32, device="cuda")
+    q = rnd(1, m, G, D).to(BF16)
+    q *= 3  # some keys outweigh the others
+    out = torch.full_like(q, 7.0)
+    assert V.voxzip_prompt_attention_workspace_size(desc, 1, m) == 0
+    if paged:
+        V.voxzip_prompt_attention_paged(desc, dict(pc, len=ln), 0, 1, q, offsets([m]), out)
+    else:
+        V.voxzip_prompt_attention(desc, 0, 1, q, offsets([m]), c["k"], c["v"], ln, out)
+    k, v = c["k"][0, 0, 0, :n], c["v"][0, 0, 0, :n]
+    for t in (0, 15, 16, 1203, 2430, 2431):
+        want, mag, size = R.attention(q[0, t:t + 1, ::5], k, v, n - m + 1 + t, 0.125)
+        close(out[0, t:t + 1, ::5], want, R.attention_bound(want, mag, size, n, D, BF16), t)
+
+
+@pytest.mark.skipif(os.environ.get("VOXZIP_CHECKED", "0") not in ("", "0"), reason="this is the checked run")
+def test_checked_build():
+    """The range-checked build, whose waits are short, gives the same and no bit of VOXZIP_DEV_BOUNDS."""
+    from paper_2608_08569_gb300.build import build_library
+    build_library(checked=True)
+    r = subprocess.run([sys.executable, "-m", "pytest", os.path.abspath(__file__), "-m", "gpu", "-x", "-q", "-p", "no:cacheprovider"],
+                       cwd=ROOT, env=dict(os.environ, VOXZIP_CHECKED="1"), capture_output=True, text=True, timeout=900)
+    assert r.returncode == 0, r.stdout[-4000:] + r.stderr[-2000:]
