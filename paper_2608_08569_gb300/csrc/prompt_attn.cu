@@ -7,14 +7,13 @@
 // pairs, so the G heads of a kv-head read its K and V once, and few tokens still fill a tile.
 #include <algorithm>
 
-#include "evict_policy.cuh"  // once_per_device
+#include "evict_policy.cuh"  // sm_count, once_per_device
 #include "prompt.cuh"
 #include "ptx.cuh"
 
 namespace voxzip {
 namespace {
 
-constexpr int kSms = 152;
 constexpr int kRows = 128, kKeys = 64;
 
 template <int D> struct Smem {
@@ -337,7 +336,7 @@ PromptPlan prompt_plan(const voxzip_cache_desc &d, int32_t layer_count, int32_t 
     plan.tiles = tile_bound(tokens, d.batch, plan.tile_tokens);
     const int64_t likely = std::min(plan.tiles, hinted);
     plan.splits = (int32_t)std::max<int64_t>(
-        1, std::min<int64_t>(per_sm * kSms / std::max<int64_t>(1, likely * units), key_tiles / least));
+        1, std::min<int64_t>((int64_t)per_sm * sm_count() / std::max<int64_t>(1, likely * units), key_tiles / least));
     // Parts are kept for the tiles that the hint allows, which are few where keys are shared out: they take up to
     // per_sm * SMs * 256 rows (bf16 20 MB, fp32 30 MB), whatever the packed tensor holds besides and however wrong the hint.
     plan.part_tiles = plan.splits == 1 ? 0 : (int32_t)likely;

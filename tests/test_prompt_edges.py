@@ -46,3 +46,9 @@ def test_the_workspace_does_not_grow_with_rows_of_no_sequence(V):
     desc = V.CacheDesc(4, 1, 32, 4, 128, 2368, torch.bfloat16)
     sizes = [V.voxzip_prompt_attention_workspace_size(desc, 1, T, 57, 2358) for T in (228, 4096, 46024)]
     assert sizes[0] > 0 and sizes[0] == sizes[1] == sizes[2]
+
+
+def test_launches_are_sized_by_the_device():
+    """As the row kernels' launches are: no number of SMs stands in the sources."""
+    for f in ("rotary.cu", "prompt_attn.cu", "prompt_attn_mma.cu"):
+        assert not re.search(r"\b1(48|52)\b(?! SM)", re.sub(r"//.*", "", SOURCES[f])), f
