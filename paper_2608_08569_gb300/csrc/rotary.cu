@@ -144,10 +144,10 @@ __device__ __forceinline__ void token_angles(const RowsParams &p, int32_t t, flo
 }
 
 // Where row `head` ([q heads][k heads][v heads]) of token t comes from and goes to; false for a unit that is skipped.
-// start: the unit's length before (kCache).
-template <typename T, int D, bool kCache>
+// start(h): the length before of the unit of kv-head h (kCache).
+template <typename T, int D, bool kCache, typename S>
 __device__ __forceinline__ bool locate(const RowsParams &p, int l, int32_t t, int32_t b, int32_t row, int head, int Hq,
-                                       const int32_t *start, const T *&from, T *&to, bool &turn) {
+                                       S start, const T *&from, T *&to, bool &turn) {
     const bool is_q = head < Hq, is_v = head >= Hq + p.Hkv;
     const int h = is_q ? head : is_v ? head - Hq - p.Hkv : head - Hq;
     const RowsView &src = is_q ? p.q : is_v ? p.v : p.k;
@@ -159,7 +159,7 @@ __device__ __forceinline__ bool locate(const RowsParams &p, int l, int32_t t, in
         to = static_cast<T *>(p.k_out) + (((int64_t)l * p.T + t) * p.Hkv + h) * D;
     } else {
         const int64_t cu = ((int64_t)b * p.L + p.layer_begin + l) * p.Hkv + h;
-        const int32_t at = start[h];
+        const int32_t at = start(h);
         if (at < 0) return false;
         const int32_t slot = at + row;
         const int64_t r = p.cache.pv.table ? paged_row(p.cache.pv, cu, slot) : cu * p.C + slot;
@@ -178,9 +178,9 @@ __device__ __forceinline__ bool locate(const RowsParams &p, int l, int32_t t, in
 }
 
 // Rows head(0), head(1), ... below n of a token, kUnroll of them on their way at once.
-template <typename T, int D, bool kCache, int kUnroll, typename F>
+template <typename T, int D, bool kCache, int kUnroll, typename S, typename F>
 __device__ __forceinline__ void move_rows(const RowsParams &p, const Part<T, D> &part, int l, int32_t t, int32_t b,
-                                          int32_t row, int Hq, const int32_t *start, int n, F head) {
+                                          int32_t row, int Hq, S start, int n, F head) {
     const int sub = (threadIdx.x & 31) / Part<T, D>::kItems;
     for (int i0 = sub; i0 < n; i0 += kUnroll * Part<T, D>::kLanes) {
         uint4 a[kUnroll], c[kUnroll];
@@ -229,8 +229,8 @@ __global__ void __launch_bounds__(32 * kWarps, 8) rows_kernel(const RowsParams p
     token_angles(p, t, angles[warp]);
     const Part<T, D> part(p.rot, angles[warp]);
     const int h0 = chunk * p.warp_heads;
-    move_rows<T, D, kCache, 2>(p, part, l, t, b, row, p.q.data ? p.Hq : 0,
-                               kCache ? p.start + ((int64_t)l * p.B + b) * p.Hkv : nullptr,
+    const int32_t *start = kCache ? p.start + ((int64_t)l * p.B + b) * p.Hkv : nullptr;
+    move_rows<T, D, kCache, 2>(p, part, l, t, b, row, p.q.data ? p.Hq : 0, [=](int h) { return start[h]; },
                                min(p.heads, h0 + p.warp_heads) - h0, [=](int i) { return h0 + i; });
 }
 
@@ -349,19 +349,19 @@ __global__ void __launch_bounds__(32 * kUnitWarps) append_unit_kernel(const Plan
     }
     ptx::cluster_arrive();
     ptx::cluster_wait();
-    int32_t start[1], rows;
+    int32_t start, rows;
     uint32_t at;
     asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(at) : "r"(ptx::smem_u32(plan)));
-    asm volatile("ld.shared::cluster.v2.s32 {%0, %1}, [%2];" : "=r"(start[0]), "=r"(rows) : "r"(at) : "memory");
+    asm volatile("ld.shared::cluster.v2.s32 {%0, %1}, [%2];" : "=r"(start), "=r"(rows) : "r"(at) : "memory");
     ptx::cluster_arrive();  // the first CTA's memory is read
     const int G = p.Hq / p.Hkv, Hq = p.q.data ? p.Hq : 0, nq = p.q.data ? G : 0;
     for (int32_t row = first; row < rows; row += ctas * kUnitWarps) {
         __syncwarp();
         if (row != first) token_angles(p, t0 + row, angles[warp]);
         const Part<T, D> part(p.rot, angles[warp]);
-        move_rows<T, D, true, 2>(p, part, ui.l_local, t0 + row, ui.b, row, Hq, start - ui.h, nq + 2, [=](int i) {
-            return i < nq ? ui.h * G + i : Hq + ui.h + (i - nq) * p.Hkv;
-        });
+        move_rows<T, D, true, 2>(
+            p, part, ui.l_local, t0 + row, ui.b, row, Hq, [=](int) { return start; }, nq + 2,
+            [=](int i) { return i < nq ? ui.h * G + i : Hq + ui.h + (i - nq) * p.Hkv; });
     }
     ptx::cluster_wait();
 }

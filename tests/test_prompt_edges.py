@@ -52,3 +52,8 @@ def test_launches_are_sized_by_the_device():
     """As the row kernels' launches are: no number of SMs stands in the sources."""
     for f in ("rotary.cu", "prompt_attn.cu", "prompt_attn_mma.cu"):
         assert not re.search(r"\b1(48|52)\b(?! SM)", re.sub(r"//.*", "", SOURCES[f])), f
+
+
+def test_no_pointer_in_front_of_an_array():
+    """A unit's rows are found by its own length, not by an array that would begin at its first kv-head."""
+    assert not re.search(r"\bstart - ", SOURCES["rotary.cu"])
