@@ -486,8 +486,9 @@ typedef enum {
 
 /* Rotary positions of the first R = rotary_dim channels of a head. Pair i (lo, hi) becomes
  *   (lo cos th - hi sin th, hi cos th + lo sin th),  th = position[axis[i]] * freq[i],
- * with th exact to 2^-60 of a turn for any int32 position, in fp32 and rounded once. Several axes (time, height and
- * width, say) give each pair a position of its own. */
+ * in fp32 and rounded once. th is taken modulo a turn within 2^-27 of a turn for any int32 position: |position| 2^-65 and 2^-32
+ * of it are the fixed point's, 2^-28 the fp32 argument's of cos and sin. Several axes (time, height and width, say) give each
+ * pair a position of its own. */
 typedef struct {
     int32_t rotary_dim;  /* R: a multiple of 16, at most the head dimension; channels from R on stay as they are */
     int32_t axes;        /* position axes, 1 to 255 */

@@ -15,7 +15,7 @@ namespace voxzip {
 constexpr int kMaxPairs = 64;  // rotated pairs of a head (D <= 128)
 
 // A rotation as the kernels take it, by value. A frequency is a fraction of a turn per position in 64-bit fixed
-// point, so position * frequency is exact modulo a turn for any 32-bit position.
+// point, so position * frequency modulo a turn is within |position| 2^-65 of one, 2^-34 for any 32-bit position.
 struct RotaryTable {
     uint64_t turns[kMaxPairs];
     uint8_t axis[kMaxPairs];

@@ -32,8 +32,8 @@ struct RowsParams {
     int32_t chunks;       // warps per token
 };
 
-// sin and cos of a fraction of a turn. The nearest quarter-turn is taken off in integers, so the argument of the
-// functions is small and exact to 2^-27 of a turn.
+// sin and cos of a fraction of a turn, of which the upper 32 bits are kept. The nearest quarter-turn is taken off in
+// integers, so the argument of the functions is small and rounded by 2^-28 of a turn at most.
 __device__ __forceinline__ float2 turn_cos_sin(uint64_t turns) {
     const int32_t t = (int32_t)(turns >> 32);  // [-1/2, 1/2) turns
     const uint32_t quarter = ((uint32_t)t + (1u << 29)) >> 30;

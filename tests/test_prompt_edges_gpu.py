@@ -191,3 +191,57 @@ def test_checked_build():
     r = subprocess.run([sys.executable, "-m", "pytest", os.path.abspath(__file__), "-m", "gpu", "-x", "-q", "-p", "no:cacheprovider"],
                        cwd=ROOT, env=dict(os.environ, VOXZIP_CHECKED="1"), capture_output=True, text=True, timeout=900)
     assert r.returncode == 0, r.stdout[-4000:] + r.stderr[-2000:]
+
+
+# ----------------------------------------------------------------------------- the bits that are kept
+
+def exact_cos_sin(positions, freqs):
+    """cos and sin of position * freq in 64 bits, the angle reduced in integers of 200 bits after the point: [T][pairs]."""
+    from fractions import Fraction
+    one = 1 << 200
+
+    def arctan_of_inverse(x):  # of 1 / x, by its series
+        total, term, k = 0, one // x, 0
+        while term:
+            total += (term if k % 2 == 0 else -term) // (2 * k + 1)
+            term //= x * x
+            k += 1
+        return total
+
+    two_pi = 8 * (4 * arctan_of_inverse(5) - arctan_of_inverse(239))  # Machin
+    turns = torch.empty(len(positions), len(freqs), dtype=torch.float64)
+    for j, f in enumerate(map(Fraction, freqs)):
+        step = f.numerator * one * one // (f.denominator * two_pi)  # of a turn, 2^-200 each
+        for i, p in enumerate(positions):
+            turns[i, j] = ((p * step + one // 2) % one - one // 2) / one
+    th = turns.cuda() * (2 * math.pi)
+    return th.cos(), th.sin()
+
+
+@pytest.mark.parametrize("pairing", ["halves", "adjacent"])
+@pytest.mark.parametrize("freqs", ["usual", "any"])
+def test_angles_at_any_position(V, pairing, freqs):
+    """fp32, positions over the whole range. With steps of 2^-24: the angle is 2^-28 + 2^-32 + 2^-34 of a turn off, 0.43 steps
+    of radians; CUDA's sincospif by a step of its result's (one unit in the last place, at most 2^-24 below 1); so each of
+    the two terms 1.43 steps of its channel's size, another for the products and one for their sum: 3.43 of |lo| + |hi|."""
+    D, T = 128, 300
+    if freqs == "usual":
+        r = V.RotaryDesc.make(D, 1e6, pairing=pairing)
+    else:
+        g = torch.Generator().manual_seed(1)
+        fs = (10.0 ** (torch.rand(64, generator=g, dtype=torch.float64) * 18 - 12)).tolist()  # 1e-12 to 1e6
+        r = V.RotaryDesc(tuple(x if i % 2 else -x for i, x in enumerate(fs[:61])) + (0.0, 1e6, -1e6), (), pairing)
+    desc, rnd = V.CacheDesc(1, 1, 4, 1, D, 8, F32), gen(9)
+    g = torch.Generator().manual_seed(2)
+    pos = torch.randint(-2 ** 31, 2 ** 31, (T,), generator=g).to(I32)
+    pos[:9] = torch.tensor([0, 1, -1, LOW, HIGH, LOW + 1, 46023, 10 ** 6, -46023], dtype=I32)
+    x, got = rnd(1, T, 4, D), torch.empty(1, T, 4, D, device="cuda")
+    V.voxzip_rotary(desc, r, pos.cuda(), q=x, q_out=got)
+    c, s = (t[None, :, None] for t in exact_cos_sin(pos.tolist(), r.freqs))
+    lo = torch.arange(64) if pairing == "halves" else torch.arange(0, D, 2)
+    hi = lo + (64 if pairing == "halves" else 1)
+    a, b = x.double()[..., lo], x.double()[..., hi]
+    for at, want in ((lo, a * c - b * s), (hi, b * c + a * s)):
+        steps = (got.double()[..., at] - want).abs() / (R.U32 * (a.abs() + b.abs()))
+        print("steps", float(steps.max()))
+        assert float(steps.max()) <= 3.43 + 1e-5
