@@ -510,7 +510,7 @@ voxzip_status voxzip_rotary(const voxzip_cache_desc *desc, const voxzip_rotary_d
                             void *q_out, void *k_out, voxzip_stream_t stream);
 
 /* Bytes of workspace voxzip_append and voxzip_append_paged need: 0 where max_rows (or tokens) says that every sequence
-   is short (and if the arguments are invalid). */
+   is short, and units are few (and if the arguments are invalid). Asked on the device of the call. */
 size_t voxzip_append_workspace_size(const voxzip_cache_desc *desc, int32_t layer_count, int32_t tokens,
                                     int32_t max_rows);
 

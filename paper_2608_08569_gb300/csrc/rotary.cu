@@ -321,7 +321,7 @@ __global__ void __launch_bounds__(128) append_next_page_kernel(const PlanParams 
     if (*entry == kWantedPage) *entry = take_page(p.pv);
 }
 
-// The same and the rows in one launch, for short sequences: a cluster per unit has its k and v rows and its query heads',
+// The same and the rows in one launch, for short sequences of few units: a cluster per unit has its k and v rows and its query heads',
 // a token per warp. Its first CTA plans; the others read from its shared memory where the rows go.
 constexpr int kUnitWarps = 8, kUnitCtas = 8;
 template <typename T, int D>
@@ -421,14 +421,21 @@ cudaError_t launch_rotary(const voxzip_cache_desc &d, const RotaryTable &table, 
     return launch_rows(d, p, false, stream);
 }
 
-// One launch for sequences of up to a token per warp of a cluster: four of up to 57 tokens take 28 us of an eager call
-// against 40, and no workspace, for 7.7 us of the GPU against 6.4. (Several tokens a warp: 15 us of the GPU.)
-inline bool short_sequences(int32_t tokens, int32_t max_rows) {
-    return (max_rows > 0 && max_rows < tokens ? max_rows : tokens) <= kUnitCtas * kUnitWarps;
+// CTAs of a unit's cluster where an append is one launch, 0 where it is a plan and the rows. One launch is 10 us less of an
+// eager call and needs no workspace, for sequences of up to a token per warp of a cluster (with several a warp it takes twice
+// as long) and units that all start at once: each computes its tokens' angles anew, and where clusters wait for places that
+// shows. 32/4 heads, D = 128, us of the GPU in one launch and in two: one layer of four sequences of 57 to 64 tokens (128
+// CTAs) 8.0 and 8.1; two layers 8.0 and 8.7; four 14.3 and 10.4; 12 of them 37 and 15; 48 of them 151 and 52.
+inline int unit_ctas(const voxzip_cache_desc &d, int32_t layer_count, int32_t tokens, int32_t max_rows) {
+    const int32_t bound = max_rows > 0 && max_rows < tokens ? max_rows : tokens;
+    if (bound > kUnitCtas * kUnitWarps) return 0;
+    int ctas = 1;
+    while (ctas * kUnitWarps < bound) ctas *= 2;
+    return (int64_t)d.batch * layer_count * d.kv_heads * ctas <= 2 * sm_count() ? ctas : 0;
 }
 
 size_t append_workspace_bytes(const voxzip_cache_desc &d, int32_t layer_count, int32_t tokens, int32_t max_rows) {
-    if (short_sequences(tokens, max_rows)) return 0;
+    if (unit_ctas(d, layer_count, tokens, max_rows) > 0) return 0;
     return ((size_t)d.batch * layer_count * d.kv_heads * sizeof(int32_t) + 255) / 256 * 256;
 }
 
@@ -482,10 +489,7 @@ cudaError_t launch_append(const voxzip_cache_desc &d, const RotaryTable *table, 
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     cudaError_t e;
-    if (short_sequences(tokens, max_rows)) {
-        const int bound = max_rows > 0 && max_rows < tokens ? max_rows : tokens;
-        int ctas = 1;
-        while (ctas * kUnitWarps < bound) ctas *= 2;
+    if (const int ctas = unit_ctas(d, layer_count, tokens, max_rows)) {
         cfg.gridDim = dim3(pp.units * ctas);
         cfg.blockDim = dim3(32 * kUnitWarps);
         cudaLaunchAttribute both[2] = {attr[0], {}};

@@ -57,3 +57,11 @@ def test_launches_are_sized_by_the_device():
 def test_no_pointer_in_front_of_an_array():
     """A unit's rows are found by its own length, not by an array that would begin at its first kv-head."""
     assert not re.search(r"\bstart - ", SOURCES["rotary.cu"])
+
+
+def test_short_appends_of_many_units_are_planned_first(V):
+    """One launch where all units' clusters start at once, a plan (4 bytes a unit) where they would wait for places."""
+    desc = V.CacheDesc(4, 48, 32, 4, 128, 256, torch.bfloat16)
+    size = lambda layers, rows: V.voxzip_append_workspace_size(desc, layers, 4 * rows, rows)  # noqa: E731
+    assert size(1, 57) == 0 == size(1, 64) == size(12, 8) == size(2, 64)
+    assert size(48, 57) == 48 * 16 * 4 == size(48, 64) and size(4, 64) == 256 == size(1, 65)

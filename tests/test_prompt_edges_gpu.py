@@ -245,3 +245,31 @@ def test_angles_at_any_position(V, pairing, freqs):
         steps = (got.double()[..., at] - want).abs() / (R.U32 * (a.abs() + b.abs()))
         print("steps", float(steps.max()))
         assert float(steps.max()) <= 3.43 + 1e-5
+
+
+@pytest.mark.parametrize("paged", [False, True])
+@pytest.mark.parametrize("D,dtype", [(128, BF16), (64, F32)])
+def test_a_short_append_of_all_layers_is_that_of_each(V, paged, D, dtype):
+    """Many units are planned before their rows, a layer's few take one launch: the same rows, to the bit."""
+    B, L, Hq, H, C, ms, n0 = 3, 24, 8, 4, 192, [57, 0, 40], [60, 3, 100]
+    desc, r, T = V.CacheDesc(B, L, Hq, H, D, C, dtype), V.RotaryDesc.make(64, sections=(16, 8, 8)), sum(ms) + 2
+    assert V.voxzip_append_workspace_size(desc, L, T, 57) > 0 == V.voxzip_append_workspace_size(desc, 1, T, 57)
+    qkv = gen(4)(L, T, (Hq + 2 * H) * D).to(dtype)
+    q, k, v = (x.unflatten(-1, (-1, D)) for x in qkv.split([Hq * D, H * D, H * D], -1))
+    pos, new_pos, off = P.positions_for(3, T), torch.arange(T, dtype=I32, device="cuda"), offsets(ms)
+    got = []
+    for step in (L, 1):
+        c, qo = fill(V, desc, n0, paged=paged), torch.zeros(L, T, Hq, D, dtype=dtype, device="cuda")
+        for l in range(0, L, step):
+            at = slice(l, l + step)
+            P.append(V, desc, c, l, step, k[at], v[at], new_pos, off, rotary=r, positions=pos, q=q[at], q_out=qo[at], max_rows=57)
+        if paged:
+            check_pages(desc, c)
+        got.append((c, qo))
+    (a, qa), (b, qb) = got
+    assert torch.equal(qa, qb) and all(torch.equal(a[x], b[x]) for x in ("len", "pos", "score"))
+    for s, (m, n) in enumerate(zip(ms, n0)):
+        for l in range(L):
+            for h in range(H):
+                for x, y in zip(P.unit_rows(a, s, l, h, n + m), P.unit_rows(b, s, l, h, n + m)):
+                    assert torch.equal(x, y)
