@@ -273,3 +273,101 @@ def test_a_short_append_of_all_layers_is_that_of_each(V, paged, D, dtype):
             for h in range(H):
                 for x, y in zip(P.unit_rows(a, s, l, h, n + m), P.unit_rows(b, s, l, h, n + m)):
                     assert torch.equal(x, y)
+
+
+# ----------------------------------------------------------------------------- many items, long page lists
+
+def plain(q, k, v, first, scale):
+    """q [m][G][D] over finite k, v [n][D]: as R.attention, all rows at once."""
+    m, n = len(q), len(k)
+    if n == 0:
+        z = torch.zeros(q.shape, dtype=torch.float64, device=q.device)
+        return z, z, z[..., 0]
+    q, k, v = q.double(), k.double(), v.double()
+    seen = torch.arange(n, device=q.device)[None] < (first + torch.arange(m, device=q.device))[:, None]
+    x = (torch.einsum("mgd,nd->mgn", q, k) * scale).masked_fill(~seen[:, None], -math.inf)
+    p = torch.softmax(x, -1).nan_to_num(0.0)  # (a row that sees nothing)
+    return p @ v, p @ v.abs(), (q.abs() @ k.abs().t()).amax(-1) * scale
+
+
+@pytest.mark.parametrize("paged", [False, True])
+@pytest.mark.parametrize("Hq,H,D,L", [(4, 4, 128, 16), (16, 2, 64, 8), (16, 4, 128, 5)])
+def test_several_items_for_each_cta(V, paged, Hq, H, D, L):
+    """Four hundred items and more: a CTA takes three or more of them, long and short ones, with one row tile alive or both,
+    of units without rows, of rows that see nothing, and with infinities that the mask hides from some."""
+    ms, G, C = [1, 300, 700, 0, 129, 513, 31], Hq // H, 1280
+    B, T, per = len(ms), sum(ms) + 3, 2 * (128 // G)
+    items = sum(-(-m // per) for m in ms) * H * L
+    assert items > 3 * 152
+    desc = V.CacheDesc(B, L, Hq, H, D, C, BF16)
+    assert V.voxzip_prompt_attention_workspace_size(desc, L, T) == 0
+    c = fill(V, desc, [C] * B, seed=D + G, paged=paged)
+    pick = torch.Generator().manual_seed(G)
+    ln = torch.empty(B, L, H, dtype=I32)
+    for b, m in enumerate(ms):
+        choice = torch.tensor([0, m // 2, m, min(C, m + 37), min(C, m + 128), 1200, C], dtype=I32)
+        ln[b] = choice[torch.randint(0, len(choice), (L, H), generator=pick)]
+    c["len"].copy_(ln)
+    dirty = {}  # of some units, an infinity in V's channel 3 in the middle of the turn
+    for b, m in enumerate(ms):
+        for l in range(0, L, 2):
+            n = int(ln[b, l, 0])
+            if m > 20 and n >= m:
+                slot = n - m // 2
+                dirty[b, l, 0] = slot
+                if paged:
+                    c["v_pool"][int(c["page_table"][b, l, 0, slot // 64]), slot % 64, 3] = math.inf
+                else:
+                    c["v"][b, l, 0, slot, 3] = math.inf
+    q = gen(31)(L, T, Hq, D).to(BF16)
+    out = torch.full_like(q, 7.0)
+    P.attend(V, desc, c, 0, L, q, offsets(ms), out)
+    assert V.voxzip_get_status() == 0 and (out[:, sum(ms):] == 7).all()
+    end = 0
+    for b, m in enumerate(ms):
+        t = slice(end, end + m)
+        end += m
+        for l in range(L):
+            for h in range(H):
+                n, heads = int(ln[b, l, h]), slice(h * G, (h + 1) * G)
+                k, v = P.unit_rows(c, b, l, h, n)
+                got, slot = out[l, t, heads], dirty.get((b, l, h))
+                if slot is not None:
+                    sees = torch.arange(n - m, n, device="cuda") >= slot
+                    assert (got[sees][..., 3] == math.inf).all() and torch.isfinite(got[~sees]).all()
+                    k, v, got = k.clone(), v.clone(), got.clone()
+                    v[slot, 3] = 0.0
+                want, mag, size = plain(q[l, t, heads], k, v, n - m + 1, D ** -0.5)
+                if slot is not None:
+                    got[..., 3][sees] = want[..., 3][sees].to(BF16)
+                close(got, want, R.attention_bound(want, mag, size, n, D, BF16), (b, l, h))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("L", [1, 10])  # keys shared out, at page offsets of any kind, and whole tiles
+def test_units_of_many_pages(V, dtype, L):
+    """70 shuffled pages a unit, of which a turn of 2 300 rows takes 36 from the middle of the 34th on."""
+    H, G, D, n0, m = 16, 1, 64, 33 * 64 + 29, 2300
+    C, n = 72 * 64, n0 + m
+    desc, rnd = V.CacheDesc(1, L, H * G, H, D, C, dtype), gen(L)
+    c = fill(V, desc, [n0], seed=3, paged=True)
+    assert int(c["page_table"].max()) > 64
+    k, v = rnd(L, m, H, D).to(dtype), rnd(L, m, H, D).to(dtype)
+    V.voxzip_append_paged(desc, c, 0, L, k, v, torch.arange(m, dtype=I32, device="cuda"), offsets([m]))
+    assert V.voxzip_get_status() == 0 and (c["len"] == n).all()
+    check_pages(desc, c)
+    for l in range(L):
+        for h in range(H):
+            kk, vv = P.unit_rows(c, 0, l, h, n)
+            assert torch.equal(kk[n0:], k[l, :, h]) and torch.equal(vv[n0:], v[l, :, h])
+    last = 40  # of the turn's tokens attend
+    q, off = rnd(L, last, H * G, D).to(dtype), offsets([last])
+    out = torch.empty_like(q)
+    shared = V.voxzip_prompt_attention_workspace_size(desc, L, last) > 0
+    assert shared == (L == 1 or dtype is F32)
+    V.voxzip_prompt_attention_paged(desc, c, 0, L, q, off, out)
+    for l in range(0, L, 3):
+        for h in range(H):
+            kk, vv = P.unit_rows(c, 0, l, h, n)
+            want, mag, size = plain(q[l, :, h:h + 1], kk, vv, n - last + 1, D ** -0.5)
+            close(out[l, :, h:h + 1], want, R.attention_bound(want, mag, size, n, D, dtype), (l, h))
