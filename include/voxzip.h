@@ -559,7 +559,8 @@ size_t voxzip_prompt_attention_workspace_size(const voxzip_cache_desc *desc, int
  * token i's queries see slots [0, n - m + i] of their kv-head's unit, all kept rows and the turn's own up to it:
  *   out = softmax(scale * q K^T) V.
  * A token that sees no slot (n - m + i < 0) gets 0. What lies in slots that a token does not see, infinities and NaN
- * too, has no part in its result. Scores do not change: they follow the decode steps.
+ * too, has no part in its result. Scores do not change: they follow the decode steps. Logits and sums are fp32; with bf16
+ * rows each weight is rounded to bf16 before it meets V, as in a decode step.
  *   q          rows of q_heads heads, rotated;  out [layer_count][tokens][Hq][D]
  *   seq_off    [B + 1] device int32;  len [B][L][Hkv] device int32, read
  *   sm_scale   logit scale; <= 0 selects 1/sqrt(D)

@@ -321,8 +321,9 @@ template <int D> cudaError_t launch_rows(const PromptAttn &p, cudaStream_t strea
 PromptPlan prompt_plan(const voxzip_cache_desc &d, int32_t layer_count, int32_t tokens, int32_t max_rows,
                        int32_t max_len) {
     // Rows and keys of a CTA's tiles. Keys are shared out where there are fewer CTAs than the GPU takes at once. fp32
-    // (a key tile is 9 us of a CTA's work): up to three for each SM, as the last rows of a prompt see twice the keys of
-    // the average one (631 tokens, 32/4 heads: 164 us unsplit); bf16 (1.5 us): one, with two key tiles or more.
+    // (a key tile is 13.6 us of a CTA's work at the 47 TFLOP/s of a long prompt): up to three for each SM, as the last rows
+    // of a prompt see twice the keys of the average one (631 tokens, 32/4 heads: 118 us, 164 unsplit); bf16 (1.5 us): one,
+    // with two key tiles or more.
     const int G = d.q_heads / d.kv_heads;
     const bool mma = d.dtype == VOXZIP_BF16;
     const int keys = mma ? 128 : kKeys, least = mma ? 2 : 1, per_sm = mma ? 1 : 3;

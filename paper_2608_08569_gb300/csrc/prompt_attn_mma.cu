@@ -3,19 +3,20 @@
 // A CTA has 256 rows ((token, head of the group) pairs) of a unit as two tiles of 128, which take turns on the tensor
 // cores: while a warpgroup turns one tile's logits into weights, the other tile's products run.
 //   S_t = Q_t K_j'           128 x 128, fp32, tensor memory
-//   P_t = 2^(c S_t - m - 8)  bf16, over S_t's columns; rounding it costs 2^-8 of each weight, as much as the output's
+//   P_t = 2^(c S_t - m - 8)  bf16, over S_t's columns; rounding it costs 2^-8 of each weight, as much as the output's (V is
+//                            bf16 and both operands are of one type; a row's sum is of the weights before it)
 //   O_t += P_t V_j           128 x D, fp32, tensor memory
 // (a tile's products run in the order in which its one warp issues them, so S_t's next logits may overwrite P_t).
 // m is a row's reference, not its running maximum: it moves (and O_t with it) only when the maximum has grown by more
 // than 2^8 over it, so weights stay at most 1 and nearly every tile leaves O_t to the tensor cores alone.
 // A CTA that is done takes the place of one that has not started: the copies and logits of its next tile begin while the
-// results of the last are on their way out (10-min prompt 380 us against 397, 32 ragged ones 5.0 ms against 5.3; a fixed
+// results of the last are on their way out (10-min prompt without outlier channels of K 380 us against 397, 32 ragged ones 5.0 ms against 5.3; a fixed
 // share for each CTA 401 us).
 // Warps 0-7 and 8-15: a tile's weights, a quarter of two rows per thread (a thread per row took 1500 cycles, which the
 // other tile's 1000 cycles of products cannot hide). Warps 16 and 19: a tile's matrix instructions (one warp for both
 // would wait for one tile's weights while the other's lie ready). Warp 17: items, and copies of their tiles into a ring of
 // K and V. Warp 18: what the mask hides of V.
-// 46 024 tokens, 32/4 heads, D = 128: 11.4 to 12.1 ms by box, up to 1 520 TFLOP/s, 0.78 of the measured burst rate and 0.88
+// 46 024 tokens, 32/4 heads, D = 128: 11.4 to 12.3 ms by box, up to 1 520 TFLOP/s, 0.78 of the measured burst rate and 0.88
 // of the sustained one: the card is then at its power limit (1 390 W at 1 940 MHz, sw_power_cap), the tensor cores busy
 // for 63% of the cycles.
 #include <algorithm>
