@@ -33,11 +33,14 @@ namespace {
 constexpr int kTile = 128;       // rows of a tile, keys of a tile
 constexpr int kMatrixWarp = 16, kCopyWarp = 17, kMaskWarp = 18, kMatrixWarp1 = 19;
 constexpr int kThreads = 20 * 32;
-// Polls of a wait: 4 s (3.8 us a poll; 8 ms in checked builds, shorter than the items of their tests).
-#ifdef VOXZIP_CHECKED
-constexpr uint32_t kPolls = 1u << 11;
-#else
+// Polls of a wait for a few tiles: 4 s by a whole warp (7 850 cycles a poll), 38 ms by one lane, which is not suspended (70).
+// The longest, for the results of an item in which the mask hides infinities, takes 0.1 ms.
 constexpr uint32_t kPolls = 1u << 20;
+// Those of a wait for an item without any step of the copies: 4 s, in checked builds 8 ms, shorter than their tests' items.
+#ifdef VOXZIP_CHECKED
+constexpr uint32_t kItemPolls = 1u << 11;
+#else
+constexpr uint32_t kItemPolls = 1u << 20;
 #endif
 constexpr float kSlack = 8.f;    // growth of a row's maximum that its reference lets pass (log2)
 
@@ -92,12 +95,12 @@ template <int D> __device__ __forceinline__ bool wait(Shared<D> &sh, uint64_t *b
     return false;
 }
 
-// The same for what takes as long as an item: it gives up when the copy warp has not come further for kPolls. (A tile's copy
+// The same for what takes as long as an item: it gives up when the copy warp has not come further for kItemPolls. (A tile's copy
 // waits for the products of the one whose place it takes, so while there are copies all warps advance, and an item has so
 // many tiles. Every other wait is for a few tiles.)
 template <int D> __device__ __forceinline__ bool wait_item(Shared<D> &sh, uint64_t *bar, uint32_t parity) {
     uint32_t steps = 0;  // (before the first one)
-    for (uint32_t i = 0; i < kPolls / 64; ++i) {
+    for (uint32_t i = 0; i < kItemPolls / 64; ++i) {
         if (ptx::mbar_wait_bounded(bar, parity, 64)) return true;
         if (*reinterpret_cast<volatile int *>(&sh.dead)) return false;
         const uint32_t now = *reinterpret_cast<volatile uint32_t *>(&sh.steps);
