@@ -550,7 +550,7 @@ voxzip_status voxzip_append_paged(const voxzip_cache_desc *desc, const voxzip_pa
 
 /* Bytes of workspace voxzip_prompt_attention and its paged form need: 0 for a call whose rows fill the GPU (and if the
    arguments are invalid); otherwise the parts of the keys that CTAs share out, before they are joined: up to 21 MB (bf16) or
-   32 MB (fp32), whatever the hints say and however many rows belong to no sequence. */
+   32 MB (fp32), whatever the hints say and however many rows belong to no sequence. Asked on the device of the call. */
 size_t voxzip_prompt_attention_workspace_size(const voxzip_cache_desc *desc, int32_t layer_count, int32_t tokens,
                                               int32_t max_rows, int32_t max_len);
 

@@ -318,7 +318,9 @@ __global__ void __launch_bounds__(128) append_next_page_kernel(const PlanParams 
     const int32_t n = p.len[ui.cache_unit];
     if (n <= 0 || n % kPageTokens != 0 || n / kPageTokens >= p.pv.max_pages) return;
     int32_t *entry = p.pv.table + ui.cache_unit * p.pv.max_pages + n / kPageTokens;
-    if (*entry == kWantedPage) *entry = take_page(p.pv);
+    if (*entry != kWantedPage) return;
+    const int32_t at = take_pages(p.pv, 1);  // (never below the count that an append beside this one reads)
+    *entry = at >= 0 ? p.pv.free_pages[at] : -1;
 }
 
 // The same and the rows in one launch, for short sequences of few units: a cluster per unit has its k and v rows and its query heads',
