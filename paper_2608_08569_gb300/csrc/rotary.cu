@@ -323,8 +323,8 @@ __global__ void __launch_bounds__(128) append_next_page_kernel(const PlanParams 
     *entry = at >= 0 ? p.pv.free_pages[at] : -1;
 }
 
-// The same and the rows in one launch, for short sequences of few units: a cluster per unit has its k and v rows and its query heads',
-// a token per warp. Its first CTA plans; the others read from its shared memory where the rows go.
+// The same and the rows in one launch, for short sequences of few units: a cluster per unit has its k and v rows and its
+// query heads', a token per warp. Its first CTA plans; the others read from its shared memory where the rows go.
 constexpr int kUnitWarps = 8, kUnitCtas = 8;
 template <typename T, int D>
 __global__ void __launch_bounds__(32 * kUnitWarps) append_unit_kernel(const PlanParams pp, const RowsParams p, int ctas) {
